@@ -1,0 +1,249 @@
+// pf_norm.cu -- residual addition, root-mean-square norm and 8-bit output in one pass.
+//
+//   a = x + r,  y = a * rsqrt(mean(a^2) + eps) * w,  s_g = max_g |y| / 448,  q = e4m3(y / s_g)
+//
+// One block per row: the row is read once and stays in registers (fp32) between the sum of squares, the maxima and the
+// stores, so the traffic is what the outputs need and nothing else: the kernel is bound by HBM for many rows and by the
+// chain load -> reduce -> store for few.  A thread owns runs of 8 neighbouring elements (16-byte loads of 16-bit types,
+// 8-byte stores of q); 16 lanes own one 128-element scale group, so its maximum takes four shuffles and no barrier.
+#include <math.h>
+
+#include "pf_ops.cuh"
+
+namespace pf {
+
+struct NormArgs {
+    const void *x, *res, *w;
+    void *sum, *y;
+    uint8_t *q;
+    float *scale;
+    int64_t xs, rs, ss, ys;   // row strides, elements
+    int H, groups;            // groups: scales per row
+    float eps;
+};
+
+template <typename T, bool ALIGNED>
+__device__ __forceinline__ void load8(const T *p, int n, float (&v)[8])
+{
+    if (ALIGNED) {
+        const uint4 u = *reinterpret_cast<const uint4 *>(p);
+        const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+        for (int i = 0; i < 4; i++) {
+            const float2 f = pair_to_f32<T>(w[i]);
+            v[2 * i] = f.x;
+            v[2 * i + 1] = f.y;
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; i++) v[i] = i < n ? pair_to_f32<T>((uint32_t)p[i].bits).x : 0.f;
+    }
+}
+template <>
+__device__ __forceinline__ void load8<float, true>(const float *p, int, float (&v)[8])
+{
+    const float4 a = reinterpret_cast<const float4 *>(p)[0], b = reinterpret_cast<const float4 *>(p)[1];
+    v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w;
+    v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+}
+template <>
+__device__ __forceinline__ void load8<float, false>(const float *p, int n, float (&v)[8])
+{
+#pragma unroll
+    for (int i = 0; i < 8; i++) v[i] = i < n ? p[i] : 0.f;
+}
+template <typename T, bool ALIGNED>
+__device__ __forceinline__ void store8(T *p, int n, const float (&v)[8])
+{
+    if (ALIGNED) {
+        *reinterpret_cast<uint4 *>(p) = make_uint4(pair_of_f32<T>(v[0], v[1]), pair_of_f32<T>(v[2], v[3]),
+                                                   pair_of_f32<T>(v[4], v[5]), pair_of_f32<T>(v[6], v[7]));
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; i++)
+            if (i < n) p[i].bits = (uint16_t)pair_of_f32<T>(v[i], 0.f);
+    }
+}
+template <>
+__device__ __forceinline__ void store8<float, true>(float *p, int, const float (&v)[8])
+{
+    reinterpret_cast<float4 *>(p)[0] = make_float4(v[0], v[1], v[2], v[3]);
+    reinterpret_cast<float4 *>(p)[1] = make_float4(v[4], v[5], v[6], v[7]);
+}
+template <>
+__device__ __forceinline__ void store8<float, false>(float *p, int n, const float (&v)[8])
+{
+#pragma unroll
+    for (int i = 0; i < 8; i++)
+        if (i < n) p[i] = v[i];
+}
+
+template <bool MAX>
+__device__ __forceinline__ float warp_all(float v)
+{
+#pragma unroll
+    for (int m = 16; m; m >>= 1) {
+        const float o = __shfl_xor_sync(0xFFFFFFFFu, v, m);
+        v = MAX ? fmaxf(v, o) : v + o;
+    }
+    return v;
+}
+// every thread gets the block's sum / maximum; `part` holds one word per warp and is used once per call site
+template <int THREADS, bool MAX>
+__device__ __forceinline__ float block_all(float v, float *part)
+{
+    v = warp_all<MAX>(v);
+    if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = v;
+    __syncthreads();
+    const int lane = threadIdx.x & 31;
+    return warp_all<MAX>(lane < THREADS / 32 ? part[lane] : 0.f);
+}
+
+template <typename T, int THREADS, int NV, bool ALIGNED>
+__global__ void __launch_bounds__(THREADS) norm_kernel(const NormArgs A)
+{
+    __shared__ float part[2][32];
+    const int64_t row = blockIdx.x;
+    const T *x = (const T *)A.x + row * A.xs;
+    const T *res = A.res ? (const T *)A.res + row * A.rs : nullptr;
+    float a[NV][8];
+    float ss = 0.f;
+#pragma unroll
+    for (int i = 0; i < NV; i++) {
+        const int e = 8 * (threadIdx.x + i * THREADS), n = A.H - e;
+#pragma unroll
+        for (int j = 0; j < 8; j++) a[i][j] = 0.f;
+        if (n > 0) {
+            load8<T, ALIGNED>(x + e, n, a[i]);
+            if (res) {
+                float r[8];
+                load8<T, ALIGNED>(res + e, n, r);
+#pragma unroll
+                for (int j = 0; j < 8; j++) a[i][j] += r[j];
+            }
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < NV; i++) {
+        const int e = 8 * (threadIdx.x + i * THREADS), n = A.H - e;
+        if (A.sum && n > 0) store8<T, ALIGNED>((T *)A.sum + row * A.ss + e, n, a[i]);
+#pragma unroll
+        for (int j = 0; j < 8; j++) ss = fmaf(a[i][j], a[i][j], ss);
+    }
+    const float rstd = rsqrtf(block_all<THREADS, false>(ss, part[0]) / (float)A.H + A.eps);
+    float row_max = 0.f;
+#pragma unroll
+    for (int i = 0; i < NV; i++) {
+        const int e = 8 * (threadIdx.x + i * THREADS), n = A.H - e;
+        float w[8];
+        if (A.w && n > 0) load8<T, ALIGNED>((const T *)A.w + e, n, w);
+#pragma unroll
+        for (int j = 0; j < 8; j++) {
+            a[i][j] *= rstd;
+            if (A.w && n > 0) a[i][j] *= w[j];
+        }
+        if (A.y && n > 0) store8<T, ALIGNED>((T *)A.y + row * A.ys + e, n, a[i]);
+        if (!A.q) continue;
+        float m = 0.f;
+#pragma unroll
+        for (int j = 0; j < 8; j++)
+            if (j < n) m = fmaxf(m, fabsf(a[i][j]));
+        if (A.groups == 1) {
+            row_max = fmaxf(row_max, m);
+            continue;
+        }
+#pragma unroll
+        for (int o = 8; o; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, o));
+        if (n <= 0) continue;
+        const float s = m > 0.f ? fmaxf(m / kE4m3Max, kMinScale) : 1.f;
+        if ((threadIdx.x & 15) == 0) A.scale[row * A.groups + e / PF_SCALE_GROUP] = s;
+        const float inv = 1.f / s;
+        uint8_t *q = A.q + row * A.H + e;
+        const uint32_t lo = e4m3x4(a[i][0] * inv, a[i][1] * inv, a[i][2] * inv, a[i][3] * inv);
+        const uint32_t hi = e4m3x4(a[i][4] * inv, a[i][5] * inv, a[i][6] * inv, a[i][7] * inv);
+        if (ALIGNED) {
+            *reinterpret_cast<uint2 *>(q) = make_uint2(lo, hi);
+        } else {
+#pragma unroll
+            for (int j = 0; j < 8; j++)
+                if (j < n) q[j] = (uint8_t)((j < 4 ? lo : hi) >> (8 * (j & 3)));
+        }
+    }
+    if (!A.q || A.groups != 1) return;
+    const float m = block_all<THREADS, true>(row_max, part[1]);
+    const float s = m > 0.f ? fmaxf(m / kE4m3Max, kMinScale) : 1.f, inv = 1.f / s;
+    if (threadIdx.x == 0) A.scale[row] = s;
+#pragma unroll
+    for (int i = 0; i < NV; i++) {
+        const int e = 8 * (threadIdx.x + i * THREADS), n = A.H - e;
+        if (n <= 0) continue;
+        uint8_t *q = A.q + row * A.H + e;
+        const uint32_t lo = e4m3x4(a[i][0] * inv, a[i][1] * inv, a[i][2] * inv, a[i][3] * inv);
+        const uint32_t hi = e4m3x4(a[i][4] * inv, a[i][5] * inv, a[i][6] * inv, a[i][7] * inv);
+        if (ALIGNED) {
+            *reinterpret_cast<uint2 *>(q) = make_uint2(lo, hi);
+        } else {
+#pragma unroll
+            for (int j = 0; j < 8; j++)
+                if (j < n) q[j] = (uint8_t)((j < 4 ? lo : hi) >> (8 * (j & 3)));
+        }
+    }
+}
+
+template <typename T, bool ALIGNED>
+static void norm_launch(const NormArgs &a, unsigned rows, bool few_rows, cudaStream_t st)
+{
+    if (few_rows && a.H > 2048) {
+        if (a.H <= 8192) norm_kernel<T, 1024, 1, ALIGNED><<<rows, 1024, 0, st>>>(a);
+        else norm_kernel<T, 1024, 2, ALIGNED><<<rows, 1024, 0, st>>>(a);
+        return;
+    }
+    if (a.H <= 1024) norm_kernel<T, 128, 1, ALIGNED><<<rows, 128, 0, st>>>(a);
+    else if (a.H <= 2048) norm_kernel<T, 256, 1, ALIGNED><<<rows, 256, 0, st>>>(a);
+    else if (a.H <= 4096) norm_kernel<T, 256, 2, ALIGNED><<<rows, 256, 0, st>>>(a);
+    else if (a.H <= 8192) norm_kernel<T, 256, 4, ALIGNED><<<rows, 256, 0, st>>>(a);
+    else norm_kernel<T, 256, 8, ALIGNED><<<rows, 256, 0, st>>>(a);
+}
+
+}  // namespace pf
+
+using namespace pf;
+
+extern "C" int pf_add_rms_norm(int32_t dtype, int64_t rows, int32_t H, const void *d_x, int64_t x_stride, const void *d_residual,
+                               int64_t residual_stride, const void *d_weight, float eps, int32_t group, void *d_sum,
+                               int64_t sum_stride, void *d_y, int64_t y_stride, uint8_t *d_q, float *d_scale, void *stream)
+{
+    if (dtype != PF_DT_BF16 && dtype != PF_DT_F16 && dtype != PF_DT_F32) return PF_EINVAL;
+    if (group != 0 && group != PF_SCALE_GROUP) return PF_EINVAL;
+    if (!(eps >= 0.f) || isinf(eps)) return PF_EINVAL;
+    if (H < 1 || H > PF_NORM_MAX_H || rows < 0 || rows >= (1ll << 31)) return PF_ERANGE;
+    if (rows == 0) return PF_OK;
+    if (!d_sum && !d_y && !d_q) return PF_EINVAL;
+    if (d_q && !d_scale) return PF_EINVAL;
+    if (x_stride < H || (d_residual && residual_stride < H) || (d_sum && sum_stride < H) || (d_y && y_stride < H)) return PF_EINVAL;
+    if (!d_x) return PF_EINVAL;
+    const int esize = dtype == PF_DT_F32 ? 4 : 2;
+    if ((uintptr_t)d_x % esize || (uintptr_t)d_residual % esize || (uintptr_t)d_weight % esize || (uintptr_t)d_sum % esize ||
+        (uintptr_t)d_y % esize || (uintptr_t)d_scale % 4)
+        return PF_EINVAL;
+    const int per16 = 16 / esize;
+    const bool aligned = H % 8 == 0 && aligned16(d_x) && x_stride % per16 == 0 && aligned16(d_weight) &&
+                         (!d_residual || (aligned16(d_residual) && residual_stride % per16 == 0)) &&
+                         (!d_sum || (aligned16(d_sum) && sum_stride % per16 == 0)) &&
+                         (!d_y || (aligned16(d_y) && y_stride % per16 == 0)) && (uintptr_t)d_q % 8 == 0;
+    int device, sms;
+    if (int rc = current_sm_count(&device, &sms)) return rc;
+    NormArgs a;
+    a.x = d_x; a.res = d_residual; a.w = d_weight; a.sum = d_sum; a.y = d_y; a.q = d_q; a.scale = d_scale;
+    a.xs = x_stride; a.rs = residual_stride; a.ss = sum_stride; a.ys = y_stride;
+    a.H = H; a.groups = group ? (H + group - 1) / group : 1; a.eps = eps;
+    cudaStream_t st = (cudaStream_t)stream;
+    const bool few = rows <= sms;
+    // a row of at most one group takes the row path: one scale either way
+    if (dtype == PF_DT_BF16) aligned ? norm_launch<Bf16, true>(a, (unsigned)rows, few, st) : norm_launch<Bf16, false>(a, (unsigned)rows, few, st);
+    else if (dtype == PF_DT_F16) aligned ? norm_launch<F16, true>(a, (unsigned)rows, few, st) : norm_launch<F16, false>(a, (unsigned)rows, few, st);
+    else aligned ? norm_launch<float, true>(a, (unsigned)rows, few, st) : norm_launch<float, false>(a, (unsigned)rows, few, st);
+    PF_CUDA_TRY(cudaGetLastError(), "norm_kernel launch");
+    count_launch();
+    return PF_OK;
+}
