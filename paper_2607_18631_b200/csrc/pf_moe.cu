@@ -7,11 +7,12 @@
 //  - pf_moe_pack lays the matrices out once in the order in which the lanes of a warp hold them for the matrix
 //    instruction (m16n8k16: 16 weight rows times up to 8 tokens), so a warp's copies are contiguous and no lane
 //    needs another lane's bytes.
-//  - moe_route_kernel: router logits (partial sums over slices of H), and for e4m3 weights the tokens as fp16.
+//  - moe_route_kernel: router logits (partial sums over slices of H), and the tokens as the second kernel's products take them.
 //  - moe_kernel: one block per SM, launched cooperatively, does everything else.  Its blocks choose the experts, then run
 //    through the row tiles of the chosen experts' gate and up matrices, meet, run through the tiles of the down matrices,
-//    meet, and add up each token's parts in a fixed order.  Asynchronous copies fill a ring of kStages stages in shared memory;
-//    while blocks meet, the ring already fills with the down matrices' first stages, which do not depend on the meeting.
+//    meet, and add up each token's parts in a fixed order.  One warp of a block copies (bulk copies into a ring of a few
+//    stages, completion on an mbarrier), eight multiply; a multiplying warp waits for nothing but its stage.  While the blocks
+//    meet, the ring already fills with the down matrices' first stages, which do not depend on the meeting.
 //  - 8 gate rows and the same 8 up rows form one 16-row tile: a lane's accumulators hold both factors of its products.
 // Sums are fp32.  bf16 weights multiply bf16 tokens; the hidden activations (fp32) enter the second product as the
 // sum of two bf16 numbers (16 bits of mantissa).  e4m3 weights are widened to fp16, which is exact; tokens and hidden activations
@@ -21,10 +22,11 @@
 
 namespace pf {
 
-constexpr int kMoeWarps = 8, kMoeThreads = kMoeWarps * 32;
+constexpr int kMoeWarps = 8, kMoeThreads = kMoeWarps * 32;   // that multiply
+constexpr int kMoeBlock = kMoeThreads + 32;                  // and one warp that copies
 constexpr int kSliceBytes = 2048;          // 16 rows x KW elements, KW = 64 (bf16) or 128 (e4m3)
-constexpr int kMoeStages = 5;
-constexpr unsigned kMeetLimit = 1u << 22;  // polls of a meeting before it gives up (a poll takes about a microsecond)
+constexpr unsigned kMeetLimit = 1u << 21;  // polls of a meeting before it gives up (a poll takes about a microsecond)
+constexpr unsigned kRingLimit = 1u << 20;  // waits of up to a microsecond for a stage before they give up
 
 struct MoeArgs {
     pf_moe_t m;
@@ -32,6 +34,7 @@ struct MoeArgs {
     int n_sets;                            // n_local + n_shared
     int f_tiles, h_tiles, ks_up, ks_down;  // row tiles and column slices of the packed matrices
     int Fp;                                // 8 * f_tiles
+    int Hk, Fk;                            // H and F rounded up to whole slices: row lengths of the products' inputs
     size_t set_bytes, down_at;             // packed bytes per expert, offset of its down part
     const uint16_t *x;
     int64_t xs;
@@ -48,10 +51,10 @@ struct MoeArgs {
     unsigned *ctl;                         // [0] arrivals, [1] a meeting failed
     unsigned *h_max;                       // [pairs] bits of max |h| (e4m3 weights)
     float *logits;                         // [h_splits][T][n_experts]
-    uint16_t *xh;                          // [T][H] fp16 tokens (e4m3 weights)
+    uint16_t *xh;                          // [T][Hk] tokens, zero behind H: bf16, or fp16 times a power of two (e4m3 weights)
     float *xh_scale;                       // [T] power of two
     float *h32;                            // [pairs][Fp] (e4m3 weights)
-    uint16_t *hop;                         // bf16: [pairs][2][Fp] high and low parts; e4m3: [pairs][Fp] fp16
+    uint16_t *hop;                         // zero behind F; bf16: [pairs][2][Fk] high and low parts; e4m3: [pairs][Fk] fp16
     float *y;                              // [pairs][H]
     int h_splits, e_tiles, t_chunks;       // router grid
 };
@@ -104,7 +107,8 @@ __device__ __forceinline__ int fp16_exponent(float amax)
 }
 __device__ __forceinline__ float exp2i(int e) { return __uint_as_float((uint32_t)(min(127, max(-126, e)) + 127) << 23); }
 
-constexpr int kRouteTokens = 32;
+constexpr int kRouteTokens = 32, kRouteSplits = 8;
+template <bool E4M3>
 __global__ void __launch_bounds__(kMoeThreads) moe_route_kernel(const __grid_constant__ MoeArgs A)
 {
     __shared__ float red[kMoeWarps][16][kRouteTokens + 1];
@@ -159,8 +163,13 @@ __global__ void __launch_bounds__(kMoeThreads) moe_route_kernel(const __grid_con
         }
         return;
     }
-    // e4m3 weights: token t as fp16 times a power of two; its pairs' maxima start at zero
     const int t = blockIdx.x - n_gemm;
+    if constexpr (!E4M3) {
+        for (int k = tid * 8; k < A.Hk; k += kMoeThreads * 8)
+            *reinterpret_cast<uint4 *>(A.xh + (size_t)t * A.Hk + k) =
+                k < H ? *reinterpret_cast<const uint4 *>(A.x + (int64_t)t * A.xs + k) : make_uint4(0, 0, 0, 0);
+    } else {
+    // token t as fp16 times a power of two; its pairs' maxima start at zero
     for (int j = tid; j < A.choices; j += kMoeThreads) A.h_max[t * A.choices + j] = 0u;
     const int groups = (H + PF_SCALE_GROUP - 1) / PF_SCALE_GROUP;
     auto value8 = [&](int k, float (&v)[8]) {
@@ -201,53 +210,98 @@ __global__ void __launch_bounds__(kMoeThreads) moe_route_kernel(const __grid_con
     const int e = fp16_exponent(m);
     const float down = exp2i(-e);
     if (tid == 0) A.xh_scale[t] = exp2i(e);
-    for (int k = tid * 8; k < H; k += kMoeThreads * 8) {
-        float v[8];
-        value8(k, v);
-        *reinterpret_cast<uint4 *>(A.xh + (int64_t)t * H + k) =
+    for (int k = tid * 8; k < A.Hk; k += kMoeThreads * 8) {
+        float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+        if (k < H) value8(k, v);
+        *reinterpret_cast<uint4 *>(A.xh + (size_t)t * A.Hk + k) =
             make_uint4(f16x2_of(v[0] * down, v[1] * down), f16x2_of(v[2] * down, v[3] * down), f16x2_of(v[4] * down, v[5] * down),
                        f16x2_of(v[6] * down, v[7] * down));
+    }
     }
 }
 
 // ------------------------------------------------------------------ the layer
-// All blocks of the (cooperative) grid meet; false where the wait ran out.
-__device__ __forceinline__ bool meet(const MoeArgs &A, unsigned &round, int *ok)
+// All blocks of the (cooperative) grid meet, each represented by one thread; false where the wait ran out.
+__device__ __forceinline__ bool arrive_and_poll(unsigned *ctl, unsigned round, bool arrive)
+{
+    if (arrive) {
+        __threadfence();
+        atomicAdd(ctl, 1u);
+    }
+    unsigned seen = 0, polls = 0;
+    do {
+        asm volatile("ld.acquire.gpu.global.u32 %0, [%1];" : "=r"(seen) : "l"(ctl) : "memory");
+    } while (seen < round && ++polls < kMeetLimit);
+    __threadfence();
+    return seen >= round;
+}
+template <int ID, int THREADS> __device__ __forceinline__ void bar()
+{
+    asm volatile("bar.sync %0, %1;" ::"n"(ID), "n"(THREADS) : "memory");
+}
+template <int ID, int THREADS> __device__ __forceinline__ void bar_arrive()
+{
+    asm volatile("bar.arrive %0, %1;" ::"n"(ID), "n"(THREADS) : "memory");
+}
+// the multiplying threads (or, before the roles part, all threads) of the block meet the other blocks'
+template <int ID, int THREADS>
+__device__ __forceinline__ bool meet(unsigned *ctl, unsigned &round, int *ok)
 {
     round += gridDim.x;
-    __syncthreads();
-    if (threadIdx.x == 0) {
-        __threadfence();
-        atomicAdd(A.ctl, 1u);
-        unsigned seen = 0, polls = 0;
-        do {
-            asm volatile("ld.acquire.gpu.global.u32 %0, [%1];" : "=r"(seen) : "l"(A.ctl) : "memory");
-        } while (seen < round && ++polls < kMeetLimit);
-        *ok = seen >= round;
-        __threadfence();
-    }
-    __syncthreads();
+    asm volatile("fence.proxy.async;" ::: "memory");      // what was written is read by bulk copies
+    bar<ID, THREADS>();
+    if (threadIdx.x == 0) *ok = arrive_and_poll(ctl, round, true);
+    bar<ID, THREADS>();
     return *ok != 0;
 }
 
-template <bool E4M3, int WM, int WK, int NT>
+// ---- mbarriers in shared memory
+__device__ __forceinline__ void mbar_init(uint32_t b, unsigned count) { asm volatile("mbarrier.init.shared.b64 [%0], %1;" ::"r"(b), "r"(count) : "memory"); }
+__device__ __forceinline__ void mbar_arrive(uint32_t b) { asm volatile("mbarrier.arrive.shared.b64 _, [%0];" ::"r"(b) : "memory"); }
+__device__ __forceinline__ void mbar_expect(uint32_t b, uint32_t bytes)
+{
+    asm volatile("mbarrier.arrive.expect_tx.shared.b64 _, [%0], %1;" ::"r"(b), "r"(bytes) : "memory");
+}
+// waits for the phase of the given parity to end; false where the wait ran out
+__device__ __forceinline__ bool mbar_wait(uint32_t b, unsigned parity)
+{
+    for (unsigned i = 0; i < kRingLimit; i++) {
+        uint32_t done;
+        asm volatile("{\n.reg .pred p;\nmbarrier.try_wait.parity.shared.b64 p, [%1], %2, %3;\nselp.u32 %0, 1, 0, p;\n}"
+                     : "=r"(done) : "r"(b), "r"(parity), "r"(1000u) : "memory");
+        if (done) return true;
+    }
+    return false;
+}
+__device__ __forceinline__ void bulk_copy(uint32_t dst, const void *src, uint32_t bytes, uint32_t mbar)
+{
+    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src), "r"(bytes), "r"(mbar) : "memory");
+}
+
+template <bool E4M3, int WM, int WK, int MI, int NT>
 struct MoeShape {
     static constexpr int KW = E4M3 ? 128 : 64;
     static constexpr int PLANES = E4M3 ? 1 : 2;               // of the hidden activations
-    static constexpr int A_BYTES = kMoeWarps * kSliceBytes;
+    static constexpr int TM = WM * MI;                        // row tiles of an item
+    static constexpr int A_BYTES = kMoeWarps * MI * kSliceBytes;
     static constexpr int PITCH = WK * KW * 2 + 64;            // a token row; 64 mod 128: two rows' quarters use all banks
     static constexpr int B_BYTES = NT * PLANES * PITCH;
     static constexpr int STAGE = A_BYTES + B_BYTES;
-    static constexpr int RED = WK * WM * 16 * NT * 4;
+    static constexpr int RED = WK * TM * 16 * NT * 4;         // one item's partial sums
+    static constexpr int BUFS = RED > 16384 ? 1 : 2;
+    static constexpr int STAGES = NT == 8 ? 4 : 3;            // what 227 KB hold beside the partial sums and the longest list of pairs
+    static constexpr int FIXED = STAGES * STAGE + BUFS * RED;
     static_assert(WM * WK == kMoeWarps, "one slice per warp and stage");
 };
 
-template <bool E4M3, int WM, int WK, int NT>
-__global__ void __launch_bounds__(kMoeThreads, 1) moe_kernel(const __grid_constant__ MoeArgs A)
+template <bool E4M3, int WM, int WK, int MI, int NT>
+__global__ void __launch_bounds__(kMoeBlock, 1) moe_kernel(const __grid_constant__ MoeArgs A)
 {
-    using S = MoeShape<E4M3, WM, WK, NT>;
+    using S = MoeShape<E4M3, WM, WK, MI, NT>;
     using MT = typename std::conditional<E4M3, F16, Bf16>::type;
+    constexpr int kStages = S::STAGES;
     extern __shared__ __align__(128) uint8_t smem[];
+    __shared__ __align__(8) uint64_t bars[2 * kStages];
     __shared__ int meet_ok;
     __shared__ int n_active_s;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, q = lane & 3;
@@ -255,8 +309,8 @@ __global__ void __launch_bounds__(kMoeThreads, 1) moe_kernel(const __grid_consta
     const int T = A.T, K = A.m.top_k, C = A.choices, E = A.m.n_experts, H = A.m.H;
     uint8_t *ring_p = smem;
     const uint32_t ring = smem_addr(ring_p);
-    float *red = reinterpret_cast<float *>(smem + kMoeStages * S::STAGE);
-    int *cnt = reinterpret_cast<int *>(smem + kMoeStages * S::STAGE + S::RED);      // [n_sets] tokens per expert, then running offsets
+    float *red = reinterpret_cast<float *>(smem + kStages * S::STAGE);
+    int *cnt = reinterpret_cast<int *>(smem + S::FIXED);      // [n_sets] tokens per expert, then running offsets
     int *off = cnt + A.n_sets;                                                       // [n_sets] first list entry
     int *act = off + A.n_sets;                                                       // [n_sets] experts with tokens
     int *cum = act + A.n_sets;                                                       // [n_sets + 1] token chunks before an active expert
@@ -265,6 +319,14 @@ __global__ void __launch_bounds__(kMoeThreads, 1) moe_kernel(const __grid_consta
 
     // ---- the choice: one warp per token.  For few tokens each block makes all of it by itself, which saves a meeting.
     const bool by_itself = T <= 2 * kMoeWarps;
+    if (tid == 0) {
+        for (int i = 0; i < kStages; i++) {
+            mbar_init(smem_addr(bars + i), 2);                   // full: the weights' and the tokens' announcements, and their bytes
+            mbar_init(smem_addr(bars + kStages + i), kMoeWarps);   // empty: the multiplying warps
+        }
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp < kMoeWarps)
     for (int t = by_itself ? warp : warp * (int)gridDim.x + (int)blockIdx.x; t < T; t += by_itself ? kMoeWarps : kMoeWarps * (int)gridDim.x) {
         uint32_t key[PF_MOE_MAX_EXPERTS / 32];
 #pragma unroll
@@ -272,8 +334,11 @@ __global__ void __launch_bounds__(kMoeThreads, 1) moe_kernel(const __grid_consta
             key[i] = 0u;
             const int e = i * 32 + lane;
             if (i * 32 < E && e < E) {
-                float s = 0.f;
-                for (int hs = 0; hs < A.h_splits; hs++) s += A.logits[((int64_t)hs * T + t) * E + e];
+                float v[kRouteSplits], s = 0.f;                 // all in flight, added in a fixed order
+#pragma unroll
+                for (int hs = 0; hs < kRouteSplits; hs++) v[hs] = hs < A.h_splits ? A.logits[((int64_t)hs * T + t) * E + e] : 0.f;
+#pragma unroll
+                for (int hs = 0; hs < kRouteSplits; hs++) s += v[hs];
                 const uint32_t b = s == s ? __float_as_uint(s) : 0xFF800000u;
                 key[i] = (b >> 31) ? ~b : (b | 0x80000000u);      // order of the floats; 0 = taken
             }
@@ -313,13 +378,13 @@ __global__ void __launch_bounds__(kMoeThreads, 1) moe_kernel(const __grid_consta
         }
     }
     if (by_itself) __syncthreads();
-    else if (!meet(A, round, &meet_ok)) {
+    else if (!meet<0, kMoeBlock>(A.ctl, round, &meet_ok)) {
         if (tid == 0 && A.status) *A.status = 1;
         return;
     }
 
     // ---- pairs by expert
-    for (int i = tid; i < A.n_sets; i += kMoeThreads) cnt[i] = 0;
+    for (int i = tid; i < A.n_sets; i += kMoeBlock) cnt[i] = 0;
     __syncthreads();
     auto set_of = [&](int p) {               // expert of pair p on this GPU, -1 if it lives elsewhere
         const int t = p / C, j = p - t * C;
@@ -327,7 +392,7 @@ __global__ void __launch_bounds__(kMoeThreads, 1) moe_kernel(const __grid_consta
         const int e = (by_itself ? reinterpret_cast<const int *>(red)[t * K + j] : A.ids[t * K + j]) - A.m.first;
         return e >= 0 && e < A.m.n_local ? e : -1;
     };
-    for (int p = tid; p < T * C; p += kMoeThreads) {
+    for (int p = tid; p < T * C; p += kMoeBlock) {
         const int s = set_of(p);
         if (s >= 0) atomicAdd(cnt + s, 1);
     }
@@ -364,10 +429,10 @@ __global__ void __launch_bounds__(kMoeThreads, 1) moe_kernel(const __grid_consta
     __syncthreads();
     // All blocks need the same order (a block takes some of an expert's chunks), so what the atomics dealt out in any order is
     // ranked by pair number within each expert.
-    for (int i = tid; i < A.n_sets; i += kMoeThreads) cnt[i] = off[i];
+    for (int i = tid; i < A.n_sets; i += kMoeBlock) cnt[i] = off[i];
     __syncthreads();
     uint16_t *dealt = reinterpret_cast<uint16_t *>(ring_p), *set_at = dealt + T * C;      // the ring is not in use yet
-    for (int p = tid; p < T * C; p += kMoeThreads) {
+    for (int p = tid; p < T * C; p += kMoeBlock) {
         const int s = set_of(p);
         if (s < 0) continue;
         const int at = atomicAdd(cnt + s, 1);
@@ -375,7 +440,7 @@ __global__ void __launch_bounds__(kMoeThreads, 1) moe_kernel(const __grid_consta
         set_at[at] = (uint16_t)s;
     }
     __syncthreads();                         // now cnt[s] is the end of expert s's pairs
-    for (int i = tid; i < (n_active_s ? cnt[act[n_active_s - 1]] : 0); i += kMoeThreads) {
+    for (int i = tid; i < (n_active_s ? cnt[act[n_active_s - 1]] : 0); i += kMoeBlock) {
         const int s = set_at[i], p = dealt[i];
         int rank = off[s];
         for (int k = off[s]; k < cnt[s]; k++) rank += dealt[k] < p;
@@ -398,172 +463,286 @@ __global__ void __launch_bounds__(kMoeThreads, 1) moe_kernel(const __grid_consta
             c = rest - r * chunks;
         }
     };
-    const int groups1 = (A.f_tiles + WM - 1) / WM, groups2 = (A.h_tiles + WM - 1) / WM;
+    const int groups1 = (A.f_tiles + S::TM - 1) / S::TM, groups2 = (A.h_tiles + S::TM - 1) / S::TM;
     const int stages1 = (A.ks_up + WK - 1) / WK, stages2 = (A.ks_down + WK - 1) / WK;
     const int items1 = groups1 * n_chunks, items2 = groups2 * n_chunks;
     const int grid = gridDim.x;
 
-    auto load_weights = [&](bool second, const Cursor &c, int slot) {
-        const int tiles = second ? A.h_tiles : A.f_tiles, ks = second ? A.ks_down : A.ks_up;
-        const int tile = c.r * WM + wm, s = c.stage * WK + wk;
-        if (tile >= tiles || s >= ks) return;
-        const uint8_t *src = A.packed + (size_t)act[c.a] * A.set_bytes + (second ? A.down_at : 0) + ((size_t)tile * ks + s) * kSliceBytes + lane * 16;
-        const uint32_t dst = ring + slot * S::STAGE + warp * kSliceBytes + lane * 16;
-#pragma unroll
-        for (int i = 0; i < 4; i++) copy16(dst + i * 512, src + i * 512, 16u);
-    };
-    auto load_tokens = [&](bool second, const Cursor &c, int slot) {
-        const int e = act[c.a], first = off[e] + c.c * NT, n = min(NT, cnt[e] - first);
-        const int rows = second ? n * S::PLANES : n, depth = second ? A.Fp : H;
-        constexpr int CPR = WK * S::KW / 8;                     // 16-byte chunks of a stage's token row
-        const uint32_t dst = ring + slot * S::STAGE + S::A_BYTES;
-        for (int i = tid; i < rows * CPR; i += kMoeThreads) {
-            const int row = i / CPR, ch = i - row * CPR, k = c.stage * WK * S::KW + ch * 8;
-            const uint16_t *src;
-            if (second) {
-                const int p = list[first + row / S::PLANES];
-                src = A.hop + ((size_t)p * S::PLANES + row % S::PLANES) * A.Fp;
-            } else {
-                const int t = list[first + row] / C;
-                src = E4M3 ? A.xh + (size_t)t * H : A.x + (int64_t)t * A.xs;
-            }
-            copy16(dst + row * S::PITCH + ch * 16, k < depth ? src + k : src, k < depth ? 16u : 0u);
-        }
-    };
-
-    // ---- the stream: positions 0 .. n1 - 1 are stages of the first product, n1 .. n1 + n2 - 1 of the second
+    // ---- the stream: positions 0 .. n1 - 1 are stages of the first product, n1 .. n1 + n2 - 1 of the second; position p uses
+    // ring slot p % kStages
     const int mine1 = items1 > (int)blockIdx.x ? (items1 - (int)blockIdx.x + grid - 1) / grid : 0;
     const int mine2 = items2 > (int)blockIdx.x ? (items2 - (int)blockIdx.x + grid - 1) / grid : 0;
     const int n1 = mine1 * stages1, n2 = mine2 * stages2;
-    Cursor l1, l2;                                              // what is loaded next
-    l1.a = l2.a = l1.stage = l2.stage = 0;
-    l1.at(blockIdx.x, groups1, cum, n_active);
-    l2.at(blockIdx.x, groups2, cum, n_active);
-    Cursor l2_start = l2;
-    auto step = [&](Cursor &c, int stages, int groups) {
-        if (++c.stage < stages) return;
-        c.stage = 0;
-        c.at(c.item + grid, groups, cum, n_active);
-    };
-    int pos_ld = 0, slot_ld = 0;
-    auto load_next_first = [&]() {                              // while the first product runs: past its end only weights
-        if (pos_ld < n1) {
-            load_weights(false, l1, slot_ld);
-            load_tokens(false, l1, slot_ld);
-            step(l1, stages1, groups1);
-        } else if (pos_ld < n1 + n2) {
-            load_weights(true, l2, slot_ld);
-            step(l2, stages2, groups2);
-        }
-        copy_commit();
-        pos_ld++;
-        slot_ld = slot_ld + 1 == kMoeStages ? 0 : slot_ld + 1;
-    };
+    const uint32_t full = smem_addr(bars), empty = full + kStages * 8;
+    asm volatile("fence.proxy.async;" ::: "memory");            // the ring held `dealt`: bulk copies write it from here on
+    __syncthreads();                                            // barriers are set up; `red` held the ids
 
-    float acc[NT / 8][4];
-    auto multiply = [&](bool second, const Cursor &c, int slot, int n) {   // this warp's slice of the stage into acc
+    if (warp == kMoeWarps) {                                    // ================= the copying warp
+        // What a stage costs this warp bounds the whole stream, so everything that belongs to an item is worked out once: where its
+        // tiles begin, and for each lane its (up to ROWS) token rows.
+        constexpr int ROWS = (NT * S::PLANES + 31) / 32;
+        struct Feed {
+            Cursor c;
+            const uint8_t *weights;
+            const uint16_t *row[ROWS];
+            int tiles, rows;
+        };
+        auto set_up = [&](bool second, Feed &f) {
+            const Cursor &c = f.c;
+            if (c.a >= n_active) return;
+            const int e = act[c.a], first = off[e] + c.c * NT, n = min(NT, cnt[e] - first);
+            f.weights = A.packed + (size_t)e * A.set_bytes + (second ? A.down_at : 0) + (size_t)(c.r * S::TM) * (second ? A.ks_down : A.ks_up) * kSliceBytes;
+            f.tiles = min(S::TM, (second ? A.h_tiles : A.f_tiles) - c.r * S::TM);
+            f.rows = second ? n * S::PLANES : n;
+#pragma unroll
+            for (int i = 0; i < ROWS; i++) {
+                const int r = i * 32 + lane;
+                if (r >= f.rows) continue;
+                const int p = list[first + (second ? r / S::PLANES : r)];
+                f.row[i] = second ? A.hop + ((size_t)p * S::PLANES + r % S::PLANES) * A.Fk : A.xh + (size_t)(p / C) * A.Hk;
+            }
+        };
+        auto begin = [&](bool second, Feed &f) {
+            f.c.a = f.c.stage = 0;
+            f.c.at(blockIdx.x, second ? groups2 : groups1, cum, n_active);
+            set_up(second, f);
+        };
+        auto advance = [&](bool second, Feed &f) {
+            if (++f.c.stage < (second ? stages2 : stages1)) return;
+            f.c.stage = 0;
+            f.c.at(f.c.item + grid, second ? groups2 : groups1, cum, n_active);
+            set_up(second, f);
+        };
+        // full barrier of a stage: one arrival announces the weights' bytes, one the tokens'
+        auto load_weights = [&](bool second, const Feed &f, int slot) {
+            if (lane != 0) return;
+            const int ks = second ? A.ks_down : A.ks_up, s0 = f.c.stage * WK;
+            const uint32_t bytes = (uint32_t)(min(WK, ks - s0) * kSliceBytes);
+            mbar_expect(full + slot * 8, f.tiles * bytes);
+#pragma unroll
+            for (int i = 0; i < S::TM; i++)
+                if (i < f.tiles)
+                    bulk_copy(ring + slot * S::STAGE + i * WK * kSliceBytes, f.weights + ((size_t)i * ks + s0) * kSliceBytes, bytes, full + slot * 8);
+        };
+        auto load_tokens = [&](bool second, const Feed &f, int slot) {
+            const int s0 = f.c.stage * WK;
+            const uint32_t bytes = (uint32_t)(min(WK, (second ? A.ks_down : A.ks_up) - s0) * S::KW * 2);
+            if (lane == 0) mbar_expect(full + slot * 8, f.rows * bytes);
+            __syncwarp();
+#pragma unroll
+            for (int i = 0; i < ROWS; i++)
+                if (i * 32 + lane < f.rows)
+                    bulk_copy(ring + slot * S::STAGE + S::A_BYTES + (i * 32 + lane) * S::PITCH, f.row[i] + s0 * S::KW, bytes, full + slot * 8);
+        };
+        bool ok = true;
+        int pos = 0, slot = 0;
+        unsigned round_of = 1;                                  // parity of the phase in which the slot was last emptied
+        auto next_slot = [&]() {                                // position pos may be filled
+            if (pos >= kStages) ok = mbar_wait(empty + slot * 8, round_of);
+            return ok;
+        };
+        auto filled = [&]() {
+            pos++;
+            if (++slot == kStages) {
+                slot = 0;
+                round_of ^= 1u;
+            }
+        };
+        Feed f;
+        begin(false, f);
+        while (pos < n1 && next_slot()) {
+            load_weights(false, f, slot);
+            load_tokens(false, f, slot);
+            filled();
+            advance(false, f);
+        }
+        begin(true, f);
+        Feed late = f;                                          // tokens of the second product follow the meeting
+        int pos_b = pos, slot_b = slot;
+        while (ok && pos < n1 + n2 && pos < n1 + kStages && next_slot()) {
+            load_weights(true, f, slot);
+            filled();
+            advance(true, f);
+        }
+        const unsigned target = round + gridDim.x * (E4M3 ? 2u : 1u);
+        if (ok && n2 > 0) ok = arrive_and_poll(A.ctl, target, false);
+        __syncwarp();
+        asm volatile("fence.proxy.async;" ::: "memory");
+        for (; ok && pos_b < pos; pos_b++) {
+            load_tokens(true, late, slot_b);
+            advance(true, late);
+            slot_b = slot_b + 1 == kStages ? 0 : slot_b + 1;
+        }
+        while (ok && pos < n1 + n2 && next_slot()) {
+            load_weights(true, f, slot);
+            load_tokens(true, f, slot);
+            filled();
+            advance(true, f);
+        }
+        // nothing may be in flight when the block ends; after a wait that ran out, the stages without tokens are closed first
+        if (!ok) {
+            for (; pos_b < pos && pos_b >= n1; pos_b++) {
+                if (lane == 0) mbar_arrive(full + slot_b * 8);
+                slot_b = slot_b + 1 == kStages ? 0 : slot_b + 1;
+            }
+            for (int i = max(0, pos - kStages); i < pos; i++) mbar_wait(full + (i % kStages) * 8, (unsigned)(i / kStages) & 1u);
+            if (lane == 0 && A.status) *A.status = 1;
+        }
+        return;
+    }
+
+    // ===================================================== the multiplying warps
+    float acc[MI][NT / 8][4], scale0[MI], scale1[MI];
+    int slot = 0;
+    unsigned parity = 0;
+    bool ok = true;
+    auto clear = [&](float (&v)[MI][NT / 8][4]) {
+#pragma unroll
+        for (int i = 0; i < MI; i++)
+#pragma unroll
+            for (int j = 0; j < NT / 8; j++) v[i][j][0] = v[i][j][1] = v[i][j][2] = v[i][j][3] = 0.f;
+    };
+    auto multiply = [&](bool second, const Cursor &c, int n) {  // this warp's slices of the stage into acc
         const int tiles = second ? A.h_tiles : A.f_tiles, ks = second ? A.ks_down : A.ks_up;
-        const int tile = c.r * WM + wm, s = c.stage * WK + wk;
-        const bool live = tile < tiles && s < ks;
-        float s0 = 1.f, s1 = 1.f;
-        if (E4M3 && live) {                                     // block scales: fetched before the wait for the stage
-            const int kb_n = second ? (A.m.F + 127) / 128 : (H + 127) / 128;
-            if (second) {
-                s0 = s1 = __ldg(A.ds + ((size_t)act[c.a] * ((H + 127) / 128) + tile / 8) * kb_n + s);
-            } else {
-                const size_t at = ((size_t)act[c.a] * ((A.m.F + 127) / 128) + tile / 16) * kb_n + s;
-                s0 = __ldg(A.gs + at);
-                s1 = __ldg(A.us + at);
-            }
-        }
-        copy_wait<kMoeStages - 2>();
-        __syncthreads();
-        if (!live) return;
-        const uint32_t wa = ring + slot * S::STAGE + warp * kSliceBytes + lane * 16;
-        const uint32_t tb = ring + slot * S::STAGE + S::A_BYTES + wk * S::KW * 2 + q * 16;
-        float sub[NT / 8][4];
+        const int tile = c.r * S::TM + wm * MI, s = c.stage * WK + wk;
+        const bool live = tile < tiles && s < ks;               // a second tile past the end multiplies old bytes of the ring; nobody reads the rows
+        float s0[MI], s1[MI];
         if (E4M3) {
+            if (c.stage % 32 == 0) {                            // block scales of 32 stages, a stage a lane
+                const int mine = (c.stage + lane) * WK + wk;
+                const int kb_n = second ? (A.m.F + 127) / 128 : (H + 127) / 128;
 #pragma unroll
-            for (int j = 0; j < NT / 8; j++) sub[j][0] = sub[j][1] = sub[j][2] = sub[j][3] = 0.f;
-        }
-        float (&sum)[NT / 8][4] = E4M3 ? sub : acc;
-#pragma unroll
-        for (int kg = 0; kg < S::KW / 32; kg++) {
-            uint32_t a[2][4];
-            if (E4M3) {
-                const uint4 v = lds128(wa + kg * 512);
-                const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-                for (int i = 0; i < 4; i++) {
-                    a[i >> 1][2 * (i & 1)] = f16x2_of_e4m3x2(w[i]);
-                    a[i >> 1][2 * (i & 1) + 1] = f16x2_of_e4m3x2(w[i] >> 16);
-                }
-            } else {
-#pragma unroll
-                for (int i = 0; i < 2; i++) {
-                    const uint4 v = lds128(wa + (2 * kg + i) * 512);
-                    a[i][0] = v.x; a[i][1] = v.y; a[i][2] = v.z; a[i][3] = v.w;
+                for (int i = 0; i < MI; i++) {
+                    const bool any = tile + i < tiles && mine < ks;
+                    if (second) {
+                        scale0[i] = any ? __ldg(A.ds + ((size_t)act[c.a] * ((H + 127) / 128) + (tile + i) / 8) * kb_n + mine) : 0.f;
+                    } else {
+                        const size_t at = ((size_t)act[c.a] * ((A.m.F + 127) / 128) + (tile + i) / 16) * kb_n + mine;
+                        scale0[i] = any ? __ldg(A.gs + at) : 0.f;
+                        scale1[i] = any ? __ldg(A.us + at) : 0.f;
+                    }
                 }
             }
+#pragma unroll
+            for (int i = 0; i < MI; i++) {
+                s0[i] = __shfl_sync(0xFFFFFFFFu, scale0[i], c.stage % 32);
+                s1[i] = second ? s0[i] : __shfl_sync(0xFFFFFFFFu, scale1[i], c.stage % 32);
+            }
+        }
+        if (ok) ok = mbar_wait(full + slot * 8, parity);
+        if (live && ok) {
+            const uint32_t wa = ring + slot * S::STAGE + (wm * MI * WK + wk) * kSliceBytes + lane * 16;
             const int planes = second ? S::PLANES : 1;
+            const uint32_t tb = ring + slot * S::STAGE + S::A_BYTES + g * (planes * S::PITCH) + wk * S::KW * 2 + q * 16;
+            float sub[MI][NT / 8][4];
+            if (E4M3) clear(sub);
+            float (&sum)[MI][NT / 8][4] = E4M3 ? sub : acc;
 #pragma unroll
-            for (int j = 0; j < NT / 8; j++) {
-                if (NT > 8 && j * 8 >= n) break;
-                for (int pl = 0; pl < planes; pl++) {
-                    const uint4 b = lds128(tb + ((j * 8 + g) * planes + pl) * S::PITCH + kg * 64);
-                    mma16<MT>(sum[j], a[0][0], a[0][1], a[0][2], a[0][3], b.x, b.y);
-                    mma16<MT>(sum[j], a[1][0], a[1][1], a[1][2], a[1][3], b.z, b.w);
+            for (int kg = 0; kg < S::KW / 32; kg++) {
+                uint32_t a[MI][2][4];
+#pragma unroll
+                for (int t = 0; t < MI; t++) {
+                    if (E4M3) {
+                        const uint4 v = lds128(wa + t * WK * kSliceBytes + kg * 512);
+                        const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+                        for (int i = 0; i < 4; i++) {
+                            a[t][i >> 1][2 * (i & 1)] = f16x2_of_e4m3x2(w[i]);
+                            a[t][i >> 1][2 * (i & 1) + 1] = f16x2_of_e4m3x2(w[i] >> 16);
+                        }
+                    } else {
+#pragma unroll
+                        for (int i = 0; i < 2; i++) {
+                            const uint4 v = lds128(wa + t * WK * kSliceBytes + (2 * kg + i) * 512);
+                            a[t][i][0] = v.x; a[t][i][1] = v.y; a[t][i][2] = v.z; a[t][i][3] = v.w;
+                        }
+                    }
+                }
+#pragma unroll
+                for (int j = 0; j < NT / 8; j++) {
+                    if (NT > 8 && j * 8 >= n) break;
+                    for (int pl = 0; pl < planes; pl++) {
+                        const uint4 b = lds128(tb + (j * 8 * planes + pl) * S::PITCH + kg * 64);
+#pragma unroll
+                        for (int t = 0; t < MI; t++) mma16<MT>(sum[t][j], a[t][0][0], a[t][0][1], a[t][0][2], a[t][0][3], b.x, b.y);
+#pragma unroll
+                        for (int t = 0; t < MI; t++) mma16<MT>(sum[t][j], a[t][1][0], a[t][1][1], a[t][1][2], a[t][1][3], b.z, b.w);
+                    }
+                }
+            }
+            if (E4M3) {
+#pragma unroll
+                for (int j = 0; j < NT / 8; j++) {
+                    if (NT > 8 && j * 8 >= n) break;
+#pragma unroll
+                    for (int t = 0; t < MI; t++) {
+                        acc[t][j][0] = fmaf(sub[t][j][0], s0[t], acc[t][j][0]);
+                        acc[t][j][1] = fmaf(sub[t][j][1], s0[t], acc[t][j][1]);
+                        acc[t][j][2] = fmaf(sub[t][j][2], s1[t], acc[t][j][2]);
+                        acc[t][j][3] = fmaf(sub[t][j][3], s1[t], acc[t][j][3]);
+                    }
                 }
             }
         }
-        if (E4M3) {
-#pragma unroll
-            for (int j = 0; j < NT / 8; j++) {
-                acc[j][0] = fmaf(sub[j][0], s0, acc[j][0]);
-                acc[j][1] = fmaf(sub[j][1], s0, acc[j][1]);
-                acc[j][2] = fmaf(sub[j][2], s1, acc[j][2]);
-                acc[j][3] = fmaf(sub[j][3], s1, acc[j][3]);
-            }
+        __syncwarp();
+        if (lane == 0) mbar_arrive(empty + slot * 8);
+        if (++slot == kStages) {
+            slot = 0;
+            parity ^= 1u;
         }
     };
-    // the WK warps' partial sums meet in `red` ([wk][row][token]); the next use is a stage's barrier away
-    auto put_partials = [&]() {
+    // The WK warps' partial sums meet in `red` ([wk][row][token]).  Where two buffers fit, two halves of the warps take turns: one
+    // finishes an item while the other already multiplies the next.  A warp puts its sums into a buffer again only after it has waited for,
+    // or finished, the item in between, and that item's barrier has seen every warp finish with the buffer.  With one buffer
+    // all warps finish every item.
+    constexpr int FINISH = S::BUFS == 2 ? kMoeThreads / 2 : kMoeThreads;
+    const int half = warp / (kMoeWarps / 2), htid = tid % FINISH;
+    int turn = 0;
+    const float *r_get = red;
+    auto put_partials = [&]() {                                 // true: this warp finishes the item, with FINISH - 1 other threads
+        float *buf = red + turn * (S::RED / 4);
+        if (S::BUFS == 1) bar<2, kMoeThreads>();                // everyone has finished the item before
 #pragma unroll
-        for (int j = 0; j < NT / 8; j++) {
-            float *r = red + ((wk * WM + wm) * 16 + g) * NT + j * 8 + 2 * q;
-            r[0] = acc[j][0];
-            r[1] = acc[j][1];
-            r[8 * NT] = acc[j][2];
-            r[8 * NT + 1] = acc[j][3];
+        for (int t = 0; t < MI; t++)
+#pragma unroll
+            for (int j = 0; j < NT / 8; j++) {
+                float *r = buf + ((wk * S::TM + wm * MI + t) * 16 + g) * NT + j * 8 + 2 * q;
+                r[0] = acc[t][j][0];
+                r[1] = acc[t][j][1];
+                r[8 * NT] = acc[t][j][2];
+                r[8 * NT + 1] = acc[t][j][3];
+            }
+        r_get = buf;
+        if (S::BUFS == 1) {
+            bar<1, kMoeThreads>();
+            return true;
         }
-        __syncthreads();
+        const bool mine = turn == half;
+        if (turn == 0) {
+            if (mine) bar<1, kMoeThreads>(); else bar_arrive<1, kMoeThreads>();
+        } else {
+            if (mine) bar<2, kMoeThreads>(); else bar_arrive<2, kMoeThreads>();
+        }
+        turn ^= 1;
+        return mine;
     };
     auto total = [&](int row, int col) {
         float v = 0.f;
 #pragma unroll
-        for (int i = 0; i < WK; i++) v += red[(i * WM * 16 + row) * NT + col];
+        for (int i = 0; i < WK; i++) v += r_get[(i * S::TM * 16 + row) * NT + col];
         return v;
     };
 
-    __syncthreads();                                            // `red` held the ids
-#pragma unroll
-    for (int i = 0; i < kMoeStages - 1; i++) load_next_first();
-    int slot = 0;
     Cursor c;
     c.a = c.stage = 0;
     c.at(blockIdx.x, groups1, cum, n_active);
     for (int it = 0; it < mine1; it++) {
         const int e = act[c.a], first = off[e] + c.c * NT, n = min(NT, cnt[e] - first);
-#pragma unroll
-        for (int j = 0; j < NT / 8; j++) acc[j][0] = acc[j][1] = acc[j][2] = acc[j][3] = 0.f;
-        for (c.stage = 0; c.stage < stages1; c.stage++) {
-            multiply(false, c, slot, n);
-            load_next_first();
-            slot = slot + 1 == kMoeStages ? 0 : slot + 1;
-        }
-        put_partials();
-        constexpr int FR = 8 * WM;                              // hidden units of the item
-        for (int i = tid; i < (FR * n + 31) / 32 * 32; i += kMoeThreads) {
+        clear(acc);
+        for (c.stage = 0; c.stage < stages1; c.stage++) multiply(false, c, n);
+        constexpr int FR = 8 * S::TM;                              // hidden units of the item
+        const bool mine = put_partials();
+        for (int i = htid; mine && i < (FR * n + 31) / 32 * 32; i += FINISH) {
             const int col = i / FR, fr = i - col * FR, f = c.r * FR + fr;
             float h = 0.f;
             int p = 0;
@@ -576,79 +755,57 @@ __global__ void __launch_bounds__(kMoeThreads, 1) moe_kernel(const __grid_consta
                     gate *= xs;
                     up *= xs;
                 }
-                if (f < A.Fp) h = gate / (1.f + expf(-gate)) * up;
                 if (f < A.Fp) {
+                    h = gate / (1.f + expf(-gate)) * up;
                     if (E4M3) {
                         A.h32[(size_t)p * A.Fp + f] = h;
                     } else {
                         const uint32_t hi = bf16x2_of(h, 0.f) & 0xFFFFu;
-                        uint16_t *dst = A.hop + (size_t)p * 2 * A.Fp + f;
+                        uint16_t *dst = A.hop + (size_t)p * 2 * A.Fk + f;
                         dst[0] = (uint16_t)hi;
-                        dst[A.Fp] = (uint16_t)bf16x2_of(h - __uint_as_float(hi << 16), 0.f);
+                        dst[A.Fk] = (uint16_t)bf16x2_of(h - __uint_as_float(hi << 16), 0.f);
                     }
                 }
             }
             if (E4M3) {
                 unsigned m = __float_as_uint(h) & 0x7FFFFFFFu;  // order of the magnitudes, infinity and NaN above all
 #pragma unroll
-                for (int o = FR / 2; o; o >>= 1) m = max(m, __shfl_xor_sync(0xFFFFFFFFu, m, o));
-                if (fr == 0 && col < n) atomicMax(A.h_max + p, m);   // a maximum: the order does not matter
+                for (int o = (FR < 32 ? FR : 32) / 2; o; o >>= 1) m = max(m, __shfl_xor_sync(0xFFFFFFFFu, m, o));
+                if (fr % 32 == 0 && col < n) atomicMax(A.h_max + p, m);   // a maximum: the order does not matter
             }
+        }
+        if (!E4M3 && mine && c.r == groups1 - 1) {              // zeros behind F
+            const int pad = A.Fk - A.Fp;
+            for (int i = htid; i < pad * n * 2; i += FINISH)
+                A.hop[((size_t)list[first + i / (2 * pad)] * 2 + i / pad % 2) * A.Fk + A.Fp + i % pad] = 0;
         }
         c.at(c.item + grid, groups1, cum, n_active);
     }
 
     // ---- all hidden activations are there
-    bool ok = meet(A, round, &meet_ok);
-    if (ok && E4M3) {                                           // as fp16 times a power of two per pair
-        const int quads = A.Fp / 4, n_pairs = n_active ? cnt[act[n_active - 1]] : 0;
+    ok = meet<3, kMoeThreads>(A.ctl, round, &meet_ok) && ok;
+    if (E4M3) {                                                 // as fp16 times a power of two per pair
+        const int quads = A.Fk / 4, n_pairs = n_active ? cnt[act[n_active - 1]] : 0;
         for (long long i = (long long)blockIdx.x * kMoeThreads + tid; i < (long long)n_pairs * quads; i += (long long)grid * kMoeThreads) {
             const int p = list[i / quads], f = (int)(i % quads) * 4;
-            const float4 v = *reinterpret_cast<const float4 *>(A.h32 + (size_t)p * A.Fp + f);
+            float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+            if (f < A.Fp) v = *reinterpret_cast<const float4 *>(A.h32 + (size_t)p * A.Fp + f);
             const float d = exp2i(-fp16_exponent(__uint_as_float(A.h_max[p])));
-            *reinterpret_cast<uint2 *>(A.hop + (size_t)p * A.Fp + f) = make_uint2(f16x2_of(v.x * d, v.y * d), f16x2_of(v.z * d, v.w * d));
+            *reinterpret_cast<uint2 *>(A.hop + (size_t)p * A.Fk + f) = make_uint2(f16x2_of(v.x * d, v.y * d), f16x2_of(v.z * d, v.w * d));
         }
-        ok = meet(A, round, &meet_ok);
-    }
-    if (!ok) {
-        if (tid == 0 && A.status) *A.status = 1;
-        copy_wait<0>();
-        return;
+        ok = meet<3, kMoeThreads>(A.ctl, round, &meet_ok) && ok;
     }
 
-    // ---- second product: the weights of the first stages are on their way, their tokens follow now
-    {
-        Cursor b = l2_start;
-        int sl = slot;
-        for (int i = 0; i < kMoeStages - 1 && i < n2; i++) {
-            load_tokens(true, b, sl);
-            step(b, stages2, groups2);
-            sl = sl + 1 == kMoeStages ? 0 : sl + 1;
-        }
-        copy_commit();
-        copy_wait<0>();
-    }
+    // ---- second product
     c.a = c.stage = 0;
     c.at(blockIdx.x, groups2, cum, n_active);
     for (int it = 0; it < mine2; it++) {
         const int e = act[c.a], first = off[e] + c.c * NT, n = min(NT, cnt[e] - first);
-#pragma unroll
-        for (int j = 0; j < NT / 8; j++) acc[j][0] = acc[j][1] = acc[j][2] = acc[j][3] = 0.f;
-        for (c.stage = 0; c.stage < stages2; c.stage++) {
-            multiply(true, c, slot, n);
-            if (pos_ld < n1 + n2) {
-                load_weights(true, l2, slot_ld);
-                load_tokens(true, l2, slot_ld);
-                step(l2, stages2, groups2);
-            }
-            copy_commit();
-            pos_ld++;
-            slot_ld = slot_ld + 1 == kMoeStages ? 0 : slot_ld + 1;
-            slot = slot + 1 == kMoeStages ? 0 : slot + 1;
-        }
-        put_partials();
-        constexpr int HR = 16 * WM;
-        for (int i = tid; i < HR * n; i += kMoeThreads) {
+        clear(acc);
+        for (c.stage = 0; c.stage < stages2; c.stage++) multiply(true, c, n);
+        constexpr int HR = 16 * S::TM;
+        const bool mine = put_partials();
+        for (int i = htid; mine && i < HR * n; i += FINISH) {
             const int col = i / HR, row = i - col * HR, hr = c.r * HR + row;
             const int p = list[first + col];
             if (hr < H) {
@@ -659,9 +816,9 @@ __global__ void __launch_bounds__(kMoeThreads, 1) moe_kernel(const __grid_consta
         }
         c.at(c.item + grid, groups2, cum, n_active);
     }
-    copy_wait<0>();
-    if (!meet(A, round, &meet_ok)) {
-        if (tid == 0 && A.status) *A.status = 1;
+    ok = meet<3, kMoeThreads>(A.ctl, round, &meet_ok) && ok;
+    if (!ok) {
+        if (lane == 0 && A.status) *A.status = 1;
         return;
     }
 
@@ -707,6 +864,8 @@ static void moe_layout(const pf_moe_t *m, MoeArgs &a)
     a.ks_up = (m->H + kw - 1) / kw;
     a.Fp = a.f_tiles * 8;
     a.ks_down = (a.Fp + kw - 1) / kw;
+    a.Hk = a.ks_up * kw;
+    a.Fk = a.ks_down * kw;
     a.down_at = (size_t)a.f_tiles * a.ks_up * kSliceBytes;
     a.set_bytes = a.down_at + (size_t)a.h_tiles * a.ks_down * kSliceBytes;
 }
@@ -727,33 +886,33 @@ static size_t moe_carve(MoeArgs &a, int T, int sms, uint8_t *base)
     // router: about one block per SM, at least 256 columns (32 per warp) for each
     const int most = (m.H + 255) / 256, want = sms / (a.e_tiles * a.t_chunks);
     a.h_splits = want < 1 ? 1 : (want < most ? want : most);
-    if (a.h_splits > 16) a.h_splits = 16;
+    if (a.h_splits > kRouteSplits) a.h_splits = kRouteSplits;
     const size_t pairs = (size_t)T * a.choices;
     size_t at = 0;
     a.ctl = (unsigned *)(base + take(at, 256));
     a.h_max = (unsigned *)(base + take(at, pairs * 4));
     a.logits = (float *)(base + take(at, (size_t)a.h_splits * T * m.n_experts * 4));
-    a.xh = (uint16_t *)(base + take(at, e4m3 ? (size_t)T * m.H * 2 : 0));
+    a.xh = (uint16_t *)(base + take(at, (size_t)T * a.Hk * 2));
     a.xh_scale = (float *)(base + take(at, (size_t)T * 4));
     a.h32 = (float *)(base + take(at, e4m3 ? pairs * a.Fp * 4 : 0));
-    a.hop = (uint16_t *)(base + take(at, pairs * a.Fp * 2 * (e4m3 ? 1 : 2)));
+    a.hop = (uint16_t *)(base + take(at, pairs * a.Fk * 2 * (e4m3 ? 1 : 2)));
     a.y = (float *)(base + take(at, pairs * m.H * 4));
     return at;
 }
 
-template <bool E4M3, int WM, int WK, int NT>
+template <bool E4M3, int WM, int WK, int MI, int NT>
 static int moe_launch(const MoeArgs &a, int device, int sms, cudaStream_t st)
 {
-    using S = MoeShape<E4M3, WM, WK, NT>;
-    const size_t smem = (size_t)kMoeStages * S::STAGE + S::RED + ((size_t)a.n_sets * 4 + 1) * 4 + (size_t)a.T * a.choices * 2;
-    PF_CUDA_TRY(ensure_dynamic_smem((const void *)moe_kernel<E4M3, WM, WK, NT>, device, smem), "moe_kernel shared memory");
-    const int n_route = a.e_tiles * a.h_splits * a.t_chunks + (E4M3 ? a.T : 0);
-    moe_route_kernel<<<n_route, kMoeThreads, 0, st>>>(a);
+    using S = MoeShape<E4M3, WM, WK, MI, NT>;
+    const size_t smem = (size_t)S::FIXED + ((size_t)a.n_sets * 4 + 1) * 4 + (size_t)a.T * a.choices * 2;
+    PF_CUDA_TRY(ensure_dynamic_smem((const void *)moe_kernel<E4M3, WM, WK, MI, NT>, device, smem), "moe_kernel shared memory");
+    const int n_route = a.e_tiles * a.h_splits * a.t_chunks + a.T;
+    moe_route_kernel<E4M3><<<n_route, kMoeThreads, 0, st>>>(a);
     PF_CUDA_TRY(cudaGetLastError(), "moe_route_kernel launch");
     count_launch();
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(sms);
-    cfg.blockDim = dim3(kMoeThreads);
+    cfg.blockDim = dim3(kMoeBlock);
     cfg.dynamicSmemBytes = smem;
     cfg.stream = st;
     cudaLaunchAttribute at[1];
@@ -761,7 +920,7 @@ static int moe_launch(const MoeArgs &a, int device, int sms, cudaStream_t st)
     at[0].val.cooperative = 1;
     cfg.attrs = at;
     cfg.numAttrs = 1;
-    PF_CUDA_TRY(cudaLaunchKernelEx(&cfg, moe_kernel<E4M3, WM, WK, NT>, a), "moe_kernel launch");
+    PF_CUDA_TRY(cudaLaunchKernelEx(&cfg, moe_kernel<E4M3, WM, WK, MI, NT>, a), "moe_kernel launch");
     count_launch();
     return PF_OK;
 }
@@ -831,8 +990,11 @@ extern "C" int pf_moe_forward(const pf_moe_t *m, int32_t T, const void *d_x, int
     a.gs = d_gate_scale; a.us = d_up_scale; a.ds = d_down_scale;
     a.out = (uint16_t *)d_out; a.ids = d_ids; a.weights = d_weights; a.status = d_status;
     cudaStream_t st = (cudaStream_t)stream;
-    // Up to 8 tokens an expert never has more than one 8-token column block: tiles of 16 rows, the columns split over the
-    // warps, fill the GPU with the fewest experts.  Beyond, 64 rows share a stage's tokens, up to 32 of them.
-    if (T <= 8) return e4m3 ? moe_launch<true, 1, 8, 8>(a, device, sms, st) : moe_launch<false, 1, 8, 8>(a, device, sms, st);
-    return e4m3 ? moe_launch<true, 4, 2, 32>(a, device, sms, st) : moe_launch<false, 4, 2, 32>(a, device, sms, st);
+    // Up to 8 tokens an expert never has more than one 8-token column block: tiles of 32 rows, the columns split over the
+    // warps, fill the GPU with the fewest experts.  Beyond, 64 rows share a stage's tokens, up to 16 of them, and with more than 8 tokens an
+    // expert on average 128 rows share up to 32.
+    if (T <= 8) return e4m3 ? moe_launch<true, 1, 8, 2, 8>(a, device, sms, st) : moe_launch<false, 1, 8, 2, 8>(a, device, sms, st);
+    if ((long long)T * m->top_k <= 8ll * m->n_experts)
+        return e4m3 ? moe_launch<true, 2, 4, 2, 16>(a, device, sms, st) : moe_launch<false, 2, 4, 2, 16>(a, device, sms, st);
+    return e4m3 ? moe_launch<true, 4, 2, 2, 32>(a, device, sms, st) : moe_launch<false, 4, 2, 2, 32>(a, device, sms, st);
 }
