@@ -103,25 +103,26 @@ typedef struct {
 #define PF_MOE_MAX_CHOICES 16   /* top_k + n_shared */
 
 /* Lay an expert set's weights out for pf_moe_forward, once: gate and up [n_local + n_shared, F, H], down [n_local +
- * n_shared, H, F], row-major and contiguous, 16-byte aligned.  d_packed: pf_moe_packed_bytes(m), 256-byte aligned; 0 where `m` is not valid.
- * PF_EINVAL: NULL or misaligned pointers, inconsistent pf_moe_t. */
+ * n_shared, H, F], row-major and contiguous, 16-byte aligned; with e4m3 weights their scales, d_gate_scale and d_up_scale
+ * [n_local + n_shared, ceil(F / 128), ceil(H / 128)], d_down_scale [.., ceil(H / 128), ceil(F / 128)] (NULL with bf16).
+ * d_packed: pf_moe_packed_bytes(m) bytes (0 where `m` is not valid), 256-byte aligned; it holds everything that
+ * pf_moe_forward needs of the weights.
+ * PF_EINVAL: NULL or misaligned pointers, inconsistent pf_moe_t, scales missing or not wanted; PF_ERANGE: more than 2^34 rows. */
 size_t pf_moe_packed_bytes(const pf_moe_t *m);
-int pf_moe_pack(const pf_moe_t *m, const void *d_gate, const void *d_up, const void *d_down, void *d_packed, void *stream);
+int pf_moe_pack(const pf_moe_t *m, const void *d_gate, const void *d_up, const void *d_down, const float *d_gate_scale,
+                const float *d_up_scale, const float *d_down_scale, void *d_packed, void *stream);
 
 /* T tokens through the layer.  d_x: T rows of H bf16 (row stride in elements, multiple of 8, 16-byte aligned), what
  * the router reads, and the experts too unless d_xq / d_xscale give the tokens in 8 bits as pf_add_rms_norm writes
- * them (group 128; e4m3 weights only).  d_router: [n_experts, H] bf16, contiguous.  d_gate_scale, d_up_scale:
- * [n_local + n_shared, ceil(F / 128), ceil(H / 128)], d_down_scale: [.., ceil(H / 128), ceil(F / 128)], e4m3 weights only.
+ * them (group 128; e4m3 weights only).  d_router: [n_experts, H] bf16, contiguous.  d_packed: see pf_moe_pack.
  * d_out: [T, H] bf16, contiguous.  d_ids [T, top_k] and d_weights [T, top_k]: the router's choice, in order of falling
  * logits (global expert indices).
  * d_status (may be NULL): one word, 0 after a complete call, 1 if a wait between the kernel's blocks ran out (d_out is
  * then not valid).
- * PF_EINVAL: NULL or misaligned pointers, inconsistent pf_moe_t, d_xq without d_xscale or with bf16 weights, missing
- * weight scales; PF_ERANGE: T outside 0 .. PF_MOE_MAX_TOKENS; PF_EWORKSPACE; T = 0 does nothing. */
+ * PF_EINVAL: NULL or misaligned pointers, inconsistent pf_moe_t, d_xq without d_xscale or with bf16 weights; PF_ERANGE: T outside 0 .. PF_MOE_MAX_TOKENS; PF_EWORKSPACE; T = 0 does nothing. */
 size_t pf_moe_workspace(const pf_moe_t *m, int32_t T);
 int pf_moe_forward(const pf_moe_t *m, int32_t T, const void *d_x, int64_t x_stride, const uint8_t *d_xq, const float *d_xscale,
-                   const void *d_router, const void *d_packed, const float *d_gate_scale, const float *d_up_scale,
-                   const float *d_down_scale, void *d_out, int32_t *d_ids, float *d_weights, int32_t *d_status,
+                   const void *d_router, const void *d_packed, void *d_out, int32_t *d_ids, float *d_weights, int32_t *d_status,
                    void *d_workspace, size_t workspace_bytes, void *stream);
 
 #ifdef __cplusplus

@@ -17,13 +17,18 @@
 // Sums are fp32.  bf16 weights multiply bf16 tokens; the hidden activations (fp32) enter the second product as the
 // sum of two bf16 numbers (16 bits of mantissa).  e4m3 weights are widened to fp16, which is exact; tokens and hidden activations
 // are scaled by a power of two per row and rounded to fp16 (11 bits); a weight block's scale is applied to the fp32 sum of
-// its 128 columns.  Two products in bf16 or fp16 cost less than half of the matrix rate at full HBM speed for 32 tokens a tile.
+// its 128 columns.  A hidden row's power of two has to be known before the row is: |h_f| <= |g_f . x| |u_f . x| <= |x|^2 max|g| max|u|
+// (Cauchy-Schwarz; |silu(a)| <= |a|), with the experts' largest row norms from pf_moe_pack.  The bound may lie 2^29 above the largest
+// |h| before fp16's least step costs more than its 11 bits (with random weights it lies a factor H above).  Two products in bf16 or fp16 cost less than half of the matrix rate at full HBM speed for 32 tokens a tile.
+#include <type_traits>
+
 #include "pf_ops.cuh"
 
 namespace pf {
 
-constexpr int kMoeWarps = 8, kMoeThreads = kMoeWarps * 32;   // that multiply
-constexpr int kMoeBlock = kMoeThreads + 32;                  // and one warp that copies
+constexpr int kMoeWarps = 16, kMoeThreads = kMoeWarps * 32;   // that multiply
+constexpr int kCopyWarps = 4;                                // that copy
+constexpr int kMoeBlock = kMoeThreads + kCopyWarps * 32;
 constexpr int kSliceBytes = 2048;          // 16 rows x KW elements, KW = 64 (bf16) or 128 (e4m3)
 constexpr unsigned kMeetLimit = 1u << 21;  // polls of a meeting before it gives up (a poll takes about a microsecond)
 constexpr unsigned kRingLimit = 1u << 20;  // waits of up to a microsecond for a stage before they give up
@@ -36,24 +41,26 @@ struct MoeArgs {
     int Fp;                                // 8 * f_tiles
     int Hk, Fk;                            // H and F rounded up to whole slices: row lengths of the products' inputs
     size_t set_bytes, down_at;             // packed bytes per expert, offset of its down part
+    size_t n_up_scales, n_down_scales;     // block scales of one expert's gate (or up) and down matrices
+    size_t packed_bytes;                   // matrices, then gate, up and down scales, then row norms
     const uint16_t *x;
     int64_t xs;
     const uint8_t *xq;
     const float *xscale;
     const uint16_t *router;
     const uint8_t *packed;
-    const float *gs, *us, *ds;
+    const float *gs, *us, *ds;             // block scales and bounds, behind the packed matrices (e4m3 weights)
+    const float *row_max;                  // [n_sets][2] largest squared row norm of gate and of up
     uint16_t *out;
     int32_t *ids;
     float *weights;
     int32_t *status;
     // workspace
     unsigned *ctl;                         // [0] arrivals, [1] a meeting failed
-    unsigned *h_max;                       // [pairs] bits of max |h| (e4m3 weights)
     float *logits;                         // [h_splits][T][n_experts]
     uint16_t *xh;                          // [T][Hk] tokens, zero behind H: bf16, or fp16 times a power of two (e4m3 weights)
-    float *xh_scale;                       // [T] power of two
-    float *h32;                            // [pairs][Fp] (e4m3 weights)
+    float *xh_scale;                       // [T] that power of two
+    float *x_norm2;                        // [T] |x|^2 (e4m3 weights)
     uint16_t *hop;                         // zero behind F; bf16: [pairs][2][Fk] high and low parts; e4m3: [pairs][Fk] fp16
     float *y;                              // [pairs][H]
     int h_splits, e_tiles, t_chunks;       // router grid
@@ -98,6 +105,27 @@ __global__ void __launch_bounds__(256) moe_pack_kernel(const pf_moe_t m, int n_s
     }
 }
 
+// largest squared row norms of an expert's gate and up matrices (e4m3 with block scales): one warp per row, maxima over rows
+__global__ void __launch_bounds__(256) moe_row_norm_kernel(const pf_moe_t m, int n_sets, const uint8_t *gate, const uint8_t *up, const float *gs,
+                                                           const float *us, float *row_max)
+{
+    const long long row = ((long long)blockIdx.x * blockDim.x + threadIdx.x) / 32;
+    if (row >= (long long)n_sets * m.F * 2) return;
+    const int lane = threadIdx.x & 31, which = (int)(row & 1), f = (int)((row >> 1) % m.F), set = (int)((row >> 1) / m.F);
+    const int kb = (m.H + 127) / 128, fb = (m.F + 127) / 128;
+    const uint8_t *w = (which ? up : gate) + ((size_t)set * m.F + f) * m.H;
+    const float *sc = (which ? us : gs) + ((size_t)set * fb + f / 128) * kb;
+    float ss = 0.f;
+    for (int k = lane * 2; k < m.H; k += 64) {
+        const float2 v = f32x2_of_f16x2(f16x2_of_e4m3x2(*reinterpret_cast<const uint16_t *>(w + k)));
+        const float s = sc[k / 128];
+        ss = fmaf(v.x * s, v.x * s, fmaf(v.y * s, v.y * s, ss));
+    }
+#pragma unroll
+    for (int o = 16; o; o >>= 1) ss += __shfl_xor_sync(0xFFFFFFFFu, ss, o);
+    if (lane == 0) atomicMax(reinterpret_cast<unsigned *>(row_max + set * 2 + which), __float_as_uint(ss));   // not negative: bits in the order of the values
+}
+
 // ------------------------------------------------------------------ router logits, tokens as fp16
 // exponent that brings a row's largest magnitude into [2^13, 2^14): what is 2^-27 of it keeps 11 bits in fp16
 __device__ __forceinline__ int fp16_exponent(float amax)
@@ -107,12 +135,21 @@ __device__ __forceinline__ int fp16_exponent(float amax)
 }
 __device__ __forceinline__ float exp2i(int e) { return __uint_as_float((uint32_t)(min(127, max(-126, e)) + 127) << 23); }
 
-constexpr int kRouteTokens = 32, kRouteSplits = 8;
-template <bool E4M3>
-__global__ void __launch_bounds__(kMoeThreads) moe_route_kernel(const __grid_constant__ MoeArgs A)
+// a hidden row's exponent: 2^-e brings |x|^2 |g| |u| (squares of the norms given), and so the row, below 2^15.  2 % cover the tokens' rounding.
+__device__ __forceinline__ int hidden_exponent(float x2, float g2, float u2)
 {
-    __shared__ float red[kMoeWarps][16][kRouteTokens + 1];
-    __shared__ float part[kMoeWarps];
+    const float b = 1.02f * x2 * sqrtf(g2) * sqrtf(u2);
+    if (!(b > 0.f)) return 0;
+    return max(-112, min(112, (int)(__float_as_uint(b) >> 23) - 127 + 1 - 15));
+}
+
+constexpr int kRouteSplits = 8, kRouteWarps = 8, kRouteThreads = kRouteWarps * 32;
+template <bool E4M3, int JT>
+__global__ void __launch_bounds__(kRouteThreads) moe_route_kernel(const __grid_constant__ MoeArgs A)
+{
+    constexpr int kTokens = 8 * JT;                          // of a block: route_tokens() on the host
+    __shared__ float red[kRouteWarps][16][kTokens + 1];
+    __shared__ float part[2][kRouteWarps];
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, q = lane & 3;
     const int n_gemm = A.e_tiles * A.h_splits * A.t_chunks;
     const int H = A.m.H, E = A.m.n_experts;
@@ -124,53 +161,51 @@ __global__ void __launch_bounds__(kMoeThreads) moe_route_kernel(const __grid_con
         const int et = blockIdx.x % A.e_tiles, r = blockIdx.x / A.e_tiles, hs = r % A.h_splits, tc = r / A.h_splits;
         const int groups = (H + 31) / 32;                    // 32 columns at a time
         const int k_lo = (int)((long long)groups * hs / A.h_splits), k_hi = (int)((long long)groups * (hs + 1) / A.h_splits);
-        const int t0 = tc * kRouteTokens, n = min(kRouteTokens, A.T - t0);
-        float c[kRouteTokens / 8][4];
+        const int t0 = tc * kTokens, n = min(kTokens, A.T - t0);
+        float c[JT][4];
 #pragma unroll
-        for (int j = 0; j < kRouteTokens / 8; j++) c[j][0] = c[j][1] = c[j][2] = c[j][3] = 0.f;
+        for (int j = 0; j < JT; j++) c[j][0] = c[j][1] = c[j][2] = c[j][3] = 0.f;
         const int r0 = et * 16 + g, r1 = r0 + 8;
 #pragma unroll 4
-        for (int kg = k_lo + warp; kg < k_hi; kg += kMoeWarps) {
+        for (int kg = k_lo + warp; kg < k_hi; kg += kRouteWarps) {
             const int k = kg * 32 + q * 8;
-            uint4 a = make_uint4(0, 0, 0, 0), b = a;
-            if (k < H) {
-                if (r0 < E) a = __ldg(reinterpret_cast<const uint4 *>(A.router + (int64_t)r0 * H + k));
-                if (r1 < E) b = __ldg(reinterpret_cast<const uint4 *>(A.router + (int64_t)r1 * H + k));
-            }
+            const uint4 zero = make_uint4(0, 0, 0, 0);
+            const uint4 a = k < H && r0 < E ? __ldg(reinterpret_cast<const uint4 *>(A.router + (int64_t)r0 * H + k)) : zero;
+            const uint4 b = k < H && r1 < E ? __ldg(reinterpret_cast<const uint4 *>(A.router + (int64_t)r1 * H + k)) : zero;
+            uint4 x[JT];
 #pragma unroll
-            for (int j = 0; j < kRouteTokens / 8; j++) {
-                if (j * 8 >= n) break;
-                uint4 x = make_uint4(0, 0, 0, 0);
-                if (k < H && j * 8 + g < n) x = __ldg(reinterpret_cast<const uint4 *>(A.x + (int64_t)(t0 + j * 8 + g) * A.xs + k));
-                mma16<Bf16>(c[j], a.x, b.x, a.y, b.y, x.x, x.y);
-                mma16<Bf16>(c[j], a.z, b.z, a.w, b.w, x.z, x.w);
+            for (int j = 0; j < JT; j++)
+                x[j] = k < H && j * 8 + g < n ? __ldg(reinterpret_cast<const uint4 *>(A.x + (int64_t)(t0 + j * 8 + g) * A.xs + k)) : zero;
+#pragma unroll
+            for (int j = 0; j < JT; j++) {
+                mma16<Bf16>(c[j], a.x, b.x, a.y, b.y, x[j].x, x[j].y);
+                mma16<Bf16>(c[j], a.z, b.z, a.w, b.w, x[j].z, x[j].w);
             }
         }
 #pragma unroll
-        for (int j = 0; j < kRouteTokens / 8; j++) {
+        for (int j = 0; j < JT; j++) {
             red[warp][g][j * 8 + 2 * q] = c[j][0];
             red[warp][g][j * 8 + 2 * q + 1] = c[j][1];
             red[warp][g + 8][j * 8 + 2 * q] = c[j][2];
             red[warp][g + 8][j * 8 + 2 * q + 1] = c[j][3];
         }
         __syncthreads();
-        for (int i = tid; i < 16 * n; i += kMoeThreads) {
+        for (int i = tid; i < 16 * n; i += kRouteThreads) {
             const int e = i & 15, t = i >> 4;
             float s = 0.f;
 #pragma unroll
-            for (int wv = 0; wv < kMoeWarps; wv++) s += red[wv][e][t];
+            for (int wv = 0; wv < kRouteWarps; wv++) s += red[wv][e][t];
             if (et * 16 + e < E) A.logits[((int64_t)hs * A.T + t0 + t) * E + et * 16 + e] = s;
         }
         return;
     }
     const int t = blockIdx.x - n_gemm;
     if constexpr (!E4M3) {
-        for (int k = tid * 8; k < A.Hk; k += kMoeThreads * 8)
+        for (int k = tid * 8; k < A.Hk; k += kRouteThreads * 8)
             *reinterpret_cast<uint4 *>(A.xh + (size_t)t * A.Hk + k) =
                 k < H ? *reinterpret_cast<const uint4 *>(A.x + (int64_t)t * A.xs + k) : make_uint4(0, 0, 0, 0);
     } else {
-    // token t as fp16 times a power of two; its pairs' maxima start at zero
-    for (int j = tid; j < A.choices; j += kMoeThreads) A.h_max[t * A.choices + j] = 0u;
+    // token t as fp16 times a power of two
     const int groups = (H + PF_SCALE_GROUP - 1) / PF_SCALE_GROUP;
     auto value8 = [&](int k, float (&v)[8]) {
         if (A.xq) {
@@ -194,23 +229,39 @@ __global__ void __launch_bounds__(kMoeThreads) moe_route_kernel(const __grid_con
             }
         }
     };
-    float m = 0.f;
-    for (int k = tid * 8; k < H; k += kMoeThreads * 8) {
+    float m = 0.f, ss = 0.f;
+    for (int k = tid * 8; k < H; k += kRouteThreads * 8) {
         float v[8];
         value8(k, v);
 #pragma unroll
-        for (int i = 0; i < 8; i++) m = fmaxf(m, fabsf(v[i]));
+        for (int i = 0; i < 8; i++) {
+            m = fmaxf(m, fabsf(v[i]));
+            ss = fmaf(v[i], v[i], ss);
+        }
     }
 #pragma unroll
-    for (int o = 16; o; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, o));
-    if (lane == 0) part[warp] = m;
+    for (int o = 16; o; o >>= 1) {
+        m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, o));
+        ss += __shfl_xor_sync(0xFFFFFFFFu, ss, o);
+    }
+    if (lane == 0) {
+        part[0][warp] = m;
+        part[1][warp] = ss;
+    }
     __syncthreads();
+    ss = 0.f;
 #pragma unroll
-    for (int i = 0; i < kMoeWarps; i++) m = fmaxf(m, part[i]);
+    for (int i = 0; i < kRouteWarps; i++) {
+        m = fmaxf(m, part[0][i]);
+        ss += part[1][i];
+    }
     const int e = fp16_exponent(m);
     const float down = exp2i(-e);
-    if (tid == 0) A.xh_scale[t] = exp2i(e);
-    for (int k = tid * 8; k < A.Hk; k += kMoeThreads * 8) {
+    if (tid == 0) {
+        A.xh_scale[t] = exp2i(e);
+        A.x_norm2[t] = ss;
+    }
+    for (int k = tid * 8; k < A.Hk; k += kRouteThreads * 8) {
         float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
         if (k < H) value8(k, v);
         *reinterpret_cast<uint4 *>(A.xh + (size_t)t * A.Hk + k) =
@@ -278,26 +329,80 @@ __device__ __forceinline__ void bulk_copy(uint32_t dst, const void *src, uint32_
     asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src), "r"(bytes), "r"(mbar) : "memory");
 }
 
-template <bool E4M3, int WM, int WK, int MI, int NT>
+// One warp chooses token t's experts: `keep` ([T][top_k], may be NULL) gets the indices, and the outputs too where `write`.
+template <int KEYS>
+__device__ __forceinline__ void choose(const MoeArgs &A, int t, int *keep, bool write)
+{
+    const int lane = threadIdx.x & 31, T = A.T, K = A.m.top_k, E = A.m.n_experts;
+    float v[KEYS];
+    uint32_t key[KEYS];
+#pragma unroll
+    for (int i = 0; i < KEYS; i++) v[i] = 0.f;
+#pragma unroll
+    for (int hs = 0; hs < kRouteSplits; hs++)                   // added in a fixed order
+#pragma unroll
+        for (int i = 0; i < KEYS; i++) {
+            const int e = i * 32 + lane;
+            v[i] += hs < A.h_splits && e < E ? A.logits[((int64_t)hs * T + t) * E + e] : 0.f;
+        }
+#pragma unroll
+    for (int i = 0; i < KEYS; i++) {
+        const uint32_t b = v[i] == v[i] ? __float_as_uint(v[i]) : 0xFF800000u;
+        key[i] = i * 32 + lane < E ? ((b >> 31) ? ~b : (b | 0x80000000u)) : 0u;      // order of the floats; 0 = not there, or taken
+    }
+    float top = 0.f, sum = 0.f, mine = 0.f;
+    int my_id = 0;
+    for (int j = 0; j < K; j++) {
+        uint32_t best = 0u, at = 0xFFFFFFFFu;
+#pragma unroll
+        for (int i = 0; i < KEYS; i++) best = max(best, key[i]);
+        const uint32_t all = __reduce_max_sync(0xFFFFFFFFu, best);
+#pragma unroll
+        for (int i = KEYS - 1; i >= 0; i--)
+            if (key[i] == all) at = i * 32 + lane;
+        at = __reduce_min_sync(0xFFFFFFFFu, at);
+#pragma unroll
+        for (int i = 0; i < KEYS; i++)
+            if (at == (uint32_t)(i * 32 + lane)) key[i] = 0u;
+        const float l = __uint_as_float((all >> 31) ? all & 0x7FFFFFFFu : ~all);
+        if (j == 0) top = l;
+        const float w = expf(l - top);
+        sum += w;
+        if (lane == j) {
+            mine = w;
+            my_id = (int)at;
+        }
+    }
+    if (lane < K) {
+        if (keep) keep[t * K + lane] = my_id;
+        if (write) {
+            A.ids[t * K + lane] = my_id;
+            A.weights[t * K + lane] = mine / sum;
+        }
+    }
+}
+
+template <bool E4M3, int NT>
 struct MoeShape {
     static constexpr int KW = E4M3 ? 128 : 64;
     static constexpr int PLANES = E4M3 ? 1 : 2;               // of the hidden activations
-    static constexpr int TM = WM * MI;                        // row tiles of an item
-    static constexpr int A_BYTES = kMoeWarps * MI * kSliceBytes;
-    static constexpr int PITCH = WK * KW * 2 + 64;            // a token row; 64 mod 128: two rows' quarters use all banks
-    static constexpr int B_BYTES = NT * PLANES * PITCH;
+    static constexpr int LWK = NT == 8 || (NT == 16 && !E4M3) ? 2 : 1;               // log2 of the fewest warps that share a row tile
+    static constexpr int TM = kMoeWarps >> LWK;               // row tiles of an item, at most
+    static constexpr int A_BYTES = kMoeWarps * kSliceBytes;
+    // a stage's token row, for 2^lwk slices; 64 mod 128: two rows' quarters use all banks
+    static constexpr __host__ __device__ int pitch(int lwk) { return (KW * 2 << lwk) + 64; }
+    static constexpr int B_BYTES = NT * PLANES * ((KW * 2 << LWK) + 64);
     static constexpr int STAGE = A_BYTES + B_BYTES;
-    static constexpr int RED = WK * TM * 16 * NT * 4;         // one item's partial sums
+    static constexpr int RED = kMoeWarps * 16 * NT * 4;       // one item's partial sums
     static constexpr int BUFS = RED > 16384 ? 1 : 2;
-    static constexpr int STAGES = NT == 8 ? 4 : 3;            // what 227 KB hold beside the partial sums and the longest list of pairs
+    static constexpr int STAGES = NT == 8 ? 5 : NT == 16 && E4M3 ? 4 : 3;      // what 227 KB hold beside the partial sums and the longest list of pairs
     static constexpr int FIXED = STAGES * STAGE + BUFS * RED;
-    static_assert(WM * WK == kMoeWarps, "one slice per warp and stage");
 };
 
-template <bool E4M3, int WM, int WK, int MI, int NT>
+template <bool E4M3, int NT>
 __global__ void __launch_bounds__(kMoeBlock, 1) moe_kernel(const __grid_constant__ MoeArgs A)
 {
-    using S = MoeShape<E4M3, WM, WK, MI, NT>;
+    using S = MoeShape<E4M3, NT>;
     using MT = typename std::conditional<E4M3, F16, Bf16>::type;
     constexpr int kStages = S::STAGES;
     extern __shared__ __align__(128) uint8_t smem[];
@@ -305,7 +410,6 @@ __global__ void __launch_bounds__(kMoeBlock, 1) moe_kernel(const __grid_constant
     __shared__ int meet_ok;
     __shared__ int n_active_s;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, q = lane & 3;
-    const int wm = warp / WK, wk = warp % WK;
     const int T = A.T, K = A.m.top_k, C = A.choices, E = A.m.n_experts, H = A.m.H;
     uint8_t *ring_p = smem;
     const uint32_t ring = smem_addr(ring_p);
@@ -315,66 +419,27 @@ __global__ void __launch_bounds__(kMoeBlock, 1) moe_kernel(const __grid_constant
     int *act = off + A.n_sets;                                                       // [n_sets] experts with tokens
     int *cum = act + A.n_sets;                                                       // [n_sets + 1] token chunks before an active expert
     uint16_t *list = reinterpret_cast<uint16_t *>(cum + A.n_sets + 1);               // [T * C] pairs by expert
+    unsigned *local = reinterpret_cast<unsigned *>(list + (T * C + 1) / 2 * 2);      // [T] which of a token's choices are here
     unsigned round = 0;
 
     // ---- the choice: one warp per token.  For few tokens each block makes all of it by itself, which saves a meeting.
-    const bool by_itself = T <= 2 * kMoeWarps;
+    const bool by_itself = T <= kMoeWarps;
     if (tid == 0) {
         for (int i = 0; i < kStages; i++) {
-            mbar_init(smem_addr(bars + i), 2);                   // full: the weights' and the tokens' announcements, and their bytes
+            mbar_init(smem_addr(bars + i), 2 * kCopyWarps);      // full: each copying warp's announcements of weights and of tokens, and their bytes
             mbar_init(smem_addr(bars + kStages + i), kMoeWarps);   // empty: the multiplying warps
         }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
-    if (warp < kMoeWarps)
-    for (int t = by_itself ? warp : warp * (int)gridDim.x + (int)blockIdx.x; t < T; t += by_itself ? kMoeWarps : kMoeWarps * (int)gridDim.x) {
-        uint32_t key[PF_MOE_MAX_EXPERTS / 32];
-#pragma unroll
-        for (int i = 0; i < PF_MOE_MAX_EXPERTS / 32; i++) {
-            key[i] = 0u;
-            const int e = i * 32 + lane;
-            if (i * 32 < E && e < E) {
-                float v[kRouteSplits], s = 0.f;                 // all in flight, added in a fixed order
-#pragma unroll
-                for (int hs = 0; hs < kRouteSplits; hs++) v[hs] = hs < A.h_splits ? A.logits[((int64_t)hs * T + t) * E + e] : 0.f;
-#pragma unroll
-                for (int hs = 0; hs < kRouteSplits; hs++) s += v[hs];
-                const uint32_t b = s == s ? __float_as_uint(s) : 0xFF800000u;
-                key[i] = (b >> 31) ? ~b : (b | 0x80000000u);      // order of the floats; 0 = taken
-            }
-        }
-        float top = 0.f, sum = 0.f, mine = 0.f;
-        int my_id = 0;
-        for (int j = 0; j < K; j++) {
-            uint32_t best = 0u;
-#pragma unroll
-            for (int i = 0; i < PF_MOE_MAX_EXPERTS / 32; i++) best = max(best, key[i]);
-            const uint32_t all = __reduce_max_sync(0xFFFFFFFFu, best);
-            uint32_t at = 0xFFFFFFFFu;
-#pragma unroll
-            for (int i = PF_MOE_MAX_EXPERTS / 32 - 1; i >= 0; i--)
-                if (key[i] == all) at = i * 32 + lane;
-            at = __reduce_min_sync(0xFFFFFFFFu, at);
-#pragma unroll
-            for (int i = 0; i < PF_MOE_MAX_EXPERTS / 32; i++)
-                if (at == (uint32_t)(i * 32 + lane)) key[i] = 0u;
-            const float l = __uint_as_float((all >> 31) ? all & 0x7FFFFFFFu : ~all);
-            if (j == 0) top = l;
-            const float w = expf(l - top);
-            sum += w;
-            if (lane == j) {
-                mine = w;
-                my_id = (int)at;
-            }
-        }
-        if (lane < K) {
-            if (by_itself) {
-                reinterpret_cast<int *>(red)[t * K + lane] = my_id;
-            }
-            if (!by_itself || blockIdx.x == 0) {
-                A.ids[t * K + lane] = my_id;
-                A.weights[t * K + lane] = mine / sum;
-            }
+    if (warp < kMoeWarps) {
+        const int t0 = by_itself ? warp : warp * (int)gridDim.x + (int)blockIdx.x, dt = by_itself ? kMoeWarps : kMoeWarps * (int)gridDim.x;
+        int *keep = by_itself ? reinterpret_cast<int *>(red) : nullptr;
+        const bool write = !by_itself || blockIdx.x == 0;
+        for (int t = t0; t < T; t += dt) {
+            if (E <= 64) choose<2>(A, t, keep, write);
+            else if (E <= 128) choose<4>(A, t, keep, write);
+            else if (E <= 256) choose<8>(A, t, keep, write);
+            else choose<16>(A, t, keep, write);
         }
     }
     if (by_itself) __syncthreads();
@@ -383,156 +448,244 @@ __global__ void __launch_bounds__(kMoeBlock, 1) moe_kernel(const __grid_constant
         return;
     }
 
-    // ---- pairs by expert
-    for (int i = tid; i < A.n_sets; i += kMoeBlock) cnt[i] = 0;
-    __syncthreads();
-    auto set_of = [&](int p) {               // expert of pair p on this GPU, -1 if it lives elsewhere
-        const int t = p / C, j = p - t * C;
-        if (j >= K) return A.m.n_local + j - K;
+    // ---- pairs by expert, in pair order within each: off and cnt of every expert (cnt: the end of its pairs), the experts that
+    // have any, the chunks of NT tokens before each of those, and which of a token's choices are here.  All blocks arrive at the same.
+    const int P = T * C;
+    // The experts of all tokens come first in the list, so that what is left for its end, cut into small pieces, has few tokens.
+    auto set_of = [&](int t, int j) {        // place of the expert of token t's choice j among this GPU's, n_sets if it lives elsewhere
+        if (j >= K) return j - K;
         const int e = (by_itself ? reinterpret_cast<const int *>(red)[t * K + j] : A.ids[t * K + j]) - A.m.first;
-        return e >= 0 && e < A.m.n_local ? e : -1;
+        return e >= 0 && e < A.m.n_local ? A.m.n_shared + e : A.n_sets;
     };
-    for (int p = tid; p < T * C; p += kMoeBlock) {
-        const int s = set_of(p);
-        if (s >= 0) atomicAdd(cnt + s, 1);
-    }
-    __syncthreads();
-    if (warp == 0) {                         // offsets, active experts, chunks: a scan by one warp
-        int o = 0, a = 0, c = 0;
-        for (int i0 = 0; i0 < A.n_sets; i0 += 32) {
-            const int i = i0 + lane, n = i < A.n_sets ? cnt[i] : 0, ch = (n + NT - 1) / NT;
-            int so = n, sc = ch;
+    uint16_t *set_at = reinterpret_cast<uint16_t *>(ring_p), *dealt = set_at + (P + 7) / 8 * 8;      // the ring is not in use yet
+    if (P <= kMoeBlock) {
+        // few pairs: a thread each, which counts the pairs that come before its own
+        if (tid < T) local[tid] = 0u;
+        if (tid < (P + 7) / 8 * 8) set_at[tid] = 0xFFFFu;
+        if (tid == 0) n_active_s = cum[0] = 0;
+        __syncthreads();
+        int s = A.n_sets;
+        if (tid < P) {
+            const int t = tid / C, j = tid - t * C;
+            s = set_of(t, j);
+            set_at[tid] = (uint16_t)s;
+            if (s < A.n_sets) atomicOr(local + t, 1u << j);
+        }
+        __syncthreads();
+        int before = 0, same = 0, rank = 0;
+        const bool here = s < A.n_sets;
+        if (here) {
+            for (int k = 0; k < P; k++) {
+                const int o = set_at[k];
+                before += o < s;
+                same += o == s;
+                rank += o == s && k < tid;
+            }
+            list[before + rank] = (uint16_t)tid;
+        }
+        if (tid < P) dealt[tid] = here && rank == 0 ? (uint16_t)((same + NT - 1) / NT) : (uint16_t)0;      // an expert's first pair stands for it
+        __syncthreads();
+        if (here && rank == 0) {
+            int at = 0, chunks = 0;
+            for (int k = 0; k < P; k++) {
+                const int d = dealt[k];
+                const bool less = d != 0 && set_at[k] < s;
+                at += less;
+                chunks += less ? d : 0;
+            }
+            off[s] = before;
+            cnt[s] = before + same;
+            act[at] = s;
+            cum[at + 1] = chunks + dealt[tid];
+            atomicAdd(&n_active_s, 1);
+        }
+        __syncthreads();
+    } else {
+        for (int i = tid; i < A.n_sets; i += kMoeBlock) cnt[i] = 0;
+        __syncthreads();
+        for (int t = tid; t < T; t += kMoeBlock) {
+            unsigned mask = 0u;
+            for (int j = 0; j < C; j++) {
+                const int s = set_of(t, j);
+                if (s == A.n_sets) continue;
+                atomicAdd(cnt + s, 1);
+                mask |= 1u << j;
+            }
+            local[t] = mask;
+        }
+        __syncthreads();
+        if (warp == 0) {                     // offsets, experts with pairs, chunks: a scan by one warp
+            int o = 0, a = 0, c = 0;
+            for (int i0 = 0; i0 < A.n_sets; i0 += 32) {
+                const int i = i0 + lane, n = i < A.n_sets ? cnt[i] : 0, ch = (n + NT - 1) / NT;
+                int so = n, sc = ch;
 #pragma unroll
-            for (int d = 1; d < 32; d <<= 1) {
-                const int u = __shfl_up_sync(0xFFFFFFFFu, so, d), v = __shfl_up_sync(0xFFFFFFFFu, sc, d);
-                if (lane >= d) {
-                    so += u;
-                    sc += v;
+                for (int d = 1; d < 32; d <<= 1) {
+                    const int u = __shfl_up_sync(0xFFFFFFFFu, so, d), v = __shfl_up_sync(0xFFFFFFFFu, sc, d);
+                    if (lane >= d) {
+                        so += u;
+                        sc += v;
+                    }
                 }
+                const unsigned live = __ballot_sync(0xFFFFFFFFu, n > 0);
+                if (i < A.n_sets) off[i] = cnt[i] = o + so - n;
+                if (n > 0) {
+                    const int at = a + __popc(live & ((1u << lane) - 1u));
+                    act[at] = i;
+                    cum[at + 1] = c + sc;
+                }
+                o += __shfl_sync(0xFFFFFFFFu, so, 31);
+                c += __shfl_sync(0xFFFFFFFFu, sc, 31);
+                a += __popc(live);
             }
-            const unsigned live = __ballot_sync(0xFFFFFFFFu, n > 0);
-            if (i < A.n_sets) off[i] = o + so - n;
-            if (n > 0) {
-                const int at = a + __popc(live & ((1u << lane) - 1u));
-                act[at] = i;
-                cum[at] = c + sc - ch;
+            if (lane == 0) {
+                cum[0] = 0;
+                n_active_s = a;
             }
-            o += __shfl_sync(0xFFFFFFFFu, so, 31);
-            c += __shfl_sync(0xFFFFFFFFu, sc, 31);
-            a += __popc(live);
         }
-        if (lane == 0) {
-            cum[a] = c;
-            n_active_s = a;
+        __syncthreads();
+        // dealt out in any order, then ranked by pair number within each expert
+        for (int t = tid; t < T; t += kMoeBlock)
+            for (int j = 0; j < C; j++) {
+                const int s = set_of(t, j);
+                if (s == A.n_sets) continue;
+                const int at = atomicAdd(cnt + s, 1);
+                dealt[at] = (uint16_t)(t * C + j);
+                set_at[at] = (uint16_t)s;
+            }
+        __syncthreads();                     // now cnt[s] is the end of expert s's pairs
+        for (int i = tid; i < (n_active_s ? cnt[act[n_active_s - 1]] : 0); i += kMoeBlock) {
+            const int s = set_at[i], p = dealt[i], lo = off[s], hi = cnt[s];
+            int rank = lo;
+            for (int k = lo; k < hi; k++) rank += dealt[k] < p;
+            list[rank] = (uint16_t)p;
         }
+        __syncthreads();
     }
-    __syncthreads();
-    // All blocks need the same order (a block takes some of an expert's chunks), so what the atomics dealt out in any order is
-    // ranked by pair number within each expert.
-    for (int i = tid; i < A.n_sets; i += kMoeBlock) cnt[i] = off[i];
-    __syncthreads();
-    uint16_t *dealt = reinterpret_cast<uint16_t *>(ring_p), *set_at = dealt + T * C;      // the ring is not in use yet
-    for (int p = tid; p < T * C; p += kMoeBlock) {
-        const int s = set_of(p);
-        if (s < 0) continue;
-        const int at = atomicAdd(cnt + s, 1);
-        dealt[at] = (uint16_t)p;
-        set_at[at] = (uint16_t)s;
-    }
-    __syncthreads();                         // now cnt[s] is the end of expert s's pairs
-    for (int i = tid; i < (n_active_s ? cnt[act[n_active_s - 1]] : 0); i += kMoeBlock) {
-        const int s = set_at[i], p = dealt[i];
-        int rank = off[s];
-        for (int k = off[s]; k < cnt[s]; k++) rank += dealt[k] < p;
-        list[rank] = (uint16_t)p;
-    }
-    __syncthreads();
+    auto weights_of = [&](int place) { return place < A.m.n_shared ? A.m.n_local + place : place - A.m.n_shared; };      // index in the weight tensors
     const int n_active = n_active_s, n_chunks = cum[n_active];
 
-    // ---- row tiles: item = (expert, group of WM row tiles, chunk of NT tokens), chunks fastest so that a tile's second reading hits the L2
-    struct Cursor {
-        int item, a, r, c, chunks, stage;
-        __device__ __forceinline__ void at(int i, int groups, const int *cum, int n_active)
-        {
-            item = i;
-            while (a < n_active && i >= groups * cum[a + 1]) a++;
-            if (a >= n_active) return;
-            chunks = cum[a + 1] - cum[a];
-            const int rest = i - groups * cum[a];
-            r = rest / chunks;
-            c = rest - r * chunks;
-        }
+    // ---- The work of a product is a list: for every chunk of up to NT tokens of an expert, that expert's row tiles.  Blocks take TM
+    // tiles of it in turn, so that each gets its part of the chunks that cost more (more tokens), as long as there are TM for every
+    // block; what is left is cut into equal pieces.  (Equal contiguous pieces of the whole list: the blocks that held the experts of all
+    // tokens took 1.6 times as long as the average.)  A matrix that several chunks read comes from HBM once and then from the L2.
+    // An item's row tiles are dealt to groups of 2^lwk warps, which split the columns: with few tiles left a group is larger, as far as
+    // the stage holds its token rows, so that the warps and the stages stay full.
+    auto shape_of = [&](int tiles, int rows, int ks) {
+        int lwk = tiles > 4 ? 1 : tiles > 2 ? 2 : tiles > 1 ? 3 : 4;
+        while (lwk > S::LWK && (rows * S::pitch(lwk) > S::B_BYTES || (1 << lwk) >= 2 * ks)) lwk--;
+        return max(lwk, S::LWK);
     };
-    const int groups1 = (A.f_tiles + S::TM - 1) / S::TM, groups2 = (A.h_tiles + S::TM - 1) / S::TM;
-    const int stages1 = (A.ks_up + WK - 1) / WK, stages2 = (A.ks_down + WK - 1) / WK;
-    const int items1 = groups1 * n_chunks, items2 = groups2 * n_chunks;
+    struct Cursor {
+        int at, end, part, a, c, tile, n, tokens, lwk, stages, stage;   // tiles at .. end - 1 of the list are this block's part number `part`;
+                                                                // item: tiles tile .. tile + n - 1 of chunk c (of `tokens`) of active expert a
+    };
+    auto item = [&](bool second, Cursor &c) {
+        const int ks = second ? A.ks_down : A.ks_up;
+        c.n = min((second ? A.h_tiles : A.f_tiles) - c.tile, c.end - c.at);
+        c.tokens = min(NT, cnt[act[c.a]] - off[act[c.a]] - c.c * NT);
+        c.lwk = shape_of(c.n, second ? c.tokens * S::PLANES : c.tokens, ks);
+        c.stages = (ks + (1 << c.lwk) - 1) >> c.lwk;
+        c.stage = 0;
+    };
+    auto take = [&](bool second, Cursor &c) {                   // the next part, if there is one
+        const int tiles = second ? A.h_tiles : A.f_tiles, all = n_chunks * tiles, grid = gridDim.x, turns = all / (grid * S::TM);
+        if (c.part < turns) {
+            c.at = (c.part * grid + blockIdx.x) * S::TM;
+            c.end = c.at + S::TM;
+        } else {
+            const int done = turns * grid * S::TM, left = all - done;           // left < grid * TM
+            c.at = done + left * (int)blockIdx.x / grid;
+            c.end = c.part == turns ? done + left * ((int)blockIdx.x + 1) / grid : c.at;
+        }
+        c.part++;
+        if (c.at >= c.end) return;
+        const int v = c.at / tiles;
+        c.tile = c.at - v * tiles;
+        while (cum[c.a + 1] <= v) c.a++;
+        c.c = v - cum[c.a];
+        item(second, c);
+    };
+    auto begin = [&](bool second, Cursor &c) {
+        c.part = c.a = 0;
+        take(second, c);
+    };
+    auto more = [](const Cursor &c) { return c.at < c.end; };
+    auto next = [&](bool second, Cursor &c) {
+        c.at += c.n;
+        if (c.at >= c.end) return take(second, c);
+        c.tile = 0;                                             // a part that runs into the next chunk
+        if (++c.c == cum[c.a + 1] - cum[c.a]) {
+            c.c = 0;
+            c.a++;
+        }
+        item(second, c);
+    };
     const int grid = gridDim.x;
 
-    // ---- the stream: positions 0 .. n1 - 1 are stages of the first product, n1 .. n1 + n2 - 1 of the second; position p uses
-    // ring slot p % kStages
-    const int mine1 = items1 > (int)blockIdx.x ? (items1 - (int)blockIdx.x + grid - 1) / grid : 0;
-    const int mine2 = items2 > (int)blockIdx.x ? (items2 - (int)blockIdx.x + grid - 1) / grid : 0;
-    const int n1 = mine1 * stages1, n2 = mine2 * stages2;
+    // ---- the stream: a position per stage, those of the first product and then those of the second; position p uses ring slot p % kStages
     const uint32_t full = smem_addr(bars), empty = full + kStages * 8;
     asm volatile("fence.proxy.async;" ::: "memory");            // the ring held `dealt`: bulk copies write it from here on
     __syncthreads();                                            // barriers are set up; `red` held the ids
 
-    if (warp == kMoeWarps) {                                    // ================= the copying warp
-        // What a stage costs this warp bounds the whole stream, so everything that belongs to an item is worked out once: where its
-        // tiles begin, and for each lane its (up to ROWS) token rows.
-        constexpr int ROWS = (NT * S::PLANES + 31) / 32;
+    if (warp >= kMoeWarps) {                                    // ================= the copying warps
+        // Issuing a copy takes a warp 100 to 200 cycles, and at full HBM speed a stage lasts 1400: one warp alone held the stream at
+        // 5.4 TB/s.  So the copies of a stage (TM runs of weights, a row for each token) are dealt to kCopyWarps warps, and what
+        // belongs to an item is worked out once.
+        const int cw = warp - kMoeWarps;
+        constexpr int TILES = (S::TM + kCopyWarps - 1) / kCopyWarps;                              // tiles cw, cw + kCopyWarps, ..
+        constexpr int ROWS = (NT * S::PLANES + 32 * kCopyWarps - 1) / (32 * kCopyWarps);          // rows cw + kCopyWarps * (lane + 32 i)
         struct Feed {
             Cursor c;
-            const uint8_t *weights;
-            const uint16_t *row[ROWS];
-            int tiles, rows;
+            const uint8_t *weights;              // of tile cw, this stage
+            const uint16_t *row[ROWS];           // this stage
+            int tiles, rows;                     // this warp's share
         };
         auto set_up = [&](bool second, Feed &f) {
             const Cursor &c = f.c;
-            if (c.a >= n_active) return;
-            const int e = act[c.a], first = off[e] + c.c * NT, n = min(NT, cnt[e] - first);
-            f.weights = A.packed + (size_t)e * A.set_bytes + (second ? A.down_at : 0) + (size_t)(c.r * S::TM) * (second ? A.ks_down : A.ks_up) * kSliceBytes;
-            f.tiles = min(S::TM, (second ? A.h_tiles : A.f_tiles) - c.r * S::TM);
-            f.rows = second ? n * S::PLANES : n;
+            if (!more(c)) return;
+            const int e = act[c.a], first = off[e] + c.c * NT, n = c.tokens;
+            f.weights = A.packed + (size_t)weights_of(e) * A.set_bytes + (second ? A.down_at : 0) + (size_t)(c.tile + cw) * (second ? A.ks_down : A.ks_up) * kSliceBytes;
+            f.tiles = (c.n + kCopyWarps - 1 - cw) / kCopyWarps;
+            f.rows = ((second ? n * S::PLANES : n) + kCopyWarps - 1 - cw) / kCopyWarps;
 #pragma unroll
             for (int i = 0; i < ROWS; i++) {
-                const int r = i * 32 + lane;
-                if (r >= f.rows) continue;
+                if (i * 32 + lane >= f.rows) continue;
+                const int r = cw + kCopyWarps * (i * 32 + lane);
                 const int p = list[first + (second ? r / S::PLANES : r)];
                 f.row[i] = second ? A.hop + ((size_t)p * S::PLANES + r % S::PLANES) * A.Fk : A.xh + (size_t)(p / C) * A.Hk;
             }
         };
-        auto begin = [&](bool second, Feed &f) {
-            f.c.a = f.c.stage = 0;
-            f.c.at(blockIdx.x, second ? groups2 : groups1, cum, n_active);
-            set_up(second, f);
-        };
         auto advance = [&](bool second, Feed &f) {
-            if (++f.c.stage < (second ? stages2 : stages1)) return;
-            f.c.stage = 0;
-            f.c.at(f.c.item + grid, second ? groups2 : groups1, cum, n_active);
+            if (++f.c.stage < f.c.stages) {
+                f.weights += kSliceBytes << f.c.lwk;
+#pragma unroll
+                for (int i = 0; i < ROWS; i++) f.row[i] += S::KW << f.c.lwk;
+                return;
+            }
+            next(second, f.c);
             set_up(second, f);
         };
-        // full barrier of a stage: one arrival announces the weights' bytes, one the tokens'
+        // full barrier of a stage: each copying warp announces its weights' bytes in one arrival and its tokens' in another
         auto load_weights = [&](bool second, const Feed &f, int slot) {
             if (lane != 0) return;
-            const int ks = second ? A.ks_down : A.ks_up, s0 = f.c.stage * WK;
-            const uint32_t bytes = (uint32_t)(min(WK, ks - s0) * kSliceBytes);
+            const int ks = second ? A.ks_down : A.ks_up;
+            const uint32_t bytes = (uint32_t)(min(1 << f.c.lwk, ks - (f.c.stage << f.c.lwk)) * kSliceBytes);
             mbar_expect(full + slot * 8, f.tiles * bytes);
 #pragma unroll
-            for (int i = 0; i < S::TM; i++)
+            for (int i = 0; i < TILES; i++)
                 if (i < f.tiles)
-                    bulk_copy(ring + slot * S::STAGE + i * WK * kSliceBytes, f.weights + ((size_t)i * ks + s0) * kSliceBytes, bytes, full + slot * 8);
+                    bulk_copy(ring + slot * S::STAGE + ((cw + i * kCopyWarps) * kSliceBytes << f.c.lwk), f.weights + (size_t)(i * kCopyWarps) * ks * kSliceBytes,
+                              bytes, full + slot * 8);
         };
         auto load_tokens = [&](bool second, const Feed &f, int slot) {
-            const int s0 = f.c.stage * WK;
-            const uint32_t bytes = (uint32_t)(min(WK, (second ? A.ks_down : A.ks_up) - s0) * S::KW * 2);
+            const uint32_t bytes = (uint32_t)(min(1 << f.c.lwk, (second ? A.ks_down : A.ks_up) - (f.c.stage << f.c.lwk)) * S::KW * 2);
             if (lane == 0) mbar_expect(full + slot * 8, f.rows * bytes);
             __syncwarp();
 #pragma unroll
             for (int i = 0; i < ROWS; i++)
                 if (i * 32 + lane < f.rows)
-                    bulk_copy(ring + slot * S::STAGE + S::A_BYTES + (i * 32 + lane) * S::PITCH, f.row[i] + s0 * S::KW, bytes, full + slot * 8);
+                    bulk_copy(ring + slot * S::STAGE + S::A_BYTES + (cw + kCopyWarps * (i * 32 + lane)) * S::pitch(f.c.lwk), f.row[i], bytes, full + slot * 8);
         };
         bool ok = true;
         int pos = 0, slot = 0;
@@ -549,23 +702,26 @@ __global__ void __launch_bounds__(kMoeBlock, 1) moe_kernel(const __grid_constant
             }
         };
         Feed f;
-        begin(false, f);
-        while (pos < n1 && next_slot()) {
+        begin(false, f.c);
+        set_up(false, f);
+        while (more(f.c) && next_slot()) {
             load_weights(false, f, slot);
             load_tokens(false, f, slot);
             filled();
             advance(false, f);
         }
-        begin(true, f);
+        begin(true, f.c);
+        set_up(true, f);
         Feed late = f;                                          // tokens of the second product follow the meeting
+        const int n1 = pos;                                     // (after a failed wait it does not matter)
         int pos_b = pos, slot_b = slot;
-        while (ok && pos < n1 + n2 && pos < n1 + kStages && next_slot()) {
+        while (ok && more(f.c) && pos < n1 + kStages && next_slot()) {
             load_weights(true, f, slot);
             filled();
             advance(true, f);
         }
-        const unsigned target = round + gridDim.x * (E4M3 ? 2u : 1u);
-        if (ok && n2 > 0) ok = arrive_and_poll(A.ctl, target, false);
+        const unsigned target = round + gridDim.x;
+        if (ok && more(late.c)) ok = arrive_and_poll(A.ctl, target, false);
         __syncwarp();
         asm volatile("fence.proxy.async;" ::: "memory");
         for (; ok && pos_b < pos; pos_b++) {
@@ -573,7 +729,7 @@ __global__ void __launch_bounds__(kMoeBlock, 1) moe_kernel(const __grid_constant
             advance(true, late);
             slot_b = slot_b + 1 == kStages ? 0 : slot_b + 1;
         }
-        while (ok && pos < n1 + n2 && next_slot()) {
+        while (ok && more(f.c) && next_slot()) {
             load_weights(true, f, slot);
             load_tokens(true, f, slot);
             filled();
@@ -581,7 +737,7 @@ __global__ void __launch_bounds__(kMoeBlock, 1) moe_kernel(const __grid_constant
         }
         // nothing may be in flight when the block ends; after a wait that ran out, the stages without tokens are closed first
         if (!ok) {
-            for (; pos_b < pos && pos_b >= n1; pos_b++) {
+            for (; pos_b < pos; pos_b++) {
                 if (lane == 0) mbar_arrive(full + slot_b * 8);
                 slot_b = slot_b + 1 == kStages ? 0 : slot_b + 1;
             }
@@ -592,97 +748,85 @@ __global__ void __launch_bounds__(kMoeBlock, 1) moe_kernel(const __grid_constant
     }
 
     // ===================================================== the multiplying warps
-    float acc[MI][NT / 8][4], scale0[MI], scale1[MI];
+    float acc[NT / 8][4], scale0 = 0.f, scale1 = 0.f;
     int slot = 0;
     unsigned parity = 0;
     bool ok = true;
-    auto clear = [&](float (&v)[MI][NT / 8][4]) {
-#pragma unroll
-        for (int i = 0; i < MI; i++)
-#pragma unroll
-            for (int j = 0; j < NT / 8; j++) v[i][j][0] = v[i][j][1] = v[i][j][2] = v[i][j][3] = 0.f;
-    };
-    auto multiply = [&](bool second, const Cursor &c, int n) {  // this warp's slices of the stage into acc
-        const int tiles = second ? A.h_tiles : A.f_tiles, ks = second ? A.ks_down : A.ks_up;
-        const int tile = c.r * S::TM + wm * MI, s = c.stage * WK + wk;
-        const bool live = tile < tiles && s < ks;               // a second tile past the end multiplies old bytes of the ring; nobody reads the rows
-        float s0[MI], s1[MI];
+    // This warp's slice of the stage into acc, JT column blocks of tokens; what is known at compile time leaves no branch between the
+    // loads and the products.
+    auto multiply = [&](auto second_, auto jt_, const Cursor &c) {
+        constexpr bool second = decltype(second_)::value;
+        constexpr int JT = decltype(jt_)::value, CH = E4M3 && JT <= 2 ? 2 : 1;
+        const int ks = second ? A.ks_down : A.ks_up, wm = warp >> c.lwk, wk = warp & ((1 << c.lwk) - 1), s = (c.stage << c.lwk) + wk;
+        const bool live = wm < c.n && s < ks;
+        float s0 = 1.f, s1 = 1.f;
         if (E4M3) {
             if (c.stage % 32 == 0) {                            // block scales of 32 stages, a stage a lane
-                const int mine = (c.stage + lane) * WK + wk;
+                const int mine = ((c.stage + lane) << c.lwk) + wk, tile = c.tile + wm;
+                const bool any = wm < c.n && mine < ks;
                 const int kb_n = second ? (A.m.F + 127) / 128 : (H + 127) / 128;
-#pragma unroll
-                for (int i = 0; i < MI; i++) {
-                    const bool any = tile + i < tiles && mine < ks;
-                    if (second) {
-                        scale0[i] = any ? __ldg(A.ds + ((size_t)act[c.a] * ((H + 127) / 128) + (tile + i) / 8) * kb_n + mine) : 0.f;
-                    } else {
-                        const size_t at = ((size_t)act[c.a] * ((A.m.F + 127) / 128) + (tile + i) / 16) * kb_n + mine;
-                        scale0[i] = any ? __ldg(A.gs + at) : 0.f;
-                        scale1[i] = any ? __ldg(A.us + at) : 0.f;
-                    }
+                if (second) {
+                    scale0 = any ? __ldg(A.ds + ((size_t)weights_of(act[c.a]) * ((H + 127) / 128) + tile / 8) * kb_n + mine) : 0.f;
+                } else {
+                    const size_t at = ((size_t)weights_of(act[c.a]) * ((A.m.F + 127) / 128) + tile / 16) * kb_n + mine;
+                    scale0 = any ? __ldg(A.gs + at) : 0.f;
+                    scale1 = any ? __ldg(A.us + at) : 0.f;
                 }
             }
-#pragma unroll
-            for (int i = 0; i < MI; i++) {
-                s0[i] = __shfl_sync(0xFFFFFFFFu, scale0[i], c.stage % 32);
-                s1[i] = second ? s0[i] : __shfl_sync(0xFFFFFFFFu, scale1[i], c.stage % 32);
-            }
+            s0 = __shfl_sync(0xFFFFFFFFu, scale0, c.stage % 32);
+            s1 = second ? s0 : __shfl_sync(0xFFFFFFFFu, scale1, c.stage % 32);
         }
         if (ok) ok = mbar_wait(full + slot * 8, parity);
         if (live && ok) {
-            const uint32_t wa = ring + slot * S::STAGE + (wm * MI * WK + wk) * kSliceBytes + lane * 16;
-            const int planes = second ? S::PLANES : 1;
-            const uint32_t tb = ring + slot * S::STAGE + S::A_BYTES + g * (planes * S::PITCH) + wk * S::KW * 2 + q * 16;
-            float sub[MI][NT / 8][4];
-            if (E4M3) clear(sub);
-            float (&sum)[MI][NT / 8][4] = E4M3 ? sub : acc;
+            constexpr int planes = second ? S::PLANES : 1;
+            const int pitch = S::pitch(c.lwk);
+            const uint32_t wa = ring + slot * S::STAGE + warp * kSliceBytes + lane * 16;
+            // a column without a token reads the last token's row: nothing outside the stage's rows is touched, nobody reads its sums
+            uint32_t tb[JT];
+#pragma unroll
+            for (int j = 0; j < JT; j++)
+                tb[j] = ring + slot * S::STAGE + S::A_BYTES + min(j * 8 + g, c.tokens - 1) * planes * pitch + wk * S::KW * 2 + q * 16;
+            float sub[CH][NT / 8][4];                           // a block scale's part
+            float (&sum)[NT / 8][4] = E4M3 ? sub[0] : acc, (&sum2)[NT / 8][4] = E4M3 ? sub[CH - 1] : acc;
+            if (E4M3)
+#pragma unroll
+            for (int x = 0; x < CH; x++)
+#pragma unroll
+                for (int j = 0; j < JT; j++) sub[x][j][0] = sub[x][j][1] = sub[x][j][2] = sub[x][j][3] = 0.f;
 #pragma unroll
             for (int kg = 0; kg < S::KW / 32; kg++) {
-                uint32_t a[MI][2][4];
+                uint32_t a[2][4];
+                if (E4M3) {
+                    const uint4 v = lds128(wa + kg * 512);
+                    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
-                for (int t = 0; t < MI; t++) {
-                    if (E4M3) {
-                        const uint4 v = lds128(wa + t * WK * kSliceBytes + kg * 512);
-                        const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+                    for (int i = 0; i < 4; i++) {
+                        a[i >> 1][2 * (i & 1)] = f16x2_of_e4m3x2(w[i]);
+                        a[i >> 1][2 * (i & 1) + 1] = f16x2_of_e4m3x2(w[i] >> 16);
+                    }
+                } else {
 #pragma unroll
-                        for (int i = 0; i < 4; i++) {
-                            a[t][i >> 1][2 * (i & 1)] = f16x2_of_e4m3x2(w[i]);
-                            a[t][i >> 1][2 * (i & 1) + 1] = f16x2_of_e4m3x2(w[i] >> 16);
-                        }
-                    } else {
-#pragma unroll
-                        for (int i = 0; i < 2; i++) {
-                            const uint4 v = lds128(wa + t * WK * kSliceBytes + (2 * kg + i) * 512);
-                            a[t][i][0] = v.x; a[t][i][1] = v.y; a[t][i][2] = v.z; a[t][i][3] = v.w;
-                        }
+                    for (int i = 0; i < 2; i++) {
+                        const uint4 v = lds128(wa + (2 * kg + i) * 512);
+                        a[i][0] = v.x; a[i][1] = v.y; a[i][2] = v.z; a[i][3] = v.w;
                     }
                 }
 #pragma unroll
-                for (int j = 0; j < NT / 8; j++) {
-                    if (NT > 8 && j * 8 >= n) break;
+                for (int j = 0; j < JT; j++)
+#pragma unroll
                     for (int pl = 0; pl < planes; pl++) {
-                        const uint4 b = lds128(tb + (j * 8 * planes + pl) * S::PITCH + kg * 64);
-#pragma unroll
-                        for (int t = 0; t < MI; t++) mma16<MT>(sum[t][j], a[t][0][0], a[t][0][1], a[t][0][2], a[t][0][3], b.x, b.y);
-#pragma unroll
-                        for (int t = 0; t < MI; t++) mma16<MT>(sum[t][j], a[t][1][0], a[t][1][1], a[t][1][2], a[t][1][3], b.z, b.w);
+                        const uint4 b = lds128(tb[j] + pl * pitch + kg * 64);
+                        mma16<MT>(sum[j], a[0][0], a[0][1], a[0][2], a[0][3], b.x, b.y);
+                        mma16<MT>(sum2[j], a[1][0], a[1][1], a[1][2], a[1][3], b.z, b.w);
                     }
-                }
             }
-            if (E4M3) {
+            if (E4M3)
 #pragma unroll
-                for (int j = 0; j < NT / 8; j++) {
-                    if (NT > 8 && j * 8 >= n) break;
+            for (int x = 0; x < CH; x++)
 #pragma unroll
-                    for (int t = 0; t < MI; t++) {
-                        acc[t][j][0] = fmaf(sub[t][j][0], s0[t], acc[t][j][0]);
-                        acc[t][j][1] = fmaf(sub[t][j][1], s0[t], acc[t][j][1]);
-                        acc[t][j][2] = fmaf(sub[t][j][2], s1[t], acc[t][j][2]);
-                        acc[t][j][3] = fmaf(sub[t][j][3], s1[t], acc[t][j][3]);
-                    }
-                }
-            }
+                for (int j = 0; j < JT; j++)
+#pragma unroll
+                    for (int i = 0; i < 4; i++) acc[j][i] = fmaf(sub[x][j][i], i < 2 ? s0 : s1, acc[j][i]);
         }
         __syncwarp();
         if (lane == 0) mbar_arrive(empty + slot * 8);
@@ -691,33 +835,44 @@ __global__ void __launch_bounds__(kMoeBlock, 1) moe_kernel(const __grid_constant
             parity ^= 1u;
         }
     };
-    // The WK warps' partial sums meet in `red` ([wk][row][token]).  Where two buffers fit, two halves of the warps take turns: one
-    // finishes an item while the other already multiplies the next.  A warp puts its sums into a buffer again only after it has waited for,
-    // or finished, the item in between, and that item's barrier has seen every warp finish with the buffer.  With one buffer
-    // all warps finish every item.
+    auto run_item = [&](auto second_, Cursor &c, int n) {       // an item's stages, for as many column blocks as it has tokens
+#pragma unroll
+        for (int j = 0; j < NT / 8; j++) acc[j][0] = acc[j][1] = acc[j][2] = acc[j][3] = 0.f;
+        if (NT == 8 || n <= 8) {
+            for (; c.stage < c.stages; c.stage++) multiply(second_, std::integral_constant<int, 1>(), c);
+        } else if (NT == 16 || n <= 16) {
+            for (; c.stage < c.stages; c.stage++) multiply(second_, std::integral_constant<int, (NT < 16 ? 1 : 2)>(), c);
+        } else {
+            for (; c.stage < c.stages; c.stage++) multiply(second_, std::integral_constant<int, NT / 8>(), c);
+        }
+    };
+    // The warps' partial sums meet in `red` ([warp][row][token]).  Where two buffers fit, two halves of the warps take turns: one
+    // finishes an item while the other already multiplies the next.  Before a warp puts its sums into a buffer again, every warp has
+    // finished reading it: a warp of the other half has waited at the barrier of the item in between, where each reader arrives after it
+    // is done, and the readers' own half meets once more.  With one buffer all warps finish every item.
     constexpr int FINISH = S::BUFS == 2 ? kMoeThreads / 2 : kMoeThreads;
     const int half = warp / (kMoeWarps / 2), htid = tid % FINISH;
     int turn = 0;
     const float *r_get = red;
     auto put_partials = [&]() {                                 // true: this warp finishes the item, with FINISH - 1 other threads
         float *buf = red + turn * (S::RED / 4);
+        const bool mine = S::BUFS == 1 || turn == half;
         if (S::BUFS == 1) bar<2, kMoeThreads>();                // everyone has finished the item before
+        else if (mine && half == 0) bar<4, FINISH>();
+        else if (mine) bar<5, FINISH>();
 #pragma unroll
-        for (int t = 0; t < MI; t++)
-#pragma unroll
-            for (int j = 0; j < NT / 8; j++) {
-                float *r = buf + ((wk * S::TM + wm * MI + t) * 16 + g) * NT + j * 8 + 2 * q;
-                r[0] = acc[t][j][0];
-                r[1] = acc[t][j][1];
-                r[8 * NT] = acc[t][j][2];
-                r[8 * NT + 1] = acc[t][j][3];
-            }
+        for (int j = 0; j < NT / 8; j++) {
+            float *r = buf + (warp * 16 + g) * NT + j * 8 + 2 * q;
+            r[0] = acc[j][0];
+            r[1] = acc[j][1];
+            r[8 * NT] = acc[j][2];
+            r[8 * NT + 1] = acc[j][3];
+        }
         r_get = buf;
         if (S::BUFS == 1) {
             bar<1, kMoeThreads>();
             return true;
         }
-        const bool mine = turn == half;
         if (turn == 0) {
             if (mine) bar<1, kMoeThreads>(); else bar_arrive<1, kMoeThreads>();
         } else {
@@ -726,95 +881,75 @@ __global__ void __launch_bounds__(kMoeBlock, 1) moe_kernel(const __grid_constant
         turn ^= 1;
         return mine;
     };
-    auto total = [&](int row, int col) {
+    auto total = [&](int lwk, int tile, int row, int col) {     // row of the item's tile
         float v = 0.f;
-#pragma unroll
-        for (int i = 0; i < WK; i++) v += r_get[(i * S::TM * 16 + row) * NT + col];
+        for (int i = 0; i < (1 << lwk); i++) v += r_get[(((tile << lwk) + i) * 16 + row) * NT + col];
         return v;
     };
 
     Cursor c;
-    c.a = c.stage = 0;
-    c.at(blockIdx.x, groups1, cum, n_active);
-    for (int it = 0; it < mine1; it++) {
-        const int e = act[c.a], first = off[e] + c.c * NT, n = min(NT, cnt[e] - first);
-        clear(acc);
-        for (c.stage = 0; c.stage < stages1; c.stage++) multiply(false, c, n);
+    for (begin(false, c); more(c); next(false, c)) {
+        const int e = act[c.a], first = off[e] + c.c * NT, n = c.tokens;
+        run_item(std::false_type(), c, n);
         constexpr int FR = 8 * S::TM;                              // hidden units of the item
         const bool mine = put_partials();
-        for (int i = htid; mine && i < (FR * n + 31) / 32 * 32; i += FINISH) {
-            const int col = i / FR, fr = i - col * FR, f = c.r * FR + fr;
-            float h = 0.f;
-            int p = 0;
-            if (col < n) {
-                const int row = (fr >> 3) * 16 + (fr & 7);
-                p = list[first + col];
-                float gate = total(row, col), up = total(row + 8, col);
-                if (E4M3) {
-                    const float xs = A.xh_scale[p / C];
-                    gate *= xs;
-                    up *= xs;
-                }
-                if (f < A.Fp) {
-                    h = gate / (1.f + expf(-gate)) * up;
-                    if (E4M3) {
-                        A.h32[(size_t)p * A.Fp + f] = h;
-                    } else {
-                        const uint32_t hi = bf16x2_of(h, 0.f) & 0xFFFFu;
-                        uint16_t *dst = A.hop + (size_t)p * 2 * A.Fk + f;
-                        dst[0] = (uint16_t)hi;
-                        dst[A.Fk] = (uint16_t)bf16x2_of(h - __uint_as_float(hi << 16), 0.f);
-                    }
-                }
-            }
+        float g2 = 0.f, u2 = 0.f;
+        if (E4M3 && mine) {
+            g2 = __ldg(A.row_max + weights_of(e) * 2);
+            u2 = __ldg(A.row_max + weights_of(e) * 2 + 1);
+        }
+        for (int i = htid; mine && i < FR * n; i += FINISH) {
+            const int col = i / FR, fr = i - col * FR, f = c.tile * 8 + fr;
+            if (fr >= c.n * 8) continue;
+            const int p = list[first + col];
+            float gate = total(c.lwk, fr >> 3, fr & 7, col), up = total(c.lwk, fr >> 3, (fr & 7) + 8, col);
             if (E4M3) {
-                unsigned m = __float_as_uint(h) & 0x7FFFFFFFu;  // order of the magnitudes, infinity and NaN above all
-#pragma unroll
-                for (int o = (FR < 32 ? FR : 32) / 2; o; o >>= 1) m = max(m, __shfl_xor_sync(0xFFFFFFFFu, m, o));
-                if (fr % 32 == 0 && col < n) atomicMax(A.h_max + p, m);   // a maximum: the order does not matter
+                const float xs = A.xh_scale[p / C];
+                gate *= xs;
+                up *= xs;
+            }
+            const float h = gate / (1.f + expf(-gate)) * up;
+            if (E4M3) {
+                A.hop[(size_t)p * A.Fk + f] = (uint16_t)f16x2_of(h * exp2i(-hidden_exponent(A.x_norm2[p / C], g2, u2)), 0.f);
+            } else {
+                const uint32_t hi = bf16x2_of(h, 0.f) & 0xFFFFu;
+                uint16_t *dst = A.hop + (size_t)p * 2 * A.Fk + f;
+                dst[0] = (uint16_t)hi;
+                dst[A.Fk] = (uint16_t)bf16x2_of(h - __uint_as_float(hi << 16), 0.f);
             }
         }
-        if (!E4M3 && mine && c.r == groups1 - 1) {              // zeros behind F
-            const int pad = A.Fk - A.Fp;
-            for (int i = htid; i < pad * n * 2; i += FINISH)
-                A.hop[((size_t)list[first + i / (2 * pad)] * 2 + i / pad % 2) * A.Fk + A.Fp + i % pad] = 0;
+        if (mine && c.tile + c.n == A.f_tiles) {                // zeros behind F
+            const int pad = A.Fk - A.Fp, rows = n * S::PLANES;
+            for (int i = htid; i < pad * rows; i += FINISH) {
+                const int r = i / pad;
+                A.hop[((size_t)list[first + r / S::PLANES] * S::PLANES + r % S::PLANES) * A.Fk + A.Fp + i - r * pad] = 0;
+            }
         }
-        c.at(c.item + grid, groups1, cum, n_active);
     }
 
     // ---- all hidden activations are there
     ok = meet<3, kMoeThreads>(A.ctl, round, &meet_ok) && ok;
-    if (E4M3) {                                                 // as fp16 times a power of two per pair
-        const int quads = A.Fk / 4, n_pairs = n_active ? cnt[act[n_active - 1]] : 0;
-        for (long long i = (long long)blockIdx.x * kMoeThreads + tid; i < (long long)n_pairs * quads; i += (long long)grid * kMoeThreads) {
-            const int p = list[i / quads], f = (int)(i % quads) * 4;
-            float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-            if (f < A.Fp) v = *reinterpret_cast<const float4 *>(A.h32 + (size_t)p * A.Fp + f);
-            const float d = exp2i(-fp16_exponent(__uint_as_float(A.h_max[p])));
-            *reinterpret_cast<uint2 *>(A.hop + (size_t)p * A.Fk + f) = make_uint2(f16x2_of(v.x * d, v.y * d), f16x2_of(v.z * d, v.w * d));
-        }
-        ok = meet<3, kMoeThreads>(A.ctl, round, &meet_ok) && ok;
-    }
 
     // ---- second product
-    c.a = c.stage = 0;
-    c.at(blockIdx.x, groups2, cum, n_active);
-    for (int it = 0; it < mine2; it++) {
-        const int e = act[c.a], first = off[e] + c.c * NT, n = min(NT, cnt[e] - first);
-        clear(acc);
-        for (c.stage = 0; c.stage < stages2; c.stage++) multiply(true, c, n);
+    for (begin(true, c); more(c); next(true, c)) {
+        const int e = act[c.a], first = off[e] + c.c * NT, n = c.tokens;
+        run_item(std::true_type(), c, n);
         constexpr int HR = 16 * S::TM;
         const bool mine = put_partials();
+        float g2 = 0.f, u2 = 0.f;
+        if (E4M3 && mine) {
+            g2 = __ldg(A.row_max + weights_of(e) * 2);
+            u2 = __ldg(A.row_max + weights_of(e) * 2 + 1);
+        }
         for (int i = htid; mine && i < HR * n; i += FINISH) {
-            const int col = i / HR, row = i - col * HR, hr = c.r * HR + row;
+            const int col = i / HR, row = i - col * HR, hr = c.tile * 16 + row;
             const int p = list[first + col];
-            if (hr < H) {
-                float v = total(row, col);
-                if (E4M3) v *= exp2i(fp16_exponent(__uint_as_float(A.h_max[p])));
+            if (row < c.n * 16) {
+                float v = total(c.lwk, row >> 4, row & 15, col);
+                if (E4M3) v *= exp2i(hidden_exponent(A.x_norm2[p / C], g2, u2));
                 A.y[(size_t)p * H + hr] = v;
             }
         }
-        c.at(c.item + grid, groups2, cum, n_active);
     }
     ok = meet<3, kMoeThreads>(A.ctl, round, &meet_ok) && ok;
     if (!ok) {
@@ -827,13 +962,9 @@ __global__ void __launch_bounds__(kMoeBlock, 1) moe_kernel(const __grid_constant
     for (int i = blockIdx.x * kMoeThreads + tid; i < T * quads; i += grid * kMoeThreads) {
         const int t = i / quads, h = (i - t * quads) * 4;
         float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
-        for (int j = 0; j < C; j++) {
-            float w = 1.f;
-            if (j < K) {
-                const int e = A.ids[t * K + j] - A.m.first;
-                if (e < 0 || e >= A.m.n_local) continue;
-                w = A.weights[t * K + j];
-            }
+        for (unsigned rest = local[t]; rest; rest &= rest - 1u) {
+            const int j = __ffs(rest) - 1;
+            const float w = j < K ? A.weights[t * K + j] : 1.f;
             const float4 v = *reinterpret_cast<const float4 *>(A.y + (size_t)(t * C + j) * H + h);
             s.x = fmaf(w, v.x, s.x);
             s.y = fmaf(w, v.y, s.y);
@@ -868,6 +999,18 @@ static void moe_layout(const pf_moe_t *m, MoeArgs &a)
     a.Fk = a.ks_down * kw;
     a.down_at = (size_t)a.f_tiles * a.ks_up * kSliceBytes;
     a.set_bytes = a.down_at + (size_t)a.h_tiles * a.ks_down * kSliceBytes;
+    const size_t fb = (m->F + 127) / 128, hb = (m->H + 127) / 128, n = a.n_sets;
+    a.n_up_scales = a.n_down_scales = fb * hb;
+    a.packed_bytes = a.set_bytes * n;
+    if (m->wtype == PF_DT_E4M3) a.packed_bytes += (n * (2 * a.n_up_scales + a.n_down_scales) + 2 * n) * sizeof(float);
+}
+static void moe_point(MoeArgs &a, const void *packed)
+{
+    a.packed = (const uint8_t *)packed;
+    a.gs = (const float *)(a.packed + a.set_bytes * (size_t)a.n_sets);
+    a.us = a.gs + a.n_up_scales * a.n_sets;
+    a.ds = a.us + a.n_up_scales * a.n_sets;
+    a.row_max = a.ds + a.n_down_scales * a.n_sets;
 }
 static size_t take(size_t &at, size_t bytes)
 {
@@ -875,6 +1018,8 @@ static size_t take(size_t &at, size_t bytes)
     at += (bytes + 255) & ~(size_t)255;
     return here;
 }
+// tokens of a block of the router: whole column blocks of the matrix instruction
+static int route_tokens(int T) { return T <= 8 ? 8 : T <= 16 ? 16 : 32; }
 // carves the workspace; sms: number of SMs (sizes the router's grid).  Returns its size; `base` may be NULL.
 static size_t moe_carve(MoeArgs &a, int T, int sms, uint8_t *base)
 {
@@ -882,7 +1027,8 @@ static size_t moe_carve(MoeArgs &a, int T, int sms, uint8_t *base)
     const bool e4m3 = m.wtype == PF_DT_E4M3;
     a.T = T;
     a.e_tiles = (m.n_experts + 15) / 16;
-    a.t_chunks = (T + kRouteTokens - 1) / kRouteTokens;
+    const int tokens = route_tokens(T);
+    a.t_chunks = (T + tokens - 1) / tokens;
     // router: about one block per SM, at least 256 columns (32 per warp) for each
     const int most = (m.H + 255) / 256, want = sms / (a.e_tiles * a.t_chunks);
     a.h_splits = want < 1 ? 1 : (want < most ? want : most);
@@ -890,24 +1036,27 @@ static size_t moe_carve(MoeArgs &a, int T, int sms, uint8_t *base)
     const size_t pairs = (size_t)T * a.choices;
     size_t at = 0;
     a.ctl = (unsigned *)(base + take(at, 256));
-    a.h_max = (unsigned *)(base + take(at, pairs * 4));
     a.logits = (float *)(base + take(at, (size_t)a.h_splits * T * m.n_experts * 4));
     a.xh = (uint16_t *)(base + take(at, (size_t)T * a.Hk * 2));
     a.xh_scale = (float *)(base + take(at, (size_t)T * 4));
-    a.h32 = (float *)(base + take(at, e4m3 ? pairs * a.Fp * 4 : 0));
+    a.x_norm2 = (float *)(base + take(at, (size_t)T * 4));
     a.hop = (uint16_t *)(base + take(at, pairs * a.Fk * 2 * (e4m3 ? 1 : 2)));
     a.y = (float *)(base + take(at, pairs * m.H * 4));
     return at;
 }
 
-template <bool E4M3, int WM, int WK, int MI, int NT>
+template <bool E4M3, int NT>
 static int moe_launch(const MoeArgs &a, int device, int sms, cudaStream_t st)
 {
-    using S = MoeShape<E4M3, WM, WK, MI, NT>;
-    const size_t smem = (size_t)S::FIXED + ((size_t)a.n_sets * 4 + 1) * 4 + (size_t)a.T * a.choices * 2;
-    PF_CUDA_TRY(ensure_dynamic_smem((const void *)moe_kernel<E4M3, WM, WK, MI, NT>, device, smem), "moe_kernel shared memory");
+    using S = MoeShape<E4M3, NT>;
+    const size_t smem = (size_t)S::FIXED + ((size_t)a.n_sets * 4 + 1) * 4 + ((size_t)a.T * a.choices + 1) / 2 * 4 + (size_t)a.T * 4;
+    PF_CUDA_TRY(ensure_dynamic_smem((const void *)moe_kernel<E4M3, NT>, device, smem), "moe_kernel shared memory");
     const int n_route = a.e_tiles * a.h_splits * a.t_chunks + a.T;
-    moe_route_kernel<E4M3><<<n_route, kMoeThreads, 0, st>>>(a);
+    switch (route_tokens(a.T)) {
+    case 8: moe_route_kernel<E4M3, 1><<<n_route, kRouteThreads, 0, st>>>(a); break;
+    case 16: moe_route_kernel<E4M3, 2><<<n_route, kRouteThreads, 0, st>>>(a); break;
+    default: moe_route_kernel<E4M3, 4><<<n_route, kRouteThreads, 0, st>>>(a); break;
+    }
     PF_CUDA_TRY(cudaGetLastError(), "moe_route_kernel launch");
     count_launch();
     cudaLaunchConfig_t cfg = {};
@@ -920,7 +1069,7 @@ static int moe_launch(const MoeArgs &a, int device, int sms, cudaStream_t st)
     at[0].val.cooperative = 1;
     cfg.attrs = at;
     cfg.numAttrs = 1;
-    PF_CUDA_TRY(cudaLaunchKernelEx(&cfg, moe_kernel<E4M3, WM, WK, MI, NT>, a), "moe_kernel launch");
+    PF_CUDA_TRY(cudaLaunchKernelEx(&cfg, moe_kernel<E4M3, NT>, a), "moe_kernel launch");
     count_launch();
     return PF_OK;
 }
@@ -934,25 +1083,43 @@ extern "C" size_t pf_moe_packed_bytes(const pf_moe_t *m)
     if (!moe_ok(m)) return 0;
     MoeArgs a;
     moe_layout(m, a);
-    return a.set_bytes * (size_t)a.n_sets;
+    return a.packed_bytes;
 }
 
-extern "C" int pf_moe_pack(const pf_moe_t *m, const void *d_gate, const void *d_up, const void *d_down, void *d_packed, void *stream)
+extern "C" int pf_moe_pack(const pf_moe_t *m, const void *d_gate, const void *d_up, const void *d_down, const float *d_gate_scale,
+                           const float *d_up_scale, const float *d_down_scale, void *d_packed, void *stream)
 {
     if (!moe_ok(m) || !d_gate || !d_up || !d_down || !d_packed) return PF_EINVAL;
     if (!aligned16(d_gate) || !aligned16(d_up) || !aligned16(d_down) || ((uintptr_t)d_packed & 255)) return PF_EINVAL;
+    const bool e4m3 = m->wtype == PF_DT_E4M3;
+    if (e4m3 ? (!d_gate_scale || !d_up_scale || !d_down_scale) : (d_gate_scale || d_up_scale || d_down_scale)) return PF_EINVAL;
+    if ((uintptr_t)d_gate_scale % 4 || (uintptr_t)d_up_scale % 4 || (uintptr_t)d_down_scale % 4) return PF_EINVAL;
     MoeArgs a;
     moe_layout(m, a);
-    const size_t units = a.set_bytes * (size_t)a.n_sets / 16;
+    moe_point(a, d_packed);
+    const size_t units = a.set_bytes * (size_t)a.n_sets / 16, n = a.n_sets;
     const unsigned grid = (unsigned)((units + 255) / 256 < 65536 ? (units + 255) / 256 : 65536);
     cudaStream_t st = (cudaStream_t)stream;
-    if (m->wtype == PF_DT_E4M3)
-        moe_pack_kernel<true><<<grid, 256, 0, st>>>(*m, a.n_sets, a.f_tiles, a.ks_up, a.ks_down, a.set_bytes, a.down_at, (const uint8_t *)d_gate,
-                                                    (const uint8_t *)d_up, (const uint8_t *)d_down, (uint8_t *)d_packed);
-    else
+    if (!e4m3) {
         moe_pack_kernel<false><<<grid, 256, 0, st>>>(*m, a.n_sets, a.f_tiles, a.ks_up, a.ks_down, a.set_bytes, a.down_at, (const uint8_t *)d_gate,
                                                      (const uint8_t *)d_up, (const uint8_t *)d_down, (uint8_t *)d_packed);
+        PF_CUDA_TRY(cudaGetLastError(), "moe_pack_kernel launch");
+        count_launch();
+        return PF_OK;
+    }
+    PF_CUDA_TRY(cudaMemcpyAsync((void *)a.gs, d_gate_scale, n * a.n_up_scales * 4, cudaMemcpyDeviceToDevice, st), "scale copy");
+    PF_CUDA_TRY(cudaMemcpyAsync((void *)a.us, d_up_scale, n * a.n_up_scales * 4, cudaMemcpyDeviceToDevice, st), "scale copy");
+    PF_CUDA_TRY(cudaMemcpyAsync((void *)a.ds, d_down_scale, n * a.n_down_scales * 4, cudaMemcpyDeviceToDevice, st), "scale copy");
+    PF_CUDA_TRY(cudaMemsetAsync((void *)a.row_max, 0, n * 2 * 4, st), "row norms");
+    moe_pack_kernel<true><<<grid, 256, 0, st>>>(*m, a.n_sets, a.f_tiles, a.ks_up, a.ks_down, a.set_bytes, a.down_at, (const uint8_t *)d_gate,
+                                                (const uint8_t *)d_up, (const uint8_t *)d_down, (uint8_t *)d_packed);
     PF_CUDA_TRY(cudaGetLastError(), "moe_pack_kernel launch");
+    const long long warps = (long long)n * m->F * 2;
+    if ((warps + 7) / 8 >= (1ll << 31)) return PF_ERANGE;
+    moe_row_norm_kernel<<<(unsigned)((warps + 7) / 8), 256, 0, st>>>(*m, a.n_sets, (const uint8_t *)d_gate, (const uint8_t *)d_up, d_gate_scale, d_up_scale,
+                                                                     (float *)a.row_max);
+    PF_CUDA_TRY(cudaGetLastError(), "moe_row_norm_kernel launch");
+    count_launch();
     count_launch();
     return PF_OK;
 }
@@ -967,8 +1134,7 @@ extern "C" size_t pf_moe_workspace(const pf_moe_t *m, int32_t T)
 }
 
 extern "C" int pf_moe_forward(const pf_moe_t *m, int32_t T, const void *d_x, int64_t x_stride, const uint8_t *d_xq, const float *d_xscale,
-                              const void *d_router, const void *d_packed, const float *d_gate_scale, const float *d_up_scale,
-                              const float *d_down_scale, void *d_out, int32_t *d_ids, float *d_weights, int32_t *d_status,
+                              const void *d_router, const void *d_packed, void *d_out, int32_t *d_ids, float *d_weights, int32_t *d_status,
                               void *d_workspace, size_t workspace_bytes, void *stream)
 {
     if (!moe_ok(m)) return PF_EINVAL;
@@ -979,22 +1145,19 @@ extern "C" int pf_moe_forward(const pf_moe_t *m, int32_t T, const void *d_x, int
     if (!aligned16(d_x) || x_stride < m->H || x_stride % 8 || !aligned16(d_router) || ((uintptr_t)d_packed & 255) || (uintptr_t)d_out % 8) return PF_EINVAL;
     if ((uintptr_t)d_ids % 4 || (uintptr_t)d_weights % 4 || (uintptr_t)d_status % 4) return PF_EINVAL;
     if ((d_xq != nullptr) != (d_xscale != nullptr) || (d_xq && (!e4m3 || (uintptr_t)d_xq % 8 || (uintptr_t)d_xscale % 4))) return PF_EINVAL;
-    if (e4m3 && (!d_gate_scale || !d_up_scale || !d_down_scale)) return PF_EINVAL;
     int device, sms;
     if (int rc = current_sm_count(&device, &sms)) return rc;
     MoeArgs a;
     moe_layout(m, a);
     if (!d_workspace || ((uintptr_t)d_workspace & 255) != 0 || workspace_bytes < moe_carve(a, T, sms, (uint8_t *)d_workspace)) return PF_EWORKSPACE;
     a.x = (const uint16_t *)d_x; a.xs = x_stride; a.xq = d_xq; a.xscale = d_xscale;
-    a.router = (const uint16_t *)d_router; a.packed = (const uint8_t *)d_packed;
-    a.gs = d_gate_scale; a.us = d_up_scale; a.ds = d_down_scale;
+    a.router = (const uint16_t *)d_router;
+    moe_point(a, d_packed);
     a.out = (uint16_t *)d_out; a.ids = d_ids; a.weights = d_weights; a.status = d_status;
     cudaStream_t st = (cudaStream_t)stream;
-    // Up to 8 tokens an expert never has more than one 8-token column block: tiles of 32 rows, the columns split over the
-    // warps, fill the GPU with the fewest experts.  Beyond, 64 rows share a stage's tokens, up to 16 of them, and with more than 8 tokens an
-    // expert on average 128 rows share up to 32.
-    if (T <= 8) return e4m3 ? moe_launch<true, 1, 8, 2, 8>(a, device, sms, st) : moe_launch<false, 1, 8, 2, 8>(a, device, sms, st);
-    if ((long long)T * m->top_k <= 8ll * m->n_experts)
-        return e4m3 ? moe_launch<true, 2, 4, 2, 16>(a, device, sms, st) : moe_launch<false, 2, 4, 2, 16>(a, device, sms, st);
-    return e4m3 ? moe_launch<true, 4, 2, 2, 32>(a, device, sms, st) : moe_launch<false, 4, 2, 2, 32>(a, device, sms, st);
+    // Tokens an item takes at most: 8 (a column block of the matrix instruction) where no expert can have more, then 16, and 32 with more
+    // than 8 an expert on average: a stage's token rows take room from the ring, and an expert with more tokens than that is read again.
+    if (T <= 8) return e4m3 ? moe_launch<true, 8>(a, device, sms, st) : moe_launch<false, 8>(a, device, sms, st);
+    if ((long long)T * m->top_k <= 8ll * m->n_experts) return e4m3 ? moe_launch<true, 16>(a, device, sms, st) : moe_launch<false, 16>(a, device, sms, st);
+    return e4m3 ? moe_launch<true, 32>(a, device, sms, st) : moe_launch<false, 32>(a, device, sms, st);
 }

@@ -54,8 +54,8 @@ def declare(L):
     for name, args in (("pf_add_rms_norm", [i32, i64, i32, _vp, i64, _vp, i64, _vp, f32, i32, _vp, i64, _vp, i64, _vp, _vp, _vp]),
                        ("pf_kv_append", [cache, i32, i32, i64, i32, _vp, i64, _vp, i64, _vp, _vp, _vp, i32, _vp]),
                        ("pf_decode_attention", [cache, i32, i32, i32, _vp, i64, _vp, _vp, i32, f32, _vp, i64, _vp, _vp, _sz, _vp]),
-                       ("pf_moe_pack", [moe, _vp, _vp, _vp, _vp, _vp]),
-                       ("pf_moe_forward", [moe, i32, _vp, i64] + [_vp] * 11 + [_vp, _sz, _vp])):
+                       ("pf_moe_pack", [moe] + [_vp] * 8),
+                       ("pf_moe_forward", [moe, i32, _vp, i64] + [_vp] * 8 + [_vp, _sz, _vp])):
         fn = getattr(L, name)
         fn.restype, fn.argtypes = C.c_int, args
     for name, args in (("pf_decode_attention_workspace", [cache, i32, i32]), ("pf_moe_packed_bytes", [moe]), ("pf_moe_workspace", [moe, i32])):
@@ -224,7 +224,7 @@ class MoeLayer:
     router: [experts, H] bf16.  gate, up: [local + shared, F, H], down: [local + shared, H, F], bf16, or float8_e4m3fn with
     fp32 scales per 128 x 128 block ([local + shared, ceil(rows / 128), ceil(columns / 128)]).  Experts
     first_expert .. first_expert + local - 1 live here; the last n_shared of the weight tensors are taken by every token.
-    The layer keeps a packed copy; gate, up and down may be dropped afterwards (the scales are kept)."""
+    The layer keeps a packed copy; gate, up, down and their scales may be dropped afterwards."""
 
     def __init__(self, router, gate, up, down, *, top_k: int, first_expert: int = 0, n_shared: int = 0, gate_scale=None, up_scale=None,
                  down_scale=None, stream=None):
@@ -254,10 +254,11 @@ class MoeLayer:
         if size == 0:
             _refuse(f"{what}: inconsistent sizes")
         self._L, self._torch, self._dev = L, torch, dev
-        self.router, self.scales = router, (gate_scale, up_scale, down_scale)
+        self.router = router
         with _On(torch, stream):
             self.packed = torch.empty(size, dtype=torch.uint8, device=router.device)
-        _check(L.pf_moe_pack(self.m, gate.data_ptr(), up.data_ptr(), down.data_ptr(), self.packed.data_ptr(), _stream(torch, dev, stream)), "pf_moe_pack")
+        _check(L.pf_moe_pack(self.m, gate.data_ptr(), up.data_ptr(), down.data_ptr(), _ptr(gate_scale), _ptr(up_scale), _ptr(down_scale),
+                             self.packed.data_ptr(), _stream(torch, dev, stream)), "pf_moe_pack")
 
     def forward(self, x, xq=None, xq_scale=None, *, out=None, status=None, workspace=None, stream=None) -> dict:
         """x: [tokens, H] bf16, 1 .. 512 tokens; xq, xq_scale: the same tokens in 8 bits from pf_add_rms_norm (group 128), which
@@ -284,9 +285,7 @@ class MoeLayer:
             weights = torch.empty((T, m.top_k), dtype=torch.float32, device=x.device)
             if workspace is None:
                 workspace = torch.empty(L.pf_moe_workspace(m, T), dtype=torch.uint8, device=x.device)
-        gs, us, ds = self.scales
-        status_of = L.pf_moe_forward(m, T, x.data_ptr(), xs, _ptr(xq), _ptr(xq_scale), self.router.data_ptr(), self.packed.data_ptr(), _ptr(gs), _ptr(us),
-                                     _ptr(ds), out.data_ptr(), ids.data_ptr(), weights.data_ptr(), _ptr(status), workspace.data_ptr(),
+        status_of = L.pf_moe_forward(m, T, x.data_ptr(), xs, _ptr(xq), _ptr(xq_scale), self.router.data_ptr(), self.packed.data_ptr(), out.data_ptr(), ids.data_ptr(), weights.data_ptr(), _ptr(status), workspace.data_ptr(),
                                      workspace.numel() * workspace.element_size(), _stream(torch, dev, stream))
         if status_of != PF_OK:
             _check(status_of, what)

@@ -220,3 +220,17 @@ def test_in_a_graph():
     torch.cuda.synchronize()
     want = layer.forward(x)
     assert all(torch.equal(got[n], want[n]) for n in want)
+
+
+@pytest.mark.parametrize("T,E,wtype", [(50, 64, "e4m3"), (50, 64, "bf16"), (7, 16, "bf16"), (7, 16, "e4m3"), (90, 20, "e4m3")])
+def test_short_items_give_the_same_bits_call_after_call(T, E, wtype):
+    """Experts of one or two stages: the blocks' warps hand their partial sums over as often as they can."""
+    import torch
+    from paper_2607_18631_b200 import ops
+    x, router, ws, sc = layer_inputs(T, 256, 72, E, E, 2, wtype, seed=E)
+    layer = ops.MoeLayer(router, *ws, top_k=6, n_shared=2, gate_scale=sc[0], up_scale=sc[1], down_scale=sc[2])
+    want = layer.forward(x)
+    out, tol, _ = reference(x, x.double(), router, ws, sc, want["ids"], 0, E, 2, wtype)
+    assert torch.all((want["out"].double() - out).abs() <= tol + 1e-30)
+    for _ in range(100):
+        assert torch.equal(layer.forward(x)["out"], want["out"])

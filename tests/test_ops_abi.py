@@ -95,25 +95,28 @@ BAD_MOES = [dict(H=0), dict(H=24), dict(F=0), dict(n_experts=0), dict(n_experts=
             dict(top_k=0), dict(top_k=9), dict(n_experts=64, top_k=16), dict(n_local=0, n_shared=0), dict(wtype=1), dict(wtype=2)]
 
 
-def forward(lib, m=None, T=3, x=PTR, xs=64, xq=None, xsc=None, router=PTR, packed=PTR, gs=None, us=None, ds=None, out=PTR, ids=PTR, w=PTR, st=None, ws=PTR, wb=1 << 40):
-    return lib.pf_moe_forward(m if m is not None else moe(), T, x, xs, xq, xsc, router, packed, gs, us, ds, out, ids, w, st, ws, wb, None)
+def forward(lib, m=None, T=3, x=PTR, xs=64, xq=None, xsc=None, router=PTR, packed=PTR, out=PTR, ids=PTR, w=PTR, st=None, ws=PTR, wb=1 << 40):
+    return lib.pf_moe_forward(m if m is not None else moe(), T, x, xs, xq, xsc, router, packed, out, ids, w, st, ws, wb, None)
 
 
 def test_moe_refusals(lib):
     assert forward(lib, T=0) == B.PF_OK
-    assert lib.pf_moe_forward(None, 1, *([PTR, 64] + [PTR] * 11 + [PTR, 1 << 40, None])) == B.PF_EINVAL
+    assert lib.pf_moe_forward(None, 1, *([PTR, 64] + [PTR] * 8 + [PTR, 1 << 40, None])) == B.PF_EINVAL
     for bad in BAD_MOES:
         assert forward(lib, moe(**bad)) == B.PF_EINVAL, bad
         assert lib.pf_moe_packed_bytes(moe(**bad)) == 0
-        assert lib.pf_moe_pack(moe(**bad), PTR, PTR, PTR, PTR, None) == B.PF_EINVAL
+        assert lib.pf_moe_pack(moe(**bad), PTR, PTR, PTR, None, None, None, PTR, None) == B.PF_EINVAL
     for bad in (dict(x=None), dict(router=None), dict(packed=None), dict(out=None), dict(ids=None), dict(w=None), dict(x=PTR + 2), dict(xs=63), dict(xs=68), dict(packed=PTR + 16),
                 dict(router=PTR + 2), dict(out=PTR + 2), dict(xq=PTR, xsc=PTR), dict(xq=PTR), dict(xsc=PTR), dict(st=PTR + 1)):
         assert forward(lib, **bad) == B.PF_EINVAL, bad
     m8 = moe(wtype=3)
-    assert forward(lib, m8, gs=PTR, us=PTR) == B.PF_EINVAL and forward(lib, m8, gs=PTR, us=PTR, ds=PTR, xq=PTR) == B.PF_EINVAL
+    assert forward(lib, m8, xq=PTR) == B.PF_EINVAL and forward(lib, m8, xsc=PTR) == B.PF_EINVAL
+    for scales in ((None, PTR, PTR), (PTR, None, PTR), (PTR, PTR, None), (PTR + 1, PTR, PTR)):
+        assert lib.pf_moe_pack(m8, PTR, PTR, PTR, *scales, PTR, None) == B.PF_EINVAL
     assert forward(lib, T=-1) == B.PF_ERANGE and forward(lib, T=513) == B.PF_ERANGE
     for args in ((None, PTR, PTR, PTR), (PTR, None, PTR, PTR), (PTR, PTR, None, PTR), (PTR, PTR, PTR, None), (PTR + 1, PTR, PTR, PTR), (PTR, PTR, PTR, PTR + 16)):
-        assert lib.pf_moe_pack(moe(), *args, None) == B.PF_EINVAL
+        assert lib.pf_moe_pack(moe(), *args[:3], None, None, None, args[3], None) == B.PF_EINVAL
+    assert lib.pf_moe_pack(moe(), PTR, PTR, PTR, PTR, PTR, PTR, PTR, None) == B.PF_EINVAL
 
 
 def test_packed_sizes(lib):
@@ -121,7 +124,7 @@ def test_packed_sizes(lib):
     m = moe(H=64, F=24, n_local=4, n_shared=1)
     assert lib.pf_moe_packed_bytes(m) == 5 * 2048 * (3 * 1 + 4 * 1)
     m = moe(H=7168, F=2048, n_experts=256, first=32, n_local=32, n_shared=1, top_k=8, wtype=3)
-    assert lib.pf_moe_packed_bytes(m) == 33 * 3 * 7168 * 2048
+    assert lib.pf_moe_packed_bytes(m) == 33 * (3 * 7168 * 2048 + 4 * (3 * 56 * 16 + 2))
     m = moe(H=4096, F=1408, n_experts=64, first=0, n_local=64, n_shared=2, top_k=6, wtype=0)
     assert lib.pf_moe_packed_bytes(m) == 66 * 3 * 4096 * 1408 * 2
 
