@@ -9,6 +9,7 @@ stream the call runs on (`stream`, or the current one).  There is no CPU path.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes as C
 import math
 
@@ -33,6 +34,7 @@ class PfMoe(C.Structure):
 
 _ready = None
 _dtypes = None
+_attention_workspace = {}
 
 
 def _lib():
@@ -70,9 +72,9 @@ def _refuse(what: str):
 
 def _on_device(torch, what, *tensors):
     """Every tensor on the current CUDA device; returns its index."""
-    dev = torch.cuda.current_device()
+    dev = torch._C._cuda_getDevice()
     for t in tensors:
-        if t is not None and (not t.is_cuda or t.device.index != dev):
+        if t is not None and t.get_device() != dev:
             _refuse(f"{what}: a tensor is not on the current CUDA device (cuda:{dev})")
     return dev
 
@@ -81,12 +83,15 @@ def _stream(torch, dev, stream):
     return stream.cuda_stream if stream is not None else torch._C._cuda_getCurrentRawStream(dev)
 
 
-class _On:
-    """Allocate on the given stream (the caching allocator hands memory out per stream); no-op for the current one."""
+def _like(torch, t, dtype=None):
+    """A new contiguous tensor of t's shape."""
+    if t.is_contiguous():
+        return torch.empty_like(t) if dtype is None else torch.empty_like(t, dtype=dtype)
+    return torch.empty_like(t, dtype=dtype, memory_format=torch.contiguous_format)
 
-    def __new__(cls, torch, stream):
-        import contextlib
-        return contextlib.nullcontext() if stream is None else torch.cuda.stream(stream)
+
+def _matrix(torch, rows, cols, dtype, device):
+    return torch.empty_strided((rows, cols), (cols, 1), dtype=dtype, device=device)      # the quickest way to a new tensor
 
 
 def _rows(t, what, width):
@@ -107,7 +112,10 @@ def pf_add_rms_norm(x, residual=None, weight=None, *, eps: float = 1e-6, group: 
     x, residual: [rows, H] bf16, fp16 or fp32, rows contiguous.  Returns a dict: "sum" (a rounded to x's type; where a
     residual is given; `sum_out` to write it in place, x and residual themselves allowed), "y" if asked for, and "q" (e4m3) with "scale" (fp32)
     unless q=False."""
-    L, torch = _lib()
+    L, torch = _ready or _lib()
+    if stream is not None:      # the caching allocator hands memory out per stream
+        with torch.cuda.stream(stream):
+            return pf_add_rms_norm(x, residual, weight, eps=eps, group=group, y=y, q=q, sum_out=sum_out)
     what = "pf_add_rms_norm"
     dev = _on_device(torch, what, x, residual, weight, sum_out)
     dt = _dtypes.get(x.dtype)
@@ -115,40 +123,48 @@ def pf_add_rms_norm(x, residual=None, weight=None, *, eps: float = 1e-6, group: 
         _refuse(f"{what}: {x.dtype} is not supported")
     if x.dim() != 2:
         _refuse(f"{what}: x has to be [rows, H]")
-    rows, H = x.shape
+    rows, H = shape = x.shape
     if H < 1:
         raise PlanfrontError(PF_ERANGE, f"{what}: rows without elements")
-    xs = _rows(x, what, H)
-    for t in (residual, sum_out):
-        if t is not None and (t.dtype != x.dtype or t.shape != x.shape):
-            _refuse(f"{what}: residual and sum_out have x's shape and type")
     if weight is not None and (weight.dtype != x.dtype or weight.shape != (H,) or not weight.is_contiguous()):
         _refuse(f"{what}: weight has to be a contiguous [{H}] of x's type")
     out = {}
-    with _On(torch, stream):
-        if residual is not None or sum_out is not None:
-            out["sum"] = torch.empty((rows, H), dtype=x.dtype, device=x.device) if sum_out is None else sum_out
-        if y:
-            out["y"] = torch.empty((rows, H), dtype=x.dtype, device=x.device)
-        if q:
-            out["q"] = torch.empty((rows, H), dtype=torch.float8_e4m3fn, device=x.device)
-            out["scale"] = torch.empty((rows, -(-H // group) if group else 1), dtype=torch.float32, device=x.device)
-    s = out.get("sum")
-    _check(L.pf_add_rms_norm(dt, rows, H, x.data_ptr(), xs, _ptr(residual), 0 if residual is None else _rows(residual, what, H), _ptr(weight),
-                             eps, group, _ptr(s), 0 if s is None else _rows(s, what, H), _ptr(out.get("y")), H, _ptr(out.get("q")),
-                             _ptr(out.get("scale")), _stream(torch, dev, stream)), what)
+    s_ptr = r_ptr = y_ptr = q_ptr = scale_ptr = None
+    s_stride = r_stride = 0
+    if residual is not None:
+        if residual.dtype != x.dtype or residual.shape != shape:
+            _refuse(f"{what}: residual has x's shape and type")
+        r_ptr, r_stride = residual.data_ptr(), _rows(residual, what, H)
+    if residual is not None or sum_out is not None:
+        if sum_out is not None and (sum_out.dtype != x.dtype or sum_out.shape != shape):
+            _refuse(f"{what}: sum_out has x's shape and type")
+        out["sum"] = s = _like(torch, x) if sum_out is None else sum_out
+        s_ptr, s_stride = s.data_ptr(), H if sum_out is None else _rows(s, what, H)
+    if y:
+        out["y"] = t = _like(torch, x)
+        y_ptr = t.data_ptr()
+    if q:
+        out["q"] = t = _like(torch, x, torch.float8_e4m3fn)
+        q_ptr = t.data_ptr()
+        out["scale"] = t = _matrix(torch, rows, -(-H // group) if group else 1, torch.float32, x.device)
+        scale_ptr = t.data_ptr()
+    status = L.pf_add_rms_norm(dt, rows, H, x.data_ptr(), _rows(x, what, H), r_ptr, r_stride, None if weight is None else weight.data_ptr(), eps, group,
+                               s_ptr, s_stride, y_ptr, H, q_ptr, scale_ptr, _stream(torch, dev, None))
+    if status != PF_OK:
+        _check(status, what)
     return out
 
 
 def _cache(torch, what, k_cache, v_cache, k_scale, v_scale):
-    if k_cache.dim() != 4 or k_cache.shape != v_cache.shape or k_scale.shape != k_cache.shape[:2] or v_scale.shape != k_cache.shape[:2]:
+    shape = k_cache.shape
+    if len(shape) != 4 or shape != v_cache.shape or k_scale.shape != shape[:2] or v_scale.shape != shape[:2]:
         _refuse(f"{what}: caches are [pages, kv heads, page, head_dim], scales [pages, kv heads]")
-    if k_cache.dtype != torch.float8_e4m3fn or v_cache.dtype != torch.float8_e4m3fn or k_scale.dtype != torch.float32 or v_scale.dtype != torch.float32:
+    f8, f32 = torch.float8_e4m3fn, torch.float32
+    if k_cache.dtype != f8 or v_cache.dtype != f8 or k_scale.dtype != f32 or v_scale.dtype != f32:
         _refuse(f"{what}: caches are float8_e4m3fn, scales float32")
     if not (k_cache.is_contiguous() and v_cache.is_contiguous() and k_scale.is_contiguous() and v_scale.is_contiguous()):
         _refuse(f"{what}: the cache has to be contiguous")
-    n_pages, n_kv, page, hd = k_cache.shape
-    return PfKvCache(n_pages, n_kv, page, hd, k_cache.data_ptr(), v_cache.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr())
+    return PfKvCache(*shape, k_cache.data_ptr(), v_cache.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr())
 
 
 def _heads(t, what, heads, hd):
@@ -170,7 +186,7 @@ def pf_kv_append(k_cache, v_cache, k_scale, v_scale, k, v, cu_new, lengths, tabl
     k_cache, v_cache: [pages, kv_heads, page, head_dim] float8_e4m3fn; k_scale, v_scale: [pages, kv_heads] fp32.
     k, v: [new tokens, kv_heads, head_dim] bf16 or fp16; tokens cu_new[b] .. cu_new[b + 1] - 1 go behind the lengths[b] cached
     ones of sequence b, whose pages are table[b].  max_new: the most tokens a sequence gets.  `lengths` is not advanced."""
-    L, torch = _lib()
+    L, torch = _ready or _lib()
     what = "pf_kv_append"
     dev = _on_device(torch, what, k_cache, v_cache, k_scale, v_scale, k, v, cu_new, lengths, table)
     c = _cache(torch, what, k_cache, v_cache, k_scale, v_scale)
@@ -180,9 +196,11 @@ def pf_kv_append(k_cache, v_cache, k_scale, v_scale, k, v, cu_new, lengths, tabl
     n_seq = lengths.shape[0]
     if cu_new.shape != (n_seq + 1,) or table.dim() != 2 or table.shape[0] != n_seq:
         _refuse(f"{what}: cu_new is [sequences + 1], table [sequences, columns]")
-    _check(L.pf_kv_append(c, dt, n_seq, k.shape[0], max_new, k.data_ptr(), _heads(k, what, c.n_kv, c.hd), v.data_ptr(), _heads(v, what, c.n_kv, c.hd),
-                          _int32(torch, what, cu_new, 1), _int32(torch, what, lengths, 1), _int32(torch, what, table, 2), table.shape[1],
-                          _stream(torch, dev, stream)), what)
+    status = L.pf_kv_append(c, dt, n_seq, k.shape[0], max_new, k.data_ptr(), _heads(k, what, c.n_kv, c.hd), v.data_ptr(), _heads(v, what, c.n_kv, c.hd),
+                            _int32(torch, what, cu_new, 1), _int32(torch, what, lengths, 1), _int32(torch, what, table, 2), table.shape[1],
+                            _stream(torch, dev, stream))
+    if status != PF_OK:
+        _check(status, what)
 
 
 def pf_decode_attention(q, k_cache, v_cache, k_scale, v_scale, lengths, table, *, sm_scale: float | None = None, lse: bool = False, out=None,
@@ -192,29 +210,44 @@ def pf_decode_attention(q, k_cache, v_cache, k_scale, v_scale, lengths, table, *
     q: [sequences, heads, head_dim] bf16 or fp16; head h reads key / value head h // (heads // kv_heads).  sm_scale: 1 / sqrt(head_dim)
     if None.  Returns {"out": like q} and, if asked for, {"lse": [sequences, heads] fp32}.  A sequence without tokens gives
     zeros and -inf."""
-    L, torch = _lib()
+    L, torch = _ready or _lib()
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return pf_decode_attention(q, k_cache, v_cache, k_scale, v_scale, lengths, table, sm_scale=sm_scale, lse=lse, out=out, workspace=workspace)
     what = "pf_decode_attention"
     dev = _on_device(torch, what, q, k_cache, v_cache, k_scale, v_scale, lengths, table, out, workspace)
     c = _cache(torch, what, k_cache, v_cache, k_scale, v_scale)
     dt = _dtypes.get(q.dtype)
-    if dt is None or q.dim() != 3:
+    shape = q.shape
+    if dt is None or len(shape) != 3:
         _refuse(f"{what}: q has to be [sequences, heads, head_dim] of bf16 or fp16")
-    n_seq, heads, hd = q.shape
+    n_seq, heads, _ = shape
+    hd = c.hd
     if lengths.shape != (n_seq,) or table.dim() != 2 or table.shape[0] != n_seq:
         _refuse(f"{what}: lengths is [sequences], table [sequences, columns]")
-    if out is not None and (out.dtype != q.dtype or out.shape != q.shape):
-        _refuse(f"{what}: out has q's shape and type")
     res = {}
-    with _On(torch, stream):
-        res["out"] = torch.empty((n_seq, heads, hd), dtype=q.dtype, device=q.device) if out is None else out
-        if lse:
-            res["lse"] = torch.empty((n_seq, heads), dtype=torch.float32, device=q.device)
-        if workspace is None:
-            workspace = torch.empty(L.pf_decode_attention_workspace(c, n_seq, heads), dtype=torch.uint8, device=q.device)
-    _check(L.pf_decode_attention(c, dt, n_seq, heads, q.data_ptr(), _heads(q, what, heads, c.hd), _int32(torch, what, lengths, 1),
-                                 _int32(torch, what, table, 2), table.shape[1], 1.0 / math.sqrt(c.hd) if sm_scale is None else sm_scale,
-                                 res["out"].data_ptr(), _heads(res["out"], what, heads, c.hd), _ptr(res.get("lse")), workspace.data_ptr(),
-                                 workspace.numel() * workspace.element_size(), _stream(torch, dev, stream)), what)
+    if out is None:
+        out = _like(torch, q)
+    elif out.dtype != q.dtype or out.shape != shape:
+        _refuse(f"{what}: out has q's shape and type")
+    res["out"] = out
+    lse_ptr = None
+    if lse:
+        res["lse"] = t = _matrix(torch, n_seq, heads, torch.float32, q.device)
+        lse_ptr = t.data_ptr()
+    if workspace is None:
+        size = _attention_workspace.get((dev, hd))
+        if size is None:        # depends on the device and the head size only
+            size = _attention_workspace[dev, hd] = L.pf_decode_attention_workspace(c, max(n_seq, 1), max(heads, 1))
+        workspace = torch.empty(size, dtype=torch.uint8, device=q.device)
+        size_ws = size
+    else:
+        size_ws = workspace.numel() * workspace.element_size()
+    status = L.pf_decode_attention(c, dt, n_seq, heads, q.data_ptr(), _heads(q, what, heads, hd), _int32(torch, what, lengths, 1),
+                                   _int32(torch, what, table, 2), table.shape[1], 1.0 / math.sqrt(hd) if sm_scale is None else sm_scale,
+                                   out.data_ptr(), _heads(out, what, heads, hd), lse_ptr, workspace.data_ptr(), size_ws, _stream(torch, dev, None))
+    if status != PF_OK:
+        _check(status, what)
     return res
 
 
@@ -255,8 +288,9 @@ class MoeLayer:
             _refuse(f"{what}: inconsistent sizes")
         self._L, self._torch, self._dev = L, torch, dev
         self.router = router
-        with _On(torch, stream):
+        with contextlib.nullcontext() if stream is None else torch.cuda.stream(stream):
             self.packed = torch.empty(size, dtype=torch.uint8, device=router.device)
+        self._router_ptr, self._packed_ptr, self._workspace = router.data_ptr(), self.packed.data_ptr(), {}
         _check(L.pf_moe_pack(self.m, gate.data_ptr(), up.data_ptr(), down.data_ptr(), _ptr(gate_scale), _ptr(up_scale), _ptr(down_scale),
                              self.packed.data_ptr(), _stream(torch, dev, stream)), "pf_moe_pack")
 
@@ -265,6 +299,9 @@ class MoeLayer:
         e4m3 weights then multiply (the router reads x).  Returns {"out": [tokens, H] bf16, "ids": [tokens, top_k] int32, "weights": [tokens, top_k]
         fp32}.  status: int32 tensor of one element, see pf_moe_forward."""
         L, torch, m = self._L, self._torch, self.m
+        if stream is not None:
+            with torch.cuda.stream(stream):
+                return self.forward(x, xq, xq_scale, out=out, status=status, workspace=workspace)
         what = "pf_moe_forward"
         dev = _on_device(torch, what, x, xq, xq_scale, out, status, workspace, self.packed)
         if x.dtype != torch.bfloat16:
@@ -278,15 +315,18 @@ class MoeLayer:
             _refuse(f"{what}: xq is a contiguous float8_e4m3fn of x's shape, xq_scale [tokens, ceil(H / 128)] fp32")
         if out is not None and (out.dtype != x.dtype or out.shape != x.shape or not out.is_contiguous()):
             _refuse(f"{what}: out is a contiguous bf16 of x's shape")
-        with _On(torch, stream):
-            if out is None:
-                out = torch.empty((T, m.H), dtype=x.dtype, device=x.device)
-            ids = torch.empty((T, m.top_k), dtype=torch.int32, device=x.device)
-            weights = torch.empty((T, m.top_k), dtype=torch.float32, device=x.device)
-            if workspace is None:
-                workspace = torch.empty(L.pf_moe_workspace(m, T), dtype=torch.uint8, device=x.device)
-        status_of = L.pf_moe_forward(m, T, x.data_ptr(), xs, _ptr(xq), _ptr(xq_scale), self.router.data_ptr(), self.packed.data_ptr(), out.data_ptr(), ids.data_ptr(), weights.data_ptr(), _ptr(status), workspace.data_ptr(),
-                                     workspace.numel() * workspace.element_size(), _stream(torch, dev, stream))
+        if out is None:
+            out = _like(torch, x)
+        ids, weights = (_matrix(torch, T, m.top_k, t, x.device) for t in (torch.int32, torch.float32))
+        if workspace is None:
+            size = self._workspace.get(T)
+            if size is None:
+                size = self._workspace[T] = L.pf_moe_workspace(m, T)
+            workspace = torch.empty(size, dtype=torch.uint8, device=x.device)
+        else:
+            size = workspace.numel() * workspace.element_size()
+        status_of = L.pf_moe_forward(m, T, x.data_ptr(), xs, _ptr(xq), _ptr(xq_scale), self._router_ptr, self._packed_ptr, out.data_ptr(), ids.data_ptr(),
+                                     weights.data_ptr(), _ptr(status), workspace.data_ptr(), size, _stream(torch, dev, None))
         if status_of != PF_OK:
             _check(status_of, what)
         return {"out": out, "ids": ids, "weights": weights}
