@@ -457,50 +457,74 @@ __global__ void __launch_bounds__(kMoeBlock, 1) moe_kernel(const __grid_constant
         const int e = (by_itself ? reinterpret_cast<const int *>(red)[t * K + j] : A.ids[t * K + j]) - A.m.first;
         return e >= 0 && e < A.m.n_local ? A.m.n_shared + e : A.n_sets;
     };
-    uint16_t *set_at = reinterpret_cast<uint16_t *>(ring_p), *dealt = set_at + (P + 7) / 8 * 8;      // the ring is not in use yet
+    // offsets, experts with pairs and chunks from the counts in cnt: a scan by warp 0; cnt becomes `begin` ? off : the pairs' end
+    auto scan = [&](bool begin) {
+        int o = 0, a = 0, c = 0;
+        for (int i0 = 0; i0 < A.n_sets; i0 += 32) {
+            const int i = i0 + lane, n = i < A.n_sets ? cnt[i] : 0, ch = (n + NT - 1) / NT;
+            int so = n, sc = ch;
+#pragma unroll
+            for (int d = 1; d < 32; d <<= 1) {
+                const int u = __shfl_up_sync(0xFFFFFFFFu, so, d), v = __shfl_up_sync(0xFFFFFFFFu, sc, d);
+                if (lane >= d) {
+                    so += u;
+                    sc += v;
+                }
+            }
+            const unsigned live = __ballot_sync(0xFFFFFFFFu, n > 0);
+            if (i < A.n_sets) {
+                off[i] = o + so - n;
+                cnt[i] = begin ? o + so - n : o + so;
+            }
+            if (n > 0) {
+                const int at = a + __popc(live & ((1u << lane) - 1u));
+                act[at] = i;
+                cum[at + 1] = c + sc;
+            }
+            o += __shfl_sync(0xFFFFFFFFu, so, 31);
+            c += __shfl_sync(0xFFFFFFFFu, sc, 31);
+            a += __popc(live);
+        }
+        if (lane == 0) {
+            cum[0] = 0;
+            n_active_s = a;
+        }
+    };
     if (P <= kMoeBlock) {
-        // few pairs: a thread each, which counts the pairs that come before its own
+        // a thread for each pair: its rank within its warp, and before it the pairs of the warps in front
+        uint16_t *before = reinterpret_cast<uint16_t *>(ring_p);      // [warps][n_sets]; the ring is not in use yet
+        const int used = (P + 31) / 32;
+        for (int i = tid; i < used * A.n_sets; i += kMoeBlock) before[i] = 0;
         if (tid < T) local[tid] = 0u;
-        if (tid < (P + 7) / 8 * 8) set_at[tid] = 0xFFFFu;
-        if (tid == 0) n_active_s = cum[0] = 0;
         __syncthreads();
-        int s = A.n_sets;
-        if (tid < P) {
-            const int t = tid / C, j = tid - t * C;
-            s = set_of(t, j);
-            set_at[tid] = (uint16_t)s;
-            if (s < A.n_sets) atomicOr(local + t, 1u << j);
-        }
-        __syncthreads();
-        int before = 0, same = 0, rank = 0;
-        const bool here = s < A.n_sets;
-        if (here) {
-            for (int k = 0; k < P; k++) {
-                const int o = set_at[k];
-                before += o < s;
-                same += o == s;
-                rank += o == s && k < tid;
+        int s = A.n_sets, rank = 0;
+        if (warp < used) {
+            if (tid < P) {
+                const int t = tid / C, j = tid - t * C;
+                s = set_of(t, j);
+                if (s < A.n_sets) atomicOr(local + t, 1u << j);
             }
-            list[before + rank] = (uint16_t)tid;
+            const unsigned same = __match_any_sync(0xFFFFFFFFu, s);
+            rank = __popc(same & ((1u << lane) - 1u));
+            if (s < A.n_sets && rank == 0) before[warp * A.n_sets + s] = (uint16_t)__popc(same);
         }
-        if (tid < P) dealt[tid] = here && rank == 0 ? (uint16_t)((same + NT - 1) / NT) : (uint16_t)0;      // an expert's first pair stands for it
         __syncthreads();
-        if (here && rank == 0) {
-            int at = 0, chunks = 0;
-            for (int k = 0; k < P; k++) {
-                const int d = dealt[k];
-                const bool less = d != 0 && set_at[k] < s;
-                at += less;
-                chunks += less ? d : 0;
+        for (int i = tid; i < A.n_sets; i += kMoeBlock) {
+            int c = 0;
+            for (int w = 0; w < used; w++) {
+                const int n = before[w * A.n_sets + i];
+                before[w * A.n_sets + i] = (uint16_t)c;
+                c += n;
             }
-            off[s] = before;
-            cnt[s] = before + same;
-            act[at] = s;
-            cum[at + 1] = chunks + dealt[tid];
-            atomicAdd(&n_active_s, 1);
+            cnt[i] = c;
         }
+        __syncthreads();
+        if (warp == 0) scan(false);
+        __syncthreads();
+        if (s < A.n_sets) list[off[s] + before[warp * A.n_sets + s] + rank] = (uint16_t)tid;
         __syncthreads();
     } else {
+        uint16_t *set_at = reinterpret_cast<uint16_t *>(ring_p), *dealt = set_at + P;
         for (int i = tid; i < A.n_sets; i += kMoeBlock) cnt[i] = 0;
         __syncthreads();
         for (int t = tid; t < T; t += kMoeBlock) {
@@ -514,35 +538,7 @@ __global__ void __launch_bounds__(kMoeBlock, 1) moe_kernel(const __grid_constant
             local[t] = mask;
         }
         __syncthreads();
-        if (warp == 0) {                     // offsets, experts with pairs, chunks: a scan by one warp
-            int o = 0, a = 0, c = 0;
-            for (int i0 = 0; i0 < A.n_sets; i0 += 32) {
-                const int i = i0 + lane, n = i < A.n_sets ? cnt[i] : 0, ch = (n + NT - 1) / NT;
-                int so = n, sc = ch;
-#pragma unroll
-                for (int d = 1; d < 32; d <<= 1) {
-                    const int u = __shfl_up_sync(0xFFFFFFFFu, so, d), v = __shfl_up_sync(0xFFFFFFFFu, sc, d);
-                    if (lane >= d) {
-                        so += u;
-                        sc += v;
-                    }
-                }
-                const unsigned live = __ballot_sync(0xFFFFFFFFu, n > 0);
-                if (i < A.n_sets) off[i] = cnt[i] = o + so - n;
-                if (n > 0) {
-                    const int at = a + __popc(live & ((1u << lane) - 1u));
-                    act[at] = i;
-                    cum[at + 1] = c + sc;
-                }
-                o += __shfl_sync(0xFFFFFFFFu, so, 31);
-                c += __shfl_sync(0xFFFFFFFFu, sc, 31);
-                a += __popc(live);
-            }
-            if (lane == 0) {
-                cum[0] = 0;
-                n_active_s = a;
-            }
-        }
+        if (warp == 0) scan(true);
         __syncthreads();
         // dealt out in any order, then ranked by pair number within each expert
         for (int t = tid; t < T; t += kMoeBlock)
