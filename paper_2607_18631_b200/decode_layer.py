@@ -1,0 +1,205 @@
+"""One decode layer of a ranked serving plan, run on this GPU: what the plan's per-layer step time is made of.
+
+The serving model prices a decode step per layer as the attention (projection weights and cached keys and values over
+HBM) plus the experts (the weights of those that a token chose).  `DecodeLayer` holds one layer as one GPU of a plan
+holds it -- attention heads over tp, experts over ep, expert width over what is left -- with random weights, and runs
+its step with the operators of `ops`; the projections are plain matrix products.  `measure` times the parts, and
+`with_measured_hbm` puts the rate they reached into a plan space's cluster, so that the space is ranked again with it.
+
+    python -m paper_2607_18631_b200.decode_layer [--batch N] [--context N]
+
+Plans with latent attention (attn_kind 1) are refused: the cache here holds keys and values per head.  Collectives
+between the GPUs of a plan are not run (a step's results are this GPU's parts).
+"""
+from __future__ import annotations
+
+import argparse
+import copy
+
+from .binding import PF_EINVAL, PlanfrontError
+
+CAP_SLACK = 64       # tokens a sequence may grow by after the context it starts with
+
+
+def layer_shape(cfg: dict, plan: dict) -> dict:
+    """What one GPU of a serving plan (a decoded tuple: kv, batch, dpa, ep, tp) holds of a layer."""
+    m, k = cfg["model"], cfg["kern"][plan["kv"]]
+    tp, ep, batch = plan["tp"], plan["ep"], plan["batch"]
+    if m["attn_kind"] != 0:
+        raise PlanfrontError(PF_EINVAL, "decode_layer: latent attention has no per-head cache")
+    if m["nh"] % tp or m["E"] % ep or m["nkv"] < 1:
+        raise PlanfrontError(PF_EINVAL, "decode_layer: heads do not divide by tp, or experts by ep")
+    engine = tp * ep if plan["dpa"] else tp          # GPUs of one engine, as the serving model counts them
+    moe_tp = max(1, engine // ep)
+    return dict(tokens=batch // ep if plan["dpa"] else batch, hidden=m["H"], heads=m["nh"] // tp, kv_heads=max(1, m["nkv"] // tp), head_dim=m["hd"],
+                experts=m["E"], local=m["E"] // ep, top_k=m["K"], ffn=-(-m["F"] // moe_tp), shared=m["S"] if m["Fs"] == m["F"] else 0,
+                weights="e4m3" if k["wbytes"] == 1 else "bf16")
+
+
+class DecodeLayer:
+    """A layer's weights and cache on the current device, and its decode step.  shape: see layer_shape; context: cached tokens
+    of every sequence at the start."""
+
+    def __init__(self, shape: dict, context: int, page: int = 64, seed: int = 0):
+        import torch
+
+        from . import ops
+        self.ops, self.torch, self.shape = ops, torch, dict(shape)
+        s, dev = self.shape, torch.device("cuda", torch.cuda.current_device())
+        g = torch.Generator(device=dev).manual_seed(seed)
+        H, d, nh, nkv, T = s["hidden"], s["head_dim"], s["heads"], s["kv_heads"], s["tokens"]
+
+        def weight(*dims):
+            return (torch.randn(*dims, generator=g, device=dev) * dims[-1] ** -0.5).to(torch.bfloat16)
+
+        self.norm1, self.norm2 = (torch.ones(H, dtype=torch.bfloat16, device=dev) for _ in range(2))
+        self.w_qkv, self.w_out = weight((nh + 2 * nkv) * d, H), weight(H, nh * d)
+        n = s["local"] + s["shared"]
+        mats, scales = [], [None] * 3
+        for i, dims in enumerate(((n, s["ffn"], H), (n, s["ffn"], H), (n, H, s["ffn"]))):
+            if s["weights"] == "bf16":
+                mats.append(torch.cat([weight(1, *dims[1:]) for _ in range(n)]))
+                continue
+            mats.append(torch.cat([(torch.randn(1, *dims[1:], generator=g, device=dev) * 112).clamp_(-448, 448).to(torch.float8_e4m3fn).view(torch.uint8)
+                                   for _ in range(n)]).view(torch.float8_e4m3fn))
+            scales[i] = torch.full((n, -(-dims[1] // 128), -(-dims[2] // 128)), dims[2] ** -0.5 / 112, device=dev)
+        self.moe = ops.MoeLayer(weight(s["experts"], H), *mats, top_k=s["top_k"], n_shared=s["shared"], gate_scale=scales[0], up_scale=scales[1],
+                                down_scale=scales[2])
+        cols = -(-(context + CAP_SLACK) // page)
+        self.table = torch.randperm(T * cols, generator=g, device=dev).to(torch.int32).reshape(T, cols)
+        self.cache = [torch.empty(T * cols, nkv, page, d, dtype=torch.float8_e4m3fn, device=dev) for _ in range(2)]
+        self.scales = [torch.empty(T * cols, nkv, device=dev) for _ in range(2)]
+        self.lengths = torch.zeros(T, dtype=torch.int32, device=dev)
+        self.one_each = torch.arange(T + 1, dtype=torch.int32, device=dev)
+        self.room = cols * page
+        at = 0
+        while at < context:         # the prompts, in chunks, as a prefill appends them
+            m = min(context - at, 1024)
+            k, v = (torch.randn(T * m, nkv, d, generator=g, device=dev).to(torch.bfloat16) for _ in range(2))
+            ops.pf_kv_append(*self.cache, *self.scales, k, v, self.one_each * m, self.lengths, self.table, max_new=m)
+            self.lengths += m
+            at += m
+        self.cached = context
+
+    def step(self, x, residual):
+        """One token of every sequence through the layer: x is what the layer before added, residual the stream it adds to (updated
+        in place).  Returns what this layer adds; the sequences are one token longer."""
+        ops, s = self.ops, self.shape
+        if self.cached >= self.room:
+            raise PlanfrontError(PF_EINVAL, "decode_layer: the cache is full")
+        y = ops.pf_add_rms_norm(x, residual, self.norm1, y=True, q=False, sum_out=residual)["y"]
+        q, k, v = self.project(y)
+        ops.pf_kv_append(*self.cache, *self.scales, k, v, self.one_each, self.lengths, self.table, max_new=1)
+        self.lengths += 1
+        self.cached += 1
+        a = self.attend(q)
+        n = ops.pf_add_rms_norm(a.flatten(1) @ self.w_out.t(), residual, self.norm2, y=True, sum_out=residual)
+        return self.experts(n)
+
+    def project(self, y):
+        s = self.shape
+        qkv = (y @ self.w_qkv.t()).unflatten(1, (s["heads"] + 2 * s["kv_heads"], s["head_dim"]))
+        return qkv.split((s["heads"], s["kv_heads"], s["kv_heads"]), 1)
+
+    def attend(self, q):
+        return self.ops.pf_decode_attention(q, *self.cache, *self.scales, self.lengths, self.table)["out"]
+
+    def experts(self, n):
+        eight = (n["q"], n["scale"]) if self.shape["weights"] == "e4m3" else ()
+        return self.moe.forward(n["y"], *eight)["out"]
+
+    def measure(self, repeats: int = 20) -> dict:
+        """{part: (microseconds, bytes it cannot do without)} of the attention and the experts, device time of a call."""
+        torch, s = self.torch, self.shape
+        x = torch.randn(s["tokens"], s["hidden"], device="cuda").to(torch.bfloat16)
+        n = self.ops.pf_add_rms_norm(x, None, self.norm2, y=True)
+        q = self.project(x)[0]
+        ids = self.moe.forward(n["y"])["ids"]
+        touched = int(torch.unique(ids[ids < s["local"]]).numel()) + s["shared"]
+        cache_bytes = int(self.lengths.sum()) * s["kv_heads"] * s["head_dim"] * 2
+        expert_bytes = touched * 3 * s["hidden"] * s["ffn"] * (1 if s["weights"] == "e4m3" else 2)
+        out = {}
+        for name, call, size in (("attention", lambda: self.attend(q), cache_bytes), ("experts", lambda: self.experts(n), expert_bytes)):
+            graph = torch.cuda.CUDAGraph()
+            call()
+            torch.cuda.synchronize()
+            with torch.cuda.graph(graph):
+                for _ in range(repeats):
+                    call()
+            graph.replay()
+            a, b = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+            a.record()
+            graph.replay()
+            b.record()
+            b.synchronize()
+            out[name] = (a.elapsed_time(b) * 1e3 / repeats, size)
+            del graph
+        return out
+
+
+def with_measured_hbm(cfg: dict, parts: dict) -> dict:
+    """The plan space with the HBM rate that the measured parts reached together."""
+    new = copy.deepcopy(cfg)
+    new["cluster"]["hbm_bw"] = sum(size for _, size in parts.values()) / (sum(us for us, _ in parts.values()) * 1e-6)
+    return new
+
+
+def example_space(batch: int, context: int) -> dict:
+    """A small serving space of a model with grouped key / value heads: 6 of 64 experts, bf16 and e4m3 kernels, up to 8 GPUs."""
+    kern = [dict(needs_caps=1 if fp8 else 0, avail_mask=0xFF, is_native=1, wbytes=1 if fp8 else 2, dtype_mult=2.0 if fp8 else 1.0, eff=[0.5] * 8, patch_ovh=0.0,
+                 dtype=int(fp8)) for fp8 in (False, True)]
+    return dict(
+        name="decode-layer example", phase=1,
+        model=dict(L=24, H=4096, nh=32, nkv=8, hd=128, attn_kind=0, E=64, K=6, F=1408, S=2, Fs=1408, seq=4096, vocab=102400, wb=2, gb=4, ob=12, ab=1, n_mats=3,
+                   count_embeddings=1),
+        cluster=dict(G=8, caps=1, budget_bytes=160_000_000_000, reserved_bytes=0, peak_flops=1.6e15, hbm_bw=7.7e12, bw_intra=770e9, bw_inter=50e9, alpha_intra=5e-6,
+                     alpha_inter=10e-6),
+        workload=dict(world=8, scen_P=[context], scen_O=[256]),
+        consts=dict(eff_dense=0.6, bwd_factor=2.0, dp_overlap_frac=0.5, dualpipe_startup_div=8.0, step_overhead=1e-5),
+        sched=[dict(kind=0, overlap=0, mapped=1, hide_frac=0.0, sched_ovh=0.0)], kern=kern,
+        rules=dict(ep_scope=0, layer_mode=0, tp_max=8, world_min=1, world_max=8, enforce_realizability=1),
+        axes=[("kv", [0, 1]), ("chunk", [1024, 4096]), ("batch", [batch]), ("dpa", [0]), ("ep", [1, 2, 4, 8]), ("tp", [1, 2, 4, 8]), ("scen", [0])])
+
+
+def best_plan(cfg: dict):
+    """(decoded tuple, predicted tokens/s/GPU) of the space's first plan."""
+    import torch
+
+    from .binding import Plan
+    plan = Plan(cfg)
+    out = plan.score(k=1)
+    torch.cuda.synchronize()
+    if int(out["topk_count"].item()) == 0:
+        raise PlanfrontError(PF_EINVAL, "decode_layer: no feasible plan")
+    best = plan.decode(int(out["topk_idx"][0].item())), float(out["topk_score"][0].item())
+    plan.close()
+    return best
+
+
+def main(argv=None) -> None:
+    import torch
+    ap = argparse.ArgumentParser(description=__doc__.splitlines()[0])
+    ap.add_argument("--batch", type=int, default=64)
+    ap.add_argument("--context", type=int, default=4096)
+    ap.add_argument("--steps", type=int, default=4)
+    a = ap.parse_args(argv)
+    cfg = example_space(a.batch, a.context)
+    plan, tput = best_plan(cfg)
+    shape = layer_shape(cfg, plan)
+    print(f"plan: tp {plan['tp']} ep {plan['ep']} kernel {shape['weights']} batch {plan['batch']}: predicted {tput:.1f} tokens/s/GPU")
+    layer = DecodeLayer(shape, a.context)
+    x = torch.randn(shape["tokens"], shape["hidden"], device="cuda").to(torch.bfloat16)
+    residual = torch.zeros_like(x)
+    for _ in range(a.steps):
+        x = layer.step(x, residual)
+    torch.cuda.synchronize()
+    parts = layer.measure()
+    for name, (us, size) in parts.items():
+        print(f"{name:10s} {us:9.1f} us  {size / 1e6:9.1f} MB  {size / us / 1e6:6.2f} TB/s")
+    again = with_measured_hbm(cfg, parts)
+    plan, tput = best_plan(again)
+    print(f"with {again['cluster']['hbm_bw'] / 1e12:.2f} TB/s: tp {plan['tp']} ep {plan['ep']}, predicted {tput:.1f} tokens/s/GPU")
+
+
+if __name__ == "__main__":
+    main()
