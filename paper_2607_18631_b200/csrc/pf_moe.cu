@@ -30,6 +30,7 @@ constexpr int kMoeWarps = 16, kMoeThreads = kMoeWarps * 32;   // that multiply
 constexpr int kCopyWarps = 4;                                // that copy
 constexpr int kMoeBlock = kMoeThreads + kCopyWarps * 32;
 constexpr int kSliceBytes = 2048;          // 16 rows x KW elements, KW = 64 (bf16) or 128 (e4m3)
+constexpr size_t kMoeSmem = 227 * 1024 - 1024;   // dynamic shared memory of a block, beside its static variables
 constexpr unsigned kMeetLimit = 1u << 21;  // polls of a meeting before it gives up (a poll takes about a microsecond)
 constexpr unsigned kRingLimit = 1u << 20;  // waits of up to a microsecond for a stage before they give up
 
@@ -378,7 +379,7 @@ __device__ __forceinline__ void choose(const MoeArgs &A, int t, int *keep, bool 
     }
 }
 
-template <bool E4M3, int NT>
+template <bool E4M3, int NT, int STAGES_>
 struct MoeShape {
     static constexpr int KW = E4M3 ? 128 : 64;
     static constexpr int PLANES = E4M3 ? 1 : 2;               // of the hidden activations
@@ -389,15 +390,16 @@ struct MoeShape {
     static constexpr __host__ __device__ int pitch(int lwk) { return (KW * 2 << lwk) + 64; }
     static constexpr int B_BYTES = NT * PLANES * ((KW * 2 << LWK) + 64);
     static constexpr int STAGE = A_BYTES + B_BYTES;
-    static constexpr int RED = kMoeWarps * 16 * NT * 4;       // one item's partial sums
-    static constexpr int STAGES = NT == 8 ? 5 : NT == 16 && E4M3 ? 4 : 3;      // what 227 KB hold beside the partial sums and the longest list of pairs
+    static constexpr int PASS = NT < 16 ? NT : 16;            // tokens whose partial sums meet at a time
+    static constexpr int RED = kMoeWarps * 16 * PASS * 4;
+    static constexpr int STAGES = STAGES_;
     static constexpr int FIXED = STAGES * STAGE + RED;
 };
 
-template <bool E4M3, int NT>
+template <bool E4M3, int NT, int STAGES_>
 __global__ void __launch_bounds__(kMoeBlock, 1) moe_kernel(const __grid_constant__ MoeArgs A)
 {
-    using S = MoeShape<E4M3, NT>;
+    using S = MoeShape<E4M3, NT, STAGES_>;
     using MT = typename std::conditional<E4M3, F16, Bf16>::type;
     constexpr int kStages = S::STAGES;
     extern __shared__ __align__(128) uint8_t smem[];
@@ -833,27 +835,35 @@ __global__ void __launch_bounds__(kMoeBlock, 1) moe_kernel(const __grid_constant
             for (; c.stage < c.stages; c.stage++) multiply(second_, std::integral_constant<int, 1>(), c);
         } else if (NT == 16 || n <= 16) {
             for (; c.stage < c.stages; c.stage++) multiply(second_, std::integral_constant<int, (NT < 16 ? 1 : 2)>(), c);
+        } else if (n <= 24) {
+            for (; c.stage < c.stages; c.stage++) multiply(second_, std::integral_constant<int, (NT < 32 ? 1 : 3)>(), c);
         } else {
             for (; c.stage < c.stages; c.stage++) multiply(second_, std::integral_constant<int, NT / 8>(), c);
         }
     };
-    // The warps' partial sums meet in `red` ([warp][row][token]), and all of them finish the item.  (Two buffers, two halves of the
-    // warps finishing items in turn: 349 us instead of 339 for 128 tokens, e4m3, 7168 x 2048.)
-    auto put_partials = [&]() {
-        bar<2, kMoeThreads>();                                  // everyone has finished the item before
+    // The warps' partial sums meet in `red` ([warp][row][token]), PASS tokens at a time, and all warps finish an item.  (Two buffers, two
+    // halves of the warps finishing items in turn: 349 us instead of 339 for 128 tokens, e4m3, 7168 x 2048.)
+    auto finish = [&](int n, auto &&each) {                     // each(first token, tokens) once their sums are in `red`
 #pragma unroll
-        for (int j = 0; j < NT / 8; j++) {
-            float *r = red + (warp * 16 + g) * NT + j * 8 + 2 * q;
-            r[0] = acc[j][0];
-            r[1] = acc[j][1];
-            r[8 * NT] = acc[j][2];
-            r[8 * NT + 1] = acc[j][3];
+        for (int ps = 0; ps < NT / S::PASS; ps++) {
+            if (ps * S::PASS >= n) break;
+            bar<2, kMoeThreads>();                              // everyone has read what was there before
+#pragma unroll
+            for (int j = 0; j < S::PASS / 8; j++) {
+                float *r = red + (warp * 16 + g) * S::PASS + j * 8 + 2 * q;
+                const float (&v)[4] = acc[ps * (S::PASS / 8) + j];
+                r[0] = v[0];
+                r[1] = v[1];
+                r[8 * S::PASS] = v[2];
+                r[8 * S::PASS + 1] = v[3];
+            }
+            bar<1, kMoeThreads>();
+            each(ps * S::PASS, min(S::PASS, n - ps * S::PASS));
         }
-        bar<1, kMoeThreads>();
     };
-    auto total = [&](int lwk, int tile, int row, int col) {     // row of the item's tile
+    auto total = [&](int lwk, int tile, int row, int col) {     // row of the item's tile, token of the pass
         float v = 0.f;
-        for (int i = 0; i < (1 << lwk); i++) v += red[(((tile << lwk) + i) * 16 + row) * NT + col];
+        for (int i = 0; i < (1 << lwk); i++) v += red[(((tile << lwk) + i) * 16 + row) * S::PASS + col];
         return v;
     };
 
@@ -861,33 +871,34 @@ __global__ void __launch_bounds__(kMoeBlock, 1) moe_kernel(const __grid_constant
     for (begin(false, c); more(c); next(false, c)) {
         const int e = act[c.a], first = off[e] + c.c * NT, n = c.tokens;
         run_item(std::false_type(), c, n);
-        constexpr int FR = 8 * S::TM;                              // hidden units of the item
-        put_partials();
+        constexpr int FR = 8 * S::TM;                           // hidden units of the item
         float g2 = 0.f, u2 = 0.f;
         if (E4M3) {
             g2 = __ldg(A.row_max + weights_of(e) * 2);
             u2 = __ldg(A.row_max + weights_of(e) * 2 + 1);
         }
-        for (int i = tid; i < FR * n; i += kMoeThreads) {
-            const int col = i / FR, fr = i - col * FR, f = c.tile * 8 + fr;
-            if (fr >= c.n * 8) continue;
-            const int p = list[first + col];
-            float gate = total(c.lwk, fr >> 3, fr & 7, col), up = total(c.lwk, fr >> 3, (fr & 7) + 8, col);
-            if (E4M3) {
-                const float xs = A.xh_scale[p / C];
-                gate *= xs;
-                up *= xs;
+        finish(n, [&](int t0, int nt) {
+            for (int i = tid; i < FR * nt; i += kMoeThreads) {
+                const int col = i / FR, fr = i - col * FR, f = c.tile * 8 + fr;
+                if (fr >= c.n * 8) continue;
+                const int p = list[first + t0 + col];
+                float gate = total(c.lwk, fr >> 3, fr & 7, col), up = total(c.lwk, fr >> 3, (fr & 7) + 8, col);
+                if (E4M3) {
+                    const float xs = A.xh_scale[p / C];
+                    gate *= xs;
+                    up *= xs;
+                }
+                const float h = gate / (1.f + expf(-gate)) * up;
+                if (E4M3) {
+                    A.hop[(size_t)p * A.Fk + f] = (uint16_t)f16x2_of(h * exp2i(-hidden_exponent(A.x_norm2[p / C], g2, u2)), 0.f);
+                } else {
+                    const uint32_t hi = bf16x2_of(h, 0.f) & 0xFFFFu;
+                    uint16_t *dst = A.hop + (size_t)p * 2 * A.Fk + f;
+                    dst[0] = (uint16_t)hi;
+                    dst[A.Fk] = (uint16_t)bf16x2_of(h - __uint_as_float(hi << 16), 0.f);
+                }
             }
-            const float h = gate / (1.f + expf(-gate)) * up;
-            if (E4M3) {
-                A.hop[(size_t)p * A.Fk + f] = (uint16_t)f16x2_of(h * exp2i(-hidden_exponent(A.x_norm2[p / C], g2, u2)), 0.f);
-            } else {
-                const uint32_t hi = bf16x2_of(h, 0.f) & 0xFFFFu;
-                uint16_t *dst = A.hop + (size_t)p * 2 * A.Fk + f;
-                dst[0] = (uint16_t)hi;
-                dst[A.Fk] = (uint16_t)bf16x2_of(h - __uint_as_float(hi << 16), 0.f);
-            }
-        }
+        });
         if (c.tile + c.n == A.f_tiles) {                // zeros behind F
             const int pad = A.Fk - A.Fp, rows = n * S::PLANES;
             for (int i = tid; i < pad * rows; i += kMoeThreads) {
@@ -905,21 +916,21 @@ __global__ void __launch_bounds__(kMoeBlock, 1) moe_kernel(const __grid_constant
         const int e = act[c.a], first = off[e] + c.c * NT, n = c.tokens;
         run_item(std::true_type(), c, n);
         constexpr int HR = 16 * S::TM;
-        put_partials();
         float g2 = 0.f, u2 = 0.f;
         if (E4M3) {
             g2 = __ldg(A.row_max + weights_of(e) * 2);
             u2 = __ldg(A.row_max + weights_of(e) * 2 + 1);
         }
-        for (int i = tid; i < HR * n; i += kMoeThreads) {
-            const int col = i / HR, row = i - col * HR, hr = c.tile * 16 + row;
-            const int p = list[first + col];
-            if (row < c.n * 16) {
+        finish(n, [&](int t0, int nt) {
+            for (int i = tid; i < HR * nt; i += kMoeThreads) {
+                const int col = i / HR, row = i - col * HR;
+                if (row >= c.n * 16) continue;
+                const int p = list[first + t0 + col];
                 float v = total(c.lwk, row >> 4, row & 15, col);
                 if (E4M3) v *= exp2i(hidden_exponent(A.x_norm2[p / C], g2, u2));
-                A.y[(size_t)p * H + hr] = v;
+                A.y[(size_t)p * H + c.tile * 16 + row] = v;
             }
-        }
+        });
     }
     ok = meet<3, kMoeThreads>(A.ctl, round, &meet_ok) && ok;
     if (!ok) {
@@ -1015,12 +1026,15 @@ static size_t moe_carve(MoeArgs &a, int T, int sms, uint8_t *base)
     return at;
 }
 
-template <bool E4M3, int NT>
+template <bool E4M3, int NT, int STAGES_>
 static int moe_launch(const MoeArgs &a, int device, int sms, cudaStream_t st)
 {
-    using S = MoeShape<E4M3, NT>;
-    const size_t smem = (size_t)S::FIXED + ((size_t)a.n_sets * 4 + 1) * 4 + ((size_t)a.T * a.choices + 1) / 2 * 4 + (size_t)a.T * 4;
-    PF_CUDA_TRY(ensure_dynamic_smem((const void *)moe_kernel<E4M3, NT>, device, smem), "moe_kernel shared memory");
+    using S = MoeShape<E4M3, NT, STAGES_>;
+    const size_t lists = ((size_t)a.n_sets * 4 + 1) * 4 + ((size_t)a.T * a.choices + 1) / 2 * 4 + (size_t)a.T * 4, smem = S::FIXED + lists;
+    // one stage less where the lists of pairs and experts do not leave room for it; the shortest ring fits with the longest lists
+    if constexpr (STAGES_ > 3)
+        if (smem > kMoeSmem) return moe_launch<E4M3, NT, STAGES_ - 1>(a, device, sms, st);
+    PF_CUDA_TRY(ensure_dynamic_smem((const void *)moe_kernel<E4M3, NT, STAGES_>, device, smem), "moe_kernel shared memory");
     const int n_route = a.e_tiles * a.h_splits * a.t_chunks + a.T;
     switch (route_tokens(a.T)) {
     case 8: moe_route_kernel<E4M3, 1><<<n_route, kRouteThreads, 0, st>>>(a); break;
@@ -1039,7 +1053,7 @@ static int moe_launch(const MoeArgs &a, int device, int sms, cudaStream_t st)
     at[0].val.cooperative = 1;
     cfg.attrs = at;
     cfg.numAttrs = 1;
-    PF_CUDA_TRY(cudaLaunchKernelEx(&cfg, moe_kernel<E4M3, NT>, a), "moe_kernel launch");
+    PF_CUDA_TRY(cudaLaunchKernelEx(&cfg, moe_kernel<E4M3, NT, STAGES_>, a), "moe_kernel launch");
     count_launch();
     return PF_OK;
 }
@@ -1126,8 +1140,11 @@ extern "C" int pf_moe_forward(const pf_moe_t *m, int32_t T, const void *d_x, int
     a.out = (uint16_t *)d_out; a.ids = d_ids; a.weights = d_weights; a.status = d_status;
     cudaStream_t st = (cudaStream_t)stream;
     // Tokens an item takes at most: 8 (a column block of the matrix instruction) where no expert can have more, then 16, and 32 with more
-    // than 8 an expert on average: a stage's token rows take room from the ring, and an expert with more tokens than that is read again.
-    if (T <= 8) return e4m3 ? moe_launch<true, 8>(a, device, sms, st) : moe_launch<false, 8>(a, device, sms, st);
-    if ((long long)T * m->top_k <= 8ll * m->n_experts) return e4m3 ? moe_launch<true, 16>(a, device, sms, st) : moe_launch<false, 16>(a, device, sms, st);
-    return e4m3 ? moe_launch<true, 32>(a, device, sms, st) : moe_launch<false, 32>(a, device, sms, st);
+    // than 8 an expert on average: a stage's token rows take room from the ring, and an expert with more tokens than an item is read again,
+    // mostly from the L2.  Measured with 16 and 32 (us): 24 tokens, 6 + 2 of 64 experts, e4m3, 4096 x 1408: 213, 238; 64 tokens: 262, 260; 128
+    // tokens, 8 of 256, 32 here: 335, 334.
+    if (T <= 8) return e4m3 ? moe_launch<true, 8, 5>(a, device, sms, st) : moe_launch<false, 8, 5>(a, device, sms, st);
+    if ((long long)T * m->top_k <= 8ll * m->n_experts)
+        return e4m3 ? moe_launch<true, 16, 5>(a, device, sms, st) : moe_launch<false, 16, 4>(a, device, sms, st);
+    return e4m3 ? moe_launch<true, 32, 4>(a, device, sms, st) : moe_launch<false, 32, 4>(a, device, sms, st);
 }
