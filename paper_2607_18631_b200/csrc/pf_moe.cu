@@ -10,16 +10,21 @@
 //  - moe_route_kernel: router logits (partial sums over slices of H), and the tokens as the second kernel's products take them.
 //  - moe_kernel: one block per SM, launched cooperatively, does everything else.  Its blocks choose the experts, then run
 //    through the row tiles of the chosen experts' gate and up matrices, meet, run through the tiles of the down matrices,
-//    meet, and add up each token's parts in a fixed order.  One warp of a block copies (bulk copies into a ring of a few
-//    stages, completion on an mbarrier), eight multiply; a multiplying warp waits for nothing but its stage.  While the blocks
-//    meet, the ring already fills with the down matrices' first stages, which do not depend on the meeting.
+//    meet, and add up each token's parts in a fixed order.  Four warps of a block copy (bulk copies into a ring of 3 to
+//    5 stages of 32 KB of weights, completion on an mbarrier), sixteen multiply; a multiplying warp waits for nothing but its stage.
+//    While the blocks meet, the ring already fills with the down matrices' first stages, which do not depend on the meeting.
 //  - 8 gate rows and the same 8 up rows form one 16-row tile: a lane's accumulators hold both factors of its products.
 // Sums are fp32.  bf16 weights multiply bf16 tokens; the hidden activations (fp32) enter the second product as the
 // sum of two bf16 numbers (16 bits of mantissa).  e4m3 weights are widened to fp16, which is exact; tokens and hidden activations
 // are scaled by a power of two per row and rounded to fp16 (11 bits); a weight block's scale is applied to the fp32 sum of
 // its 128 columns.  A hidden row's power of two has to be known before the row is: |h_f| <= |g_f . x| |u_f . x| <= |x|^2 max|g| max|u|
 // (Cauchy-Schwarz; |silu(a)| <= |a|), with the experts' largest row norms from pf_moe_pack.  The bound may lie 2^29 above the largest
-// |h| before fp16's least step costs more than its 11 bits (with random weights it lies a factor H above).  Two products in bf16 or fp16 cost less than half of the matrix rate at full HBM speed for 32 tokens a tile.
+// |h| before fp16's least step costs more than its 11 bits (with random weights it lies a factor H above).
+// The legacy matrix instruction is enough: at full HBM speed a scheduler gets a 2 KB slice every 333 cycles, and its products take 70 for up to
+// 8 tokens an expert.  Beyond 16 tokens an expert the reads of token rows from shared memory (4 per product) bound the kernel.
+// Measured (one B200, device time): 1 token, bf16, 6 + 2 of 64 experts of 4096 x 1408 (277 MB): 66 us; 16 tokens, e4m3, 8 of 128, 32 here, 5120 x
+// 1536 (511 MB): 121 us; 128 tokens, e4m3, 8 of 256, 32 here, 7168 x 2048 (1436 MB): 334 us.  Of the 66 us the streams of the two products take 44
+// (6.3 TB/s), the router's kernel 5, the choice and the sorting of pairs 5, the meetings 8.
 #include <type_traits>
 
 #include "pf_ops.cuh"
