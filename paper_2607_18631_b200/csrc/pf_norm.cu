@@ -7,8 +7,9 @@
 // chain load -> reduce -> store for few.  A thread owns runs of 8 neighbouring elements (16-byte loads of 16-bit types,
 // 8-byte stores of q); 16 lanes own one 128-element scale group, so its maximum takes four shuffles and no barrier.  With many
 // rows a block goes through several and has the next one's loads in flight while it reduces and stores.
-// 8192 rows of 7168, bf16, residual, all outputs (530 MB): 97 us, 0.84 of the copy rate, with one block of 1024 threads an SM and a run a thread;
-// 110 with two blocks of 512 and two runs, 119 with a row a block of 256: more rows under way at once mix reads and writes worse.
+// 8192 rows of 7168, bf16, residual, all outputs (530 MB): 92 us, 0.88 of the copy rate, with one block of 1024 threads an SM and a run a thread;
+// (before the divisions were replaced by products: 96; 110 with two blocks of 512 and two runs, 119 with a row a block of 256:
+// more rows under way at once mix reads and writes worse).  The schedulers issue in 70 % of the cycles.
 #include <math.h>
 
 #include "pf_ops.cuh"
@@ -23,7 +24,7 @@ struct NormArgs {
     int64_t xs, rs, ss, ys;   // row strides, elements
     int64_t rows;
     int H, groups;            // groups: scales per row
-    float eps;
+    float eps, inv_H;
 };
 
 // 8 elements as they lie in memory
@@ -157,7 +158,7 @@ __global__ void __launch_bounds__(THREADS, MIN_BLOCKS) norm_kernel(const NormArg
 #pragma unroll
             for (int j = 0; j < 8; j++) ss = fmaf(a[i][j], a[i][j], ss);
         }
-        const float rstd = rsqrtf(block_all<THREADS, false>(ss, part[0]) / (float)A.H + A.eps);
+        const float rstd = rsqrtf(block_all<THREADS, false>(ss, part[0]) * A.inv_H + A.eps);
         float row_max = 0.f;
 #pragma unroll
         for (int i = 0; i < NV; i++) {
@@ -182,9 +183,9 @@ __global__ void __launch_bounds__(THREADS, MIN_BLOCKS) norm_kernel(const NormArg
 #pragma unroll
             for (int o = 8; o; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, o));
             if (n <= 0) continue;
-            const float s = m > 0.f ? fmaxf(m / kE4m3Max, kMinScale) : 1.f;
+            const float s = m > 0.f ? fmaxf(m * (1.f / kE4m3Max), kMinScale) : 1.f;
             if ((threadIdx.x & 15) == 0) A.scale[row * A.groups + e / PF_SCALE_GROUP] = s;
-            const float inv = 1.f / s;
+            const float inv = __fdividef(1.f, s);      // within 2 units: far below e4m3's
             uint8_t *q = A.q + row * A.H + e;
             const uint32_t lo = e4m3x4(a[i][0] * inv, a[i][1] * inv, a[i][2] * inv, a[i][3] * inv);
             const uint32_t hi = e4m3x4(a[i][4] * inv, a[i][5] * inv, a[i][6] * inv, a[i][7] * inv);
@@ -198,7 +199,7 @@ __global__ void __launch_bounds__(THREADS, MIN_BLOCKS) norm_kernel(const NormArg
         }
         if (!A.q || A.groups != 1) continue;
         const float m = block_all<THREADS, true>(row_max, part[1]);
-        const float s = m > 0.f ? fmaxf(m / kE4m3Max, kMinScale) : 1.f, inv = 1.f / s;
+        const float s = m > 0.f ? fmaxf(m * (1.f / kE4m3Max), kMinScale) : 1.f, inv = __fdividef(1.f, s);
         if (threadIdx.x == 0) A.scale[row] = s;
 #pragma unroll
         for (int i = 0; i < NV; i++) {
@@ -274,7 +275,7 @@ extern "C" int pf_add_rms_norm(int32_t dtype, int64_t rows, int32_t H, const voi
     NormArgs a;
     a.x = d_x; a.res = d_residual; a.w = d_weight; a.sum = d_sum; a.y = d_y; a.q = d_q; a.scale = d_scale;
     a.xs = x_stride; a.rs = residual_stride; a.ss = sum_stride; a.ys = y_stride;
-    a.rows = rows; a.H = H; a.groups = group ? (H + group - 1) / group : 1; a.eps = eps;
+    a.rows = rows; a.H = H; a.groups = group ? (H + group - 1) / group : 1; a.eps = eps; a.inv_H = 1.f / (float)H;
     cudaStream_t st = (cudaStream_t)stream;
     // a row of at most one group takes the row path: one scale either way
     if (dtype == PF_DT_BF16) aligned ? norm_launch<Bf16, true>(a, sms, st) : norm_launch<Bf16, false>(a, sms, st);
