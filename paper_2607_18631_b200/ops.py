@@ -98,7 +98,7 @@ def _rows(t, what, width):
     """A 2-D tensor with contiguous rows of `width`; returns its row stride in elements."""
     if t.dim() != 2 or t.shape[1] != width or (t.stride(1) != 1 and width > 1):
         _refuse(f"{what}: expected rows of {width} contiguous elements, got shape {tuple(t.shape)}, strides {t.stride()}")
-    return max(t.stride(0), width) if t.shape[0] > 1 else width
+    return t.stride(0) if t.shape[0] > 1 else width      # below the width (an expanded row): the library refuses it
 
 
 def _ptr(t):

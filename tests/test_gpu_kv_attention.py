@@ -380,3 +380,16 @@ def test_attention_in_a_graph():
     graph.replay()
     torch.cuda.synchronize()
     assert torch.equal(out, ops.pf_decode_attention(q, *cache, ln, table)["out"])
+
+
+def test_overlapping_rows_are_refused():
+    import torch
+    from paper_2607_18631_b200 import PlanfrontError, ops
+    cache = make_cache(8, 2, 16, 64)
+    d = lambda *x: torch.tensor(x, dtype=torch.int32, device="cuda")  # noqa: E731
+    table = torch.arange(6, dtype=torch.int32, device="cuda").reshape(3, 2)
+    q, k = torch.randn(1, 4, 64, device="cuda").to(torch.bfloat16), torch.randn(1, 2, 64, device="cuda").to(torch.bfloat16)
+    with pytest.raises(PlanfrontError):
+        ops.pf_decode_attention(q.expand(3, 4, 64), *cache, d(3, 4, 5), table)
+    with pytest.raises(PlanfrontError):
+        ops.pf_kv_append(*cache, k.expand(3, 2, 64), k.expand(3, 2, 64), d(0, 1, 2, 3), d(3, 4, 5), table, max_new=1)

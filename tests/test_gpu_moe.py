@@ -234,3 +234,12 @@ def test_short_items_give_the_same_bits_call_after_call(T, E, wtype):
     assert torch.all((want["out"].double() - out).abs() <= tol + 1e-30)
     for _ in range(100):
         assert torch.equal(layer.forward(x)["out"], want["out"])
+
+
+def test_overlapping_token_rows_are_refused():
+    import torch
+    from paper_2607_18631_b200 import PlanfrontError, ops
+    x, router, ws, _ = layer_inputs(1, 128, 32, 4, 4, 0, "bf16")
+    layer = ops.MoeLayer(router, *ws, top_k=2)
+    with pytest.raises(PlanfrontError):
+        layer.forward(x.expand(5, 128))

@@ -129,3 +129,14 @@ def test_on_a_stream_of_its_own():
     got = ops.pf_add_rms_norm(x, y=True, stream=s)
     s.synchronize()
     assert torch.equal(got["y"], want["y"])
+
+
+def test_overlapping_rows_are_refused():
+    """An expanded row has stride 0: taking it for contiguous rows would read past its end."""
+    import torch
+    from paper_2607_18631_b200 import PlanfrontError, ops
+    row, x = torch.randn(1, 256, device="cuda"), torch.randn(6, 256, device="cuda")
+    for bad in (lambda: ops.pf_add_rms_norm(row.expand(6, 256)), lambda: ops.pf_add_rms_norm(x, row.expand(6, 256)),
+                lambda: ops.pf_add_rms_norm(x, x, sum_out=row.expand(6, 256)), lambda: ops.pf_add_rms_norm(row[0].unfold(0, 128, 16))):
+        with pytest.raises(PlanfrontError):
+            bad()
