@@ -816,9 +816,8 @@ struct ReduceArgs {
 
 // Pass 1, for a producers' list longer than kFastKeys keys: the list is cut into as many segments as the grid has
 // blocks -- few enough that what the blocks leave (at most k keys each) fits the final kernel's one-go sort -- and
-// block b walks its segment one tile at a time, admitting only keys above its running k-th best, and keeps the k
-// best.  A tile's admissions are counted before they are appended, so the buffer is pruned only when it would
-// really overflow.  A shorter list is left to the final kernel as it is.
+// block b walks its segment one tile at a time (tk_walk) and keeps the k best.  A shorter list is left to the final
+// kernel as it is.
 __global__ void __launch_bounds__(kReduceThreads) reduce_kernel(const ReduceArgs A)
 {
     chain_enter();
@@ -838,19 +837,7 @@ __global__ void __launch_bounds__(kReduceThreads) reduce_kernel(const ReduceArgs
         s_thr = 0ull;
     }
     __syncthreads();
-    for (unsigned int pos = lo; pos < hi; pos += kReduceThreads) {
-        const unsigned int i = pos + tid;
-        const unsigned long long key = i < hi ? A.in[i] : 0ull;
-        unsigned long long thr = s_thr;
-        const int takers = __syncthreads_count(key > thr);
-        if (s_count + takers > kTopkCap) {
-            tk_prune<kTopkCap / 2 / kReduceThreads>(s_buf, &s_count, &s_thr, k);
-            thr = s_thr;
-        }
-        tk_push(s_buf, &s_count, thr, key != 0ull, key);
-        __syncthreads();
-    }
-    tk_prune<kTopkCap / 2 / kReduceThreads>(s_buf, &s_count, &s_thr, k);
+    tk_walk<kTopkCap / 2 / kReduceThreads>(A.in, lo, hi, s_buf, &s_count, &s_thr, k);
     tk_flush(s_buf, s_count, 0ull, s_base, A.out, A.out_count);
 }
 
@@ -957,19 +944,7 @@ __global__ void __launch_bounds__(kReduceThreads) reduce_final_kernel(const Redu
             s_thr = 0ull;
         }
         __syncthreads();
-        for (unsigned int pos = 0; pos < n; pos += kReduceThreads) {
-            const unsigned int i = pos + tid;
-            const unsigned long long key = i < n ? A.in[i] : 0ull;
-            unsigned long long thr = s_thr;
-            const int takers = __syncthreads_count(key > thr);
-            if (s_count + takers > kTopkCap) {
-                tk_prune<kTopkCap / 2 / kReduceThreads>(s_big, &s_count, &s_thr, k);
-                thr = s_thr;
-            }
-            tk_push(s_big, &s_count, thr, key != 0ull, key);
-            __syncthreads();
-        }
-        tk_prune<kTopkCap / 2 / kReduceThreads>(s_big, &s_count, &s_thr, k);
+        tk_walk<kTopkCap / 2 / kReduceThreads>(A.in, 0u, n, s_big, &s_count, &s_thr, k);
         c = s_count;
     }
     for (int i = tid; i < k; i += kReduceThreads) {
