@@ -20,9 +20,11 @@
 // tokens, 32 / 8 heads (418 MB) 86 us, copies alone 68; 777 tokens, 16 heads of 64: 9.7 us.
 // Bytes are widened to fp16, which is exact; queries are scaled by a power of two into fp16's range.  Scores, maxima and
 // sums are fp32.
-// The value scale joins the exponent: with p_t = exp2(s_t + log2 vs - m) in [0, 1], the values' sum is plain and the
-// denominator is sum p_t / vs, one multiplication per page, so a page's scale costs nothing per element.  p is rounded to
-// fp16 (11 bits) for the second product.
+// The value scale joins the exponent: with p_t = exp2(s_t + log2 vs - z), the values' sum is plain and the denominator
+// is sum p_t / vs, one multiplication per page, so a page's scale costs nothing per element.  p is rounded to fp16 for the
+// second product, and z lies 15 below the maximum (rounded up, so that p <= 2^15 whatever the scores' size): weights keep
+// 11 bits down to 2^-29 of the largest and count down to 2^-40 of it.  (With p <= 1 it was 2^-14 and 2^-25: behind one
+// token of nearly all the weight, 100,000 others lost up to a sixth of theirs.)
 #include <math.h>
 
 #include "pf_ops.cuh"
@@ -32,6 +34,7 @@ namespace pf {
 constexpr int kTile = 32;                // tokens per tile
 constexpr int kBlockTiles = 8;           // a block takes no fewer tiles while others have none
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+constexpr float kLift = 15.f;            // log2 of the largest weight in the second product
 
 struct AttnArgs {
     pf_kv_cache_t c;
@@ -42,7 +45,7 @@ struct AttnArgs {
     int64_t qs, os;
     int n_seq, n_heads, group, cols, row_blocks, jobs_per_seq;   // jobs_per_seq = n_kv * row_blocks, row_blocks of 8 NB heads
     float scale_log2;                                            // sm_scale * log2(e)
-    float *part;                                                 // [warps] x (8 NB x HD values, 8 NB maxima, 8 NB sums), then [2 blocks] of the same
+    float *part;                                                 // [warps] x (8 NB x HD values, 8 NB references z, 8 NB sums), then [2 blocks] of the same
 };
 
 // length of sequence b as the kernel counts it: no negative, none past the table
@@ -165,8 +168,8 @@ __device__ __forceinline__ float ex2(float x)      // 2^x, results below the nor
     return r;
 }
 
-// A warp joins one row of up to 32 partial results at a time: lane k holds the pointer to part k (NULL: none, not for lane 0) of `count`.  Running
-// maximum, sum and values (V = HD / 32 neighbouring ones a lane) are carried from call to call.
+// A warp joins one row of up to 32 partial results at a time: lane k holds the pointer to part k (NULL: none, not for lane 0) of `count`.  Largest
+// reference, sum and values (V = HD / 32 neighbouring ones a lane) are carried from call to call.
 template <int HD, int NB>
 struct RowJoin {
     static constexpr int V = HD / 32;
@@ -373,11 +376,13 @@ __global__ void __launch_bounds__(AttnShape<HD, NB>::kWarps * 32, 1) attention_k
                         qb[nb][s][i] = f16x2_of(f.x * down, f.y * down);
                     }
         }
-        float o[NB][MT][4], m[NB][2], l[NB][2];
+        // m: the references z; l: the denominators, in two levels: 32 tiles are added up in l32 first, since the weights of a long
+        // sequence may each lie below the last bit of a sum that holds a large one
+        float o[NB][MT][4], m[NB][2], l[NB][2], l32[NB][2];
 #pragma unroll
         for (int nb = 0; nb < NB; nb++) {
             m[nb][0] = m[nb][1] = -INFINITY;
-            l[nb][0] = l[nb][1] = 0.f;
+            l[nb][0] = l[nb][1] = l32[nb][0] = l32[nb][1] = 0.f;
 #pragma unroll
             for (int j = 0; j < MT; j++) o[nb][j][0] = o[nb][j][1] = o[nb][j][2] = o[nb][j][3] = 0.f;
         }
@@ -421,7 +426,7 @@ __global__ void __launch_bounds__(AttnShape<HD, NB>::kWarps * 32, 1) attention_k
             uint32_t p[2][NB][2];
 #pragma unroll
             for (int nb = 0; nb < NB; nb++) {
-                float t0 = -INFINITY, t1 = -INFINITY;
+                float t0 = -INFINITY, t1 = -INFINITY;           // the tile's largest scores, then the references they ask for
 #pragma unroll
                 for (int mt = 0; mt < 2; mt++) {
                     const float f = score_scale * ks[mt], add = lv[mt];
@@ -440,6 +445,8 @@ __global__ void __launch_bounds__(AttnShape<HD, NB>::kWarps * 32, 1) attention_k
                     t0 = fmaxf(t0, fmaxf(s[mt][nb][0], s[mt][nb][2]));
                     t1 = fmaxf(t1, fmaxf(s[mt][nb][1], s[mt][nb][3]));
                 }
+                t0 = __fsub_ru(t0, kLift);
+                t1 = __fsub_ru(t1, kLift);
                 // a lane looks at its own tokens first: in most tiles no head has a new maximum
                 if (__any_sync(0xFFFFFFFFu, t0 > m[nb][0] || t1 > m[nb][1])) {
 #pragma unroll
@@ -453,6 +460,8 @@ __global__ void __launch_bounds__(AttnShape<HD, NB>::kWarps * 32, 1) attention_k
                     m[nb][1] = n1;
                     l[nb][0] *= a0;
                     l[nb][1] *= a1;
+                    l32[nb][0] *= a0;
+                    l32[nb][1] *= a1;
 #pragma unroll
                     for (int j = 0; j < MT; j++) {
                         o[nb][j][0] *= a0;
@@ -465,8 +474,8 @@ __global__ void __launch_bounds__(AttnShape<HD, NB>::kWarps * 32, 1) attention_k
 #pragma unroll
                 for (int mt = 0; mt < 2; mt++) {
                     const float e0 = ex2(s[mt][nb][0] - z0), e1 = ex2(s[mt][nb][1] - z1), e2 = ex2(s[mt][nb][2] - z0), e3 = ex2(s[mt][nb][3] - z1);
-                    l[nb][0] = fmaf(e0 + e2, ivs[mt], l[nb][0]);
-                    l[nb][1] = fmaf(e1 + e3, ivs[mt], l[nb][1]);
+                    l32[nb][0] = fmaf(e0 + e2, ivs[mt], l32[nb][0]);
+                    l32[nb][1] = fmaf(e1 + e3, ivs[mt], l32[nb][1]);
                     // heads as columns, tokens as rows -> the second product's other way round
                     p[mt][nb][0] = transpose8(f16x2_of(e0, e1));
                     p[mt][nb][1] = transpose8(f16x2_of(e2, e3));
@@ -505,6 +514,15 @@ __global__ void __launch_bounds__(AttnShape<HD, NB>::kWarps * 32, 1) attention_k
             slot = slot + 1 == S::kStages ? 0 : slot + 1;
             t++;
             cur.tile++;
+            if ((cur.tile & 31) == 0 || t == t_end || cur.tile == cur.n_tiles) {
+#pragma unroll
+                for (int nb = 0; nb < NB; nb++)
+#pragma unroll
+                    for (int c = 0; c < 2; c++) {
+                        l[nb][c] += l32[nb][c];
+                        l32[nb][c] = 0.f;
+                    }
+            }
         } while (t < t_end && cur.tile < cur.n_tiles);
 
         // a lane has heads 8 nb + 2q, + 1 and dims DG * g .. + DG - 1: row block j's rows are dims 2 j and 2 j + 1 of these
