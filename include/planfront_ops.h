@@ -76,6 +76,8 @@ int pf_kv_append(const pf_kv_cache_t *cache, int32_t dtype, int32_t n_seq, int64
  * strides in elements (multiples of 8, 16-byte aligned bases).  d_lse (may be NULL): [n_seq, n_heads] fp32,
  * log(sum_t exp(sm_scale * q . K[t])).  A sequence of length <= 0 gives zeros and -infinity.  Nothing beyond d_len[b] is
  * read, so what lies there may be NaN.  Tokens on a page outside the cache, or past the table's columns, are left out.
+ * A query element that is not finite makes its own head's out and lse NaN (0 and -infinity where all its scores are
+ * -infinity) and no other's.
  * Scales in the cache have to be positive and finite (below 2^-60 a value scale counts as 2^-60).
  * Several query tokens of one sequence are several rows with the same table row and their own lengths.
  * PF_EINVAL: NULL or misaligned pointers, another dtype, page or hd, n_heads not a multiple of n_kv, sm_scale not

@@ -18,7 +18,7 @@
 // the products, accumulators and exponentials, 62 us instead of 53 for one sequence of 131071 tokens, 8 key and 64 query heads of 128).
 // Measured (one B200, device time of both kernels): that sequence (269 MB) 57 us, of which the copies alone take 45; 48 ragged sequences up to 8192
 // tokens, 32 / 8 heads (418 MB) 86 us, copies alone 68; 777 tokens, 16 heads of 64: 9.7 us.
-// Bytes are widened to fp16, which is exact; queries are scaled by a power of two into fp16's range.  Scores, maxima and
+// Bytes are widened to fp16, which is exact; queries are scaled by a power of two a head into fp16's range.  Scores, maxima and
 // sums are fp32.
 // The value scale joins the exponent: with p_t = exp2(s_t + log2 vs - z), the values' sum is plain and the denominator
 // is sum p_t / vs, one multiplication per page, so a page's scale costs nothing per element.  p is rounded to fp16 for the
@@ -221,11 +221,11 @@ struct RowJoin {
     __device__ __forceinline__ void write(const AttnArgs &A, int b, int head)
     {
         const int lane = threadIdx.x & 31;
-        const float inv = sum > 0.f ? 1.f / sum : 0.f;
+        const float inv = sum == 0.f ? 0.f : 1.f / sum;      // (a sum that is not a number stays one)
         uint32_t *dst = reinterpret_cast<uint32_t *>(A.out + b * A.os + (int64_t)head * HD) + lane * V / 2;
 #pragma unroll
         for (int k = 0; k < V; k += 2) dst[k / 2] = pair_of_f32<T>(v[k] * inv, v[k + 1] * inv);
-        if (A.lse && lane == 0) A.lse[(int64_t)b * A.n_heads + head] = sum > 0.f ? (top + log2f(sum)) * kLn2 : -INFINITY;
+        if (A.lse && lane == 0) A.lse[(int64_t)b * A.n_heads + head] = sum == 0.f ? -INFINITY : (top + log2f(sum)) * kLn2;
     }
 };
 
@@ -338,43 +338,41 @@ __global__ void __launch_bounds__(AttnShape<HD, NB>::kWarps * 32, 1) attention_k
         const int heads = min(S::kHeads, A.group - rb * S::kHeads);
         const int head0 = h * A.group + rb * S::kHeads;
         uint32_t qb[NB][KS][2];
-        float score_scale;
-        {
-            // lane q of a head holds dims HD/4 * q + 4 s + {0, 1, 2, 3} at step s
-            float m = 0.f;
+        float score_scale[NB][2];
+        // lane q of a head holds dims HD/4 * q + 4 s + {0, 1, 2, 3} at step s
 #pragma unroll
-            for (int nb = 0; nb < NB; nb++) {
-                const uint16_t *src = A.q + b * A.qs + (int64_t)(head0 + nb * 8 + g) * HD + q * (HD / 4);
+        for (int nb = 0; nb < NB; nb++) {
+            const uint16_t *src = A.q + b * A.qs + (int64_t)(head0 + nb * 8 + g) * HD + q * (HD / 4);
 #pragma unroll
-                for (int i = 0; i < KS / 2; i++) {
-                    uint4 v = make_uint4(0, 0, 0, 0);
-                    if (nb * 8 + g < heads) v = *reinterpret_cast<const uint4 *>(src + 8 * i);
-                    qb[nb][2 * i][0] = v.x; qb[nb][2 * i][1] = v.y; qb[nb][2 * i + 1][0] = v.z; qb[nb][2 * i + 1][1] = v.w;
-                }
-#pragma unroll
-                for (int s = 0; s < KS; s++)
-#pragma unroll
-                    for (int i = 0; i < 2; i++) {
-                        const float2 f = pair_to_f32<T>(qb[nb][s][i]);
-                        m = fmaxf(m, fmaxf(fabsf(f.x), fabsf(f.y)));
-                    }
+            for (int i = 0; i < KS / 2; i++) {
+                uint4 v = make_uint4(0, 0, 0, 0);
+                if (nb * 8 + g < heads) v = *reinterpret_cast<const uint4 *>(src + 8 * i);
+                qb[nb][2 * i][0] = v.x; qb[nb][2 * i][1] = v.y; qb[nb][2 * i + 1][0] = v.z; qb[nb][2 * i + 1][1] = v.w;
             }
+            // A head's largest finite element goes to [2^13, 2^14): elements down to 2^-28 of it stay exact in fp16.  Each head has its own power
+            // of two: what one head's query holds, infinities included, is nothing to the others.
+            float top = 0.f;
 #pragma unroll
-            for (int o = 16; o; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, o));
-            // the largest query element goes to [2^13, 2^14): elements down to 2^-28 of it stay exact in fp16
-            int e = (m > 0.f && m < INFINITY) ? ((int)(__float_as_uint(m) >> 23) - 127) : 0;
+            for (int s = 0; s < KS; s++)
+#pragma unroll
+                for (int i = 0; i < 2; i++) {
+                    const float2 f = pair_to_f32<T>(qb[nb][s][i]);
+                    top = fmaxf(top, fmaxf(fabsf(f.x) < INFINITY ? fabsf(f.x) : 0.f, fabsf(f.y) < INFINITY ? fabsf(f.y) : 0.f));
+                }
+            top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 1));
+            top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 2));
+            int e = top > 0.f ? ((int)(__float_as_uint(top) >> 23) - 127) : 0;
             e = max(-100, e) - 13;
-            const float down = exp2f((float)-e);
-            score_scale = A.scale_log2 * exp2f((float)e);
+            const float down = exp2f((float)-e), up = A.scale_log2 * exp2f((float)e);
+            score_scale[nb][0] = __shfl_sync(0xFFFFFFFFu, up, 8 * q);        // of heads 2q and 2q + 1
+            score_scale[nb][1] = __shfl_sync(0xFFFFFFFFu, up, 8 * q + 4);
 #pragma unroll
-            for (int nb = 0; nb < NB; nb++)
+            for (int s = 0; s < KS; s++)
 #pragma unroll
-                for (int s = 0; s < KS; s++)
-#pragma unroll
-                    for (int i = 0; i < 2; i++) {
-                        const float2 f = pair_to_f32<T>(qb[nb][s][i]);
-                        qb[nb][s][i] = f16x2_of(f.x * down, f.y * down);
-                    }
+                for (int i = 0; i < 2; i++) {
+                    const float2 f = pair_to_f32<T>(qb[nb][s][i]);
+                    qb[nb][s][i] = f16x2_of(f.x * down, f.y * down);
+                }
         }
         // m: the references z; l: the denominators, in two levels: 32 tiles are added up in l32 first, since the weights of a long
         // sequence may each lie below the last bit of a sum that holds a large one
@@ -429,9 +427,9 @@ __global__ void __launch_bounds__(AttnShape<HD, NB>::kWarps * 32, 1) attention_k
                 float t0 = -INFINITY, t1 = -INFINITY;           // the tile's largest scores, then the references they ask for
 #pragma unroll
                 for (int mt = 0; mt < 2; mt++) {
-                    const float f = score_scale * ks[mt], add = lv[mt];
+                    const float f[2] = {score_scale[nb][0] * ks[mt], score_scale[nb][1] * ks[mt]};
 #pragma unroll
-                    for (int i = 0; i < 4; i++) s[mt][nb][i] = fmaf(s[mt][nb][i], f, add);
+                    for (int i = 0; i < 4; i++) s[mt][nb][i] = fmaf(s[mt][nb][i], f[i & 1], lv[mt]);
                 }
                 if (left < kTile) {
 #pragma unroll
@@ -549,7 +547,7 @@ __global__ void __launch_bounds__(AttnShape<HD, NB>::kWarps * 32, 1) attention_k
                 const int row = nb * 8 + 2 * q + c;
                 if (row >= heads) continue;
                 if (whole) {
-                    const float inv = sum > 0.f ? 1.f / sum : 0.f;
+                    const float inv = sum == 0.f ? 0.f : 1.f / sum;      // (a sum that is not a number stays one)
                     uint4 *dst = reinterpret_cast<uint4 *>(A.out + b * A.os + (int64_t)(head0 + row) * HD + g * DG);
 #pragma unroll
                     for (int j = 0; j < MT; j += 4)
@@ -557,7 +555,7 @@ __global__ void __launch_bounds__(AttnShape<HD, NB>::kWarps * 32, 1) attention_k
                                                 pair_of_f32<T>(o[nb][j + 1][c] * inv, o[nb][j + 1][c + 2] * inv),
                                                 pair_of_f32<T>(o[nb][j + 2][c] * inv, o[nb][j + 2][c + 2] * inv),
                                                 pair_of_f32<T>(o[nb][j + 3][c] * inv, o[nb][j + 3][c + 2] * inv));
-                    if (A.lse && g == 0) A.lse[(int64_t)b * A.n_heads + head0 + row] = sum > 0.f ? (m[nb][c] + log2f(sum)) * kLn2 : -INFINITY;
+                    if (A.lse && g == 0) A.lse[(int64_t)b * A.n_heads + head0 + row] = sum == 0.f ? -INFINITY : (m[nb][c] + log2f(sum)) * kLn2;
                 } else {
                     float4 *dst = reinterpret_cast<float4 *>(part + row * HD + g * DG);
 #pragma unroll

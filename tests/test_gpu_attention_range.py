@@ -81,3 +81,38 @@ def test_large_scores_stay_finite(score):
     got = ops.pf_decode_attention(q, kc, vc, ks, vs, torch.tensor([n], dtype=torch.int32, device="cuda"), table, sm_scale=float(score / top), lse=True)
     assert torch.isfinite(got["out"].float()).all() and torch.isfinite(got["lse"]).all()
     assert torch.all(got["out"].float().abs() <= 448 * vs.max() * 1.01)
+
+
+@pytest.mark.parametrize("nh,nkv,hd", [(8, 1, 128), (16, 1, 64), (12, 3, 128), (40, 2, 64)])
+@pytest.mark.parametrize("lens", [[300, 40, 1], [20_000]])
+@pytest.mark.parametrize("bad", [float("inf"), -float("inf"), float("nan")])
+def test_a_query_that_is_not_finite_spoils_its_own_head_only(nh, nkv, hd, lens, bad):
+    import torch
+    from paper_2607_18631_b200 import ops
+    B, page = len(lens), 32
+    cols = -(-max(lens) // page)
+    cache = make_cache(B * cols, nkv, page, hd, nh)
+    table = torch.arange(B * cols, dtype=torch.int32, device="cuda").reshape(B, cols)
+    ln = torch.tensor(lens, dtype=torch.int32, device="cuda")
+    q = (torch.randn(B, nh, hd, device="cuda") * 20).to(torch.bfloat16)
+    want = ops.pf_decode_attention(q, *cache, ln, table, sm_scale=0.01, lse=True)
+    heads = [1, nh - 1]
+    q[:, heads[0], 5] = bad
+    q[:, heads[1], hd - 1] = bad
+    got = ops.pf_decode_attention(q, *cache, ln, table, sm_scale=0.01, lse=True)
+    ok = [h for h in range(nh) if h not in heads]
+    assert torch.equal(got["out"][:, ok], want["out"][:, ok]) and torch.equal(got["lse"][:, ok], want["lse"][:, ok])
+    many = ln > 30                                          # enough tokens for scores of either sign
+    assert torch.isnan(got["out"][many][:, heads].float()).all() and torch.isnan(got["lse"][many][:, heads]).all()
+
+
+def test_heads_of_very_different_size_share_a_key_head():
+    import torch
+    from test_gpu_kv_attention import attend
+
+    def edit(q, cache, table):
+        q[:, 0] *= 2.0 ** 40
+        q[:, 3] *= 2.0 ** 20
+        q[:, 6] *= 2.0 ** -20
+    attend(3, 8, 1, 128, 64, [200, 33, 900], edit=edit)
+    attend(3, 16, 1, 64, 16, [200, 33, 900], edit=edit)
