@@ -101,6 +101,13 @@ def _rows(t, what, width):
     return t.stride(0) if t.shape[0] > 1 else width      # below the width (an expanded row): the library refuses it
 
 
+def _work_bytes(t, what):
+    """Size of a caller's workspace: what lies behind data_ptr() (an expanded tensor has fewer bytes than elements)."""
+    if not t.is_contiguous():
+        _refuse(f"{what}: the workspace has to be contiguous")
+    return t.numel() * t.element_size()
+
+
 def _ptr(t):
     return None if t is None else t.data_ptr()
 
@@ -242,7 +249,7 @@ def pf_decode_attention(q, k_cache, v_cache, k_scale, v_scale, lengths, table, *
         workspace = torch.empty(size, dtype=torch.uint8, device=q.device)
         size_ws = size
     else:
-        size_ws = workspace.numel() * workspace.element_size()
+        size_ws = _work_bytes(workspace, what)
     status = L.pf_decode_attention(c, dt, n_seq, heads, q.data_ptr(), _heads(q, what, heads, hd), _int32(torch, what, lengths, 1),
                                    _int32(torch, what, table, 2), table.shape[1], 1.0 / math.sqrt(hd) if sm_scale is None else sm_scale,
                                    out.data_ptr(), _heads(out, what, heads, hd), lse_ptr, workspace.data_ptr(), size_ws, _stream(torch, dev, None))
@@ -315,6 +322,8 @@ class MoeLayer:
             _refuse(f"{what}: xq is a contiguous float8_e4m3fn of x's shape, xq_scale [tokens, ceil(H / 128)] fp32")
         if out is not None and (out.dtype != x.dtype or out.shape != x.shape or not out.is_contiguous()):
             _refuse(f"{what}: out is a contiguous bf16 of x's shape")
+        if status is not None and (status.dtype != torch.int32 or status.numel() != 1):
+            _refuse(f"{what}: status is one int32")
         if out is None:
             out = _like(torch, x)
         ids, weights = (_matrix(torch, T, m.top_k, t, x.device) for t in (torch.int32, torch.float32))
@@ -324,7 +333,7 @@ class MoeLayer:
                 size = self._workspace[T] = L.pf_moe_workspace(m, T)
             workspace = torch.empty(size, dtype=torch.uint8, device=x.device)
         else:
-            size = workspace.numel() * workspace.element_size()
+            size = _work_bytes(workspace, what)
         status_of = L.pf_moe_forward(m, T, x.data_ptr(), xs, _ptr(xq), _ptr(xq_scale), self._router_ptr, self._packed_ptr, out.data_ptr(), ids.data_ptr(),
                                      weights.data_ptr(), _ptr(status), workspace.data_ptr(), size, _stream(torch, dev, None))
         if status_of != PF_OK:
