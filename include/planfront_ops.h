@@ -81,7 +81,8 @@ int pf_kv_append(const pf_kv_cache_t *cache, int32_t dtype, int32_t n_seq, int64
  * Scales in the cache have to be positive and finite (below 2^-60 a value scale counts as 2^-60).
  * Several query tokens of one sequence are several rows with the same table row and their own lengths.
  * PF_EINVAL: NULL or misaligned pointers, another dtype, page or hd, n_heads not a multiple of n_kv, sm_scale not
- * finite; PF_ERANGE: counts out of range (n_seq <= PF_ATTN_MAX_SEQ); PF_EWORKSPACE. */
+ * finite; PF_ERANGE: counts out of range (n_seq <= PF_ATTN_MAX_SEQ; the table's room, n_seq * table_cols * page, below
+ * 2^36 tokens and below 2^31 for one sequence); PF_EWORKSPACE. */
 #define PF_ATTN_MAX_SEQ 8192
 size_t pf_decode_attention_workspace(const pf_kv_cache_t *cache, int32_t n_seq, int32_t n_heads);
 int pf_decode_attention(const pf_kv_cache_t *cache, int32_t dtype, int32_t n_seq, int32_t n_heads, const void *d_q,

@@ -711,6 +711,9 @@ extern "C" int pf_decode_attention(const pf_kv_cache_t *cache, int32_t dtype, in
 {
     if (!kv_cache_ok(cache) || (dtype != PF_DT_BF16 && dtype != PF_DT_F16)) return PF_EINVAL;
     if (n_seq < 0 || n_seq > PF_ATTN_MAX_SEQ || n_heads < 0 || table_cols < 0 || (int64_t)table_cols * cache->page >= (1ll << 31)) return PF_ERANGE;
+    // the kernels count a job's tiles of all sequences in 32 bits, and the lengths, which the host does not see, are bounded by the table only
+    const int64_t tiles = ((int64_t)table_cols * cache->page + kTile - 1) / kTile;
+    if ((int64_t)n_seq * tiles >= (1ll << 31)) return PF_ERANGE;
     if (n_heads % cache->n_kv != 0 || !isfinite(sm_scale)) return PF_EINVAL;
     if (n_seq == 0 || n_heads == 0) return PF_OK;
     if (!d_q || !d_out || !d_len || !d_table || !aligned16(d_q) || !aligned16(d_out)) return PF_EINVAL;

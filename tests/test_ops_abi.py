@@ -85,6 +85,12 @@ def test_attention_refusals(lib):
         assert attention(lib, **bad) == B.PF_ERANGE, bad
 
 
+def test_attention_refuses_tables_whose_tiles_pass_32_bits(lib):
+    """The kernels add up tiles of 32 tokens over all sequences as 32-bit numbers: 2^31 of them and more are refused."""
+    for n_seq, page, cols in ((8192, 64, 1 << 17), (8192, 16, 1 << 19), (4096, 128, 1 << 17), (33, 64, (1 << 25) - 1), (64, 16, 1 << 26), (64, 128, (1 << 24) - 1)):
+        assert attention(lib, cache(page=page), n_seq=n_seq, cols=cols) == B.PF_ERANGE, (n_seq, page, cols)
+
+
 def moe(**kw):
     f = dict(H=64, F=24, n_experts=8, first=2, n_local=4, n_shared=1, top_k=2, wtype=0)
     f.update(kw)
