@@ -74,7 +74,8 @@ int pf_kv_append(const pf_kv_cache_t *cache, int32_t dtype, int32_t n_seq, int64
 /* out[b, h] = sum_t softmax_t(sm_scale * q[b, h] . K[t]) V[t] over the d_len[b] cached tokens of sequence b, query head h
  * reading key / value head h / (n_heads / n_kv).  q, out: n_seq rows of [n_heads, hd], `dtype` bf16 or f16, row
  * strides in elements (multiples of 8, 16-byte aligned bases).  d_lse (may be NULL): [n_seq, n_heads] fp32,
- * log(sum_t exp(sm_scale * q . K[t])).  A sequence of length <= 0 gives zeros and -infinity.  Nothing beyond d_len[b] is
+ * log(sum_t exp(sm_scale * q . K[t])).  A sequence of length <= 0 gives zeros and -infinity, and so
+ * does every one with a table of no columns (d_table may then be NULL).  Nothing beyond d_len[b] is
  * read, so what lies there may be NaN.  Tokens on a page outside the cache, or past the table's columns, are left out.
  * A query element that is not finite makes its own head's out and lse NaN (0 and -infinity where all its scores are
  * -infinity) and no other's.

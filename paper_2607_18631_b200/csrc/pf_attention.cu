@@ -716,7 +716,7 @@ extern "C" int pf_decode_attention(const pf_kv_cache_t *cache, int32_t dtype, in
     if ((int64_t)n_seq * tiles >= (1ll << 31)) return PF_ERANGE;
     if (n_heads % cache->n_kv != 0 || !isfinite(sm_scale)) return PF_EINVAL;
     if (n_seq == 0 || n_heads == 0) return PF_OK;
-    if (!d_q || !d_out || !d_len || !d_table || !aligned16(d_q) || !aligned16(d_out)) return PF_EINVAL;
+    if (!d_q || !d_out || !d_len || (!d_table && table_cols > 0) || !aligned16(d_q) || !aligned16(d_out)) return PF_EINVAL;
     if ((uintptr_t)d_len % 4 || (uintptr_t)d_table % 4 || (uintptr_t)d_lse % 4) return PF_EINVAL;
     const int64_t row = (int64_t)n_heads * cache->hd;
     if (q_stride < row || out_stride < row || q_stride % 8 || out_stride % 8) return PF_EINVAL;
