@@ -49,3 +49,18 @@ def test_a_status_that_is_not_one_word_is_refused():
     ok = torch.full((1,), 9, dtype=torch.int32, device="cuda")
     layer.forward(x, status=ok)
     assert int(ok) == 0
+
+
+def test_counts_that_do_not_fit_32_bits_are_refused():
+    """2^32 + 3 is not 3."""
+    import torch
+    from paper_2607_18631_b200 import ops
+    big = 1 << 32
+    d = lambda *x: torch.tensor(x, dtype=torch.int32, device="cuda")  # noqa: E731
+    cache = [torch.zeros(4, 2, 16, 64, device="cuda").to(torch.float8_e4m3fn) for _ in range(2)] + [torch.ones(4, 2, device="cuda") for _ in range(2)]
+    k, table, x = torch.randn(3, 2, 64, device="cuda").to(torch.bfloat16), d(0, 1).reshape(1, 2), torch.randn(2, 256, device="cuda")
+    refused(lambda: ops.pf_kv_append(*cache, k, k, d(0, 3), d(0), table, max_new=big + 3))
+    refused(lambda: ops.pf_add_rms_norm(x, group=big + 128))
+    w = [torch.randn(*s, device="cuda").to(torch.bfloat16) for s in ((8, 128), (8, 32, 128), (8, 32, 128), (8, 128, 32))]
+    for kw in (dict(top_k=big + 2), dict(top_k=2, first_expert=big), dict(top_k=2, n_shared=-big)):
+        refused(lambda: ops.MoeLayer(*w, **kw))
