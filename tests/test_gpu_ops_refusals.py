@@ -7,11 +7,12 @@ pytestmark = pytest.mark.gpu
 
 
 def refused(call):
-    from paper_2607_18631_b200 import PlanfrontError, load_library
-    before = load_library().pf_launch_count()
+    from paper_2607_18631_b200 import PlanfrontError
+    from paper_2607_18631_b200.binding import pf_launch_count
+    before = pf_launch_count()
     with pytest.raises(PlanfrontError):
         call()
-    assert load_library().pf_launch_count() == before
+    assert pf_launch_count() == before
 
 
 def moe_layer():
