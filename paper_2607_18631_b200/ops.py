@@ -5,6 +5,9 @@ values, the experts of a few tokens -- as hand-written CUDA on the current devic
 Tensors stay with the caller; outputs and workspaces that are not passed in come from PyTorch's allocator, on the
 stream the call runs on (`stream`, or the current one).  There is no CPU path.
 
+`stream`: the call is enqueued there, and the tensors given to it are marked as used there (they may be dropped at once).
+That they are ready on that stream, and that its results are not used elsewhere before they are, is up to the caller.
+
 8-bit tensors are torch.float8_e4m3fn.
 """
 from __future__ import annotations
@@ -90,6 +93,13 @@ def _stream(torch, dev, stream):
     return stream.cuda_stream if stream is not None else torch._C._cuda_getCurrentRawStream(dev)
 
 
+def _used_on(stream, *tensors):
+    """The allocator is not to hand these tensors' memory out again before the work now enqueued on `stream` is done."""
+    for t in tensors:
+        if t is not None:
+            t.record_stream(stream)
+
+
 def _like(torch, t, dtype=None):
     """A new contiguous tensor of t's shape."""
     if t.is_contiguous():
@@ -129,6 +139,7 @@ def pf_add_rms_norm(x, residual=None, weight=None, *, eps: float = 1e-6, group: 
     L, torch = _ready or _lib()
     if stream is not None:      # the caching allocator hands memory out per stream
         with torch.cuda.stream(stream):
+            _used_on(stream, x, residual, weight, sum_out)
             return pf_add_rms_norm(x, residual, weight, eps=eps, group=group, y=y, q=q, sum_out=sum_out)
     what = "pf_add_rms_norm"
     dev = _on_device(torch, what, x, residual, weight, sum_out)
@@ -212,6 +223,8 @@ def pf_kv_append(k_cache, v_cache, k_scale, v_scale, k, v, cu_new, lengths, tabl
     _counts(what, n_seq, max_new, *table.shape)
     if cu_new.shape != (n_seq + 1,) or table.dim() != 2 or table.shape[0] != n_seq:
         _refuse(f"{what}: cu_new is [sequences + 1], table [sequences, columns]")
+    if stream is not None:
+        _used_on(stream, k_cache, v_cache, k_scale, v_scale, k, v, cu_new, lengths, table)
     status = L.pf_kv_append(c, dt, n_seq, k.shape[0], max_new, k.data_ptr(), _heads(k, what, c.n_kv, c.hd), v.data_ptr(), _heads(v, what, c.n_kv, c.hd),
                             _int32(torch, what, cu_new, 1), _int32(torch, what, lengths, 1), _int32(torch, what, table, 2), table.shape[1],
                             _stream(torch, dev, stream))
@@ -229,6 +242,7 @@ def pf_decode_attention(q, k_cache, v_cache, k_scale, v_scale, lengths, table, *
     L, torch = _ready or _lib()
     if stream is not None:
         with torch.cuda.stream(stream):
+            _used_on(stream, q, k_cache, v_cache, k_scale, v_scale, lengths, table, out, workspace)
             return pf_decode_attention(q, k_cache, v_cache, k_scale, v_scale, lengths, table, sm_scale=sm_scale, lse=lse, out=out, workspace=workspace)
     what = "pf_decode_attention"
     dev = _on_device(torch, what, q, k_cache, v_cache, k_scale, v_scale, lengths, table, out, workspace)
@@ -274,7 +288,9 @@ class MoeLayer:
     router: [experts, H] bf16.  gate, up: [local + shared, F, H], down: [local + shared, H, F], bf16, or float8_e4m3fn with
     fp32 scales per 128 x 128 block ([local + shared, ceil(rows / 128), ceil(columns / 128)]).  Experts
     first_expert .. first_expert + local - 1 live here; the last n_shared of the weight tensors are taken by every token.
-    The layer keeps a packed copy; gate, up, down and their scales may be dropped afterwards."""
+    The layer keeps a packed copy; gate, up, down and their scales may be dropped afterwards.  With `stream` the packing runs there, behind what
+    the current stream holds already.  A forward on another stream than the packing's waits for the packing; one that is
+    captured there cannot, so the packing has to be done by then (torch.cuda.graph synchronizes before it captures)."""
 
     def __init__(self, router, gate, up, down, *, top_k: int, first_expert: int = 0, n_shared: int = 0, gate_scale=None, up_scale=None,
                  down_scale=None, stream=None):
@@ -306,11 +322,27 @@ class MoeLayer:
             _refuse(f"{what}: inconsistent sizes")
         self._L, self._torch, self._dev = L, torch, dev
         self.router = router
+        if stream is not None:
+            stream.wait_stream(torch.cuda.current_stream())
         with contextlib.nullcontext() if stream is None else torch.cuda.stream(stream):
+            if stream is not None:
+                _used_on(stream, gate, up, down, gate_scale, up_scale, down_scale)
             self.packed = torch.empty(size, dtype=torch.uint8, device=router.device)
-        self._router_ptr, self._packed_ptr, self._workspace = router.data_ptr(), self.packed.data_ptr(), {}
-        _check(L.pf_moe_pack(self.m, gate.data_ptr(), up.data_ptr(), down.data_ptr(), _ptr(gate_scale), _ptr(up_scale), _ptr(down_scale),
-                             self.packed.data_ptr(), _stream(torch, dev, stream)), "pf_moe_pack")
+            self._home = _stream(torch, dev, None)         # the packing's stream
+            _check(L.pf_moe_pack(self.m, gate.data_ptr(), up.data_ptr(), down.data_ptr(), _ptr(gate_scale), _ptr(up_scale), _ptr(down_scale),
+                                 self.packed.data_ptr(), self._home), "pf_moe_pack")
+            self._pack_done = torch.cuda.current_stream().record_event()
+        self._router_ptr, self._packed_ptr, self._workspace, self._visited = router.data_ptr(), self.packed.data_ptr(), {}, set()
+
+    def _visit(self, raw):
+        """The first forward on a stream that is not the packing's: it comes after the packing, and the layer's memory is marked as
+        used there."""
+        torch = self._torch
+        stream = torch.cuda.current_stream()
+        _used_on(stream, self.packed, self.router)
+        if not torch.cuda.is_current_stream_capturing():
+            stream.wait_event(self._pack_done)
+            self._visited.add(raw)
 
     def forward(self, x, xq=None, xq_scale=None, *, out=None, status=None, workspace=None, stream=None) -> dict:
         """x: [tokens, H] bf16, 1 .. 512 tokens; xq, xq_scale: the same tokens in 8 bits from pf_add_rms_norm (group 128), which
@@ -319,6 +351,7 @@ class MoeLayer:
         L, torch, m = self._L, self._torch, self.m
         if stream is not None:
             with torch.cuda.stream(stream):
+                _used_on(stream, x, xq, xq_scale, out, status, workspace)
                 return self.forward(x, xq, xq_scale, out=out, status=status, workspace=workspace)
         what = "pf_moe_forward"
         dev = _on_device(torch, what, x, xq, xq_scale, out, status, workspace, self.packed)
@@ -338,6 +371,9 @@ class MoeLayer:
         if out is None:
             out = _like(torch, x)
         ids, weights = (_matrix(torch, T, m.top_k, t, x.device) for t in (torch.int32, torch.float32))
+        raw = _stream(torch, dev, None)
+        if raw != self._home and raw not in self._visited:
+            self._visit(raw)
         if workspace is None:
             size = self._workspace.get(T)
             if size is None:
@@ -346,7 +382,7 @@ class MoeLayer:
         else:
             size = _work_bytes(workspace, what)
         status_of = L.pf_moe_forward(m, T, x.data_ptr(), xs, _ptr(xq), _ptr(xq_scale), self._router_ptr, self._packed_ptr, out.data_ptr(), ids.data_ptr(),
-                                     weights.data_ptr(), _ptr(status), workspace.data_ptr(), size, _stream(torch, dev, None))
+                                     weights.data_ptr(), _ptr(status), workspace.data_ptr(), size, raw)
         if status_of != PF_OK:
             _check(status_of, what)
         return {"out": out, "ids": ids, "weights": weights}
