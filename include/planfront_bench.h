@@ -55,6 +55,12 @@ int pf_check_read(pf_plan_t *plan, uint32_t *out);
  * must show bit 17, index 7, length 4. */
 int pf_check_selftest(pf_plan_t *plan);
 
+/* The limit on the waits between the blocks of pf_moe_forward's kernel (planfront_ops.h), for the process's next calls: `polls` polls (0, and at
+ * most, the library's own limit), and `missing` arrivals (0 or 1) that every meeting waits for and nobody makes.  With missing = 1 and a
+ * small limit each wait runs out: the call ends all the same, d_out is NaN and d_status 1 -- which is how that path is tested.
+ * Errors: PF_ERANGE. */
+int pf_moe_meeting(uint32_t polls, uint32_t missing);
+
 /* How the plan's latest scoring call inside pf_search was divided between the scoring kernel and the kernel that
  * streams constant blocks: the number of blocks of candidates the call's range was cut into, candidates per block,
  * how many blocks the scoring kernel took itself (the evaluated ones), and how many the fill kernel counted as

@@ -121,8 +121,8 @@ int pf_moe_pack(const pf_moe_t *m, const void *d_gate, const void *d_up, const v
  * them (group 128; e4m3 weights only).  d_router: [n_experts, H] bf16, contiguous.  d_packed: see pf_moe_pack.
  * d_out: [T, H] bf16, contiguous.  d_ids [T, top_k] and d_weights [T, top_k]: the router's choice, in order of falling
  * logits (global expert indices).
- * d_status (may be NULL): one word, 0 after a complete call, 1 if a wait between the kernel's blocks ran out (d_out is
- * then not valid).
+ * d_status (may be NULL): one word, 0 after a complete call, 1 if a wait inside the kernel ran out.  d_out is then NaN
+ * (a part of it that was complete before may be right), with or without d_status.
  * PF_EINVAL: NULL or misaligned pointers, inconsistent pf_moe_t, d_xq without d_xscale or with bf16 weights; PF_ERANGE: T outside 0 .. PF_MOE_MAX_TOKENS; PF_EWORKSPACE; T = 0 does nothing. */
 size_t pf_moe_workspace(const pf_moe_t *m, int32_t T);
 int pf_moe_forward(const pf_moe_t *m, int32_t T, const void *d_x, int64_t x_stride, const uint8_t *d_xq, const float *d_xscale,

@@ -29,7 +29,7 @@ EXPORTS = ("pf_version", "pf_strerror", "pf_reason_str", "pf_last_cuda_error", "
            "pf_search_compact_workspace", "pf_search_host_compact", "pf_select_hist", "pf_select_cut",
            "pf_select_write")
 # measurement hooks of include/planfront_bench.h that this library exports (the probes live in probes.py)
-BENCH_EXPORTS = ("pf_launch_count", "pf_timing_enable", "pf_timing_classes", "pf_timing_read", "pf_bench_fill_span", "pf_check_read", "pf_check_selftest")
+BENCH_EXPORTS = ("pf_launch_count", "pf_timing_enable", "pf_timing_classes", "pf_timing_read", "pf_bench_fill_span", "pf_check_read", "pf_check_selftest", "pf_moe_meeting")
 STATIC_SCRATCH_BYTES = 4 << 20
 T_CLASSES = ("score", "topk", "select", "simulate", "aggregate", "fill", "simprep", "compact")
 REASON_BINS = 16
@@ -159,6 +159,8 @@ def load_library(path: str | None = None):
     L.pf_search_host.restype = C.c_int
     L.pf_search_host.argtypes = [vp, u32, u64, u32, u32, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
     L.pf_launch_count.restype = u64
+    L.pf_moe_meeting.restype = C.c_int
+    L.pf_moe_meeting.argtypes = [C.c_uint32, C.c_uint32]
     L.pf_timing_enable.restype = C.c_int
     L.pf_timing_enable.argtypes = [vp, C.c_int]
     L.pf_timing_classes.restype = C.c_int

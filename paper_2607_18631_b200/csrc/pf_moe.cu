@@ -13,6 +13,9 @@
 //    meet, and add up each token's parts in a fixed order.  Four warps of a block copy (bulk copies into a ring of 3 to
 //    5 stages of 32 KB of weights, completion on an mbarrier), sixteen multiply; a multiplying warp waits for nothing but its stage.
 //    While the blocks meet, the ring already fills with the down matrices' first stages, which do not depend on the meeting.
+//  - Every wait has a limit.  Where one runs out (a block that never comes to a meeting, a copy that never arrives) the layer's work goes on as far
+//    as it goes, so that all waits of the block end and nothing is in flight when it does; the status is 1, and every block that knows of it
+//    writes NaN instead of its part of the output.
 //  - 8 gate rows and the same 8 up rows form one 16-row tile: a lane's accumulators hold both factors of its products.
 // Sums are fp32.  bf16 weights multiply bf16 tokens; the hidden activations (fp32) enter the second product as the
 // sum of two bf16 numbers (16 bits of mantissa).  e4m3 weights are widened to fp16, which is exact; tokens and hidden activations
@@ -25,6 +28,7 @@
 // Measured (one B200, device time): 1 token, bf16, 6 + 2 of 64 experts of 4096 x 1408 (277 MB): 66 us; 16 tokens, e4m3, 8 of 128, 32 here, 5120 x
 // 1536 (511 MB): 121 us; 128 tokens, e4m3, 8 of 256, 32 here, 7168 x 2048 (1436 MB): 334 us.  Of the 66 us the streams of the two products take 44
 // (6.3 TB/s), the router's kernel 5, the choice and the sorting of pairs 5, the meetings 8.
+#include <atomic>
 #include <type_traits>
 
 #include "pf_ops.cuh"
@@ -37,6 +41,8 @@ constexpr int kMoeBlock = kMoeThreads + kCopyWarps * 32;
 constexpr int kSliceBytes = 2048;          // 16 rows x KW elements, KW = 64 (bf16) or 128 (e4m3)
 constexpr size_t kMoeSmem = 227 * 1024 - 1024;   // dynamic shared memory of a block, beside its static variables
 constexpr unsigned kMeetLimit = 1u << 21;  // polls of a meeting before it gives up (a poll takes about a microsecond)
+std::atomic<unsigned> g_meet_limit{kMeetLimit}, g_meet_missing{0};      // host: what the next calls wait for (pf_moe_meeting)
+constexpr unsigned kRanOut = 1u << 31;
 constexpr unsigned kRingLimit = 1u << 20;  // waits of up to a microsecond for a stage before they give up
 
 struct MoeArgs {
@@ -62,7 +68,7 @@ struct MoeArgs {
     float *weights;
     int32_t *status;
     // workspace
-    unsigned *ctl;                         // [0] arrivals, [1] a meeting failed
+    unsigned *ctl;                         // arrivals, and kRanOut once a wait ran out
     float *logits;                         // [h_splits][T][n_experts]
     uint16_t *xh;                          // [T][Hk] tokens, zero behind H: bf16, or fp16 times a power of two (e4m3 weights)
     float *xh_scale;                       // [T] that power of two
@@ -70,6 +76,7 @@ struct MoeArgs {
     uint16_t *hop;                         // zero behind F; bf16: [pairs][2][Fk] high and low parts; e4m3: [pairs][Fk] fp16
     float *y;                              // [pairs][H]
     int h_splits, e_tiles, t_chunks;       // router grid
+    unsigned meet_limit, meet_missing;     // polls of a meeting; arrivals that it waits for and nobody makes (0 but in a test of the limit)
 };
 
 // ------------------------------------------------------------------ weight layout
@@ -160,7 +167,7 @@ __global__ void __launch_bounds__(kRouteThreads) moe_route_kernel(const __grid_c
     const int n_gemm = A.e_tiles * A.h_splits * A.t_chunks;
     const int H = A.m.H, E = A.m.n_experts;
     if (blockIdx.x == 0) {
-        if (tid < 2) A.ctl[tid] = 0u;
+        if (tid == 0) *A.ctl = 0u;
         if (tid == 0 && A.status) *A.status = 0;
     }
     if ((int)blockIdx.x < n_gemm) {
@@ -278,19 +285,25 @@ __global__ void __launch_bounds__(kRouteThreads) moe_route_kernel(const __grid_c
 }
 
 // ------------------------------------------------------------------ the layer
-// All blocks of the (cooperative) grid meet, each represented by one thread; false where the wait ran out.
-__device__ __forceinline__ bool arrive_and_poll(unsigned *ctl, unsigned round, bool arrive)
+__device__ __forceinline__ void wait_ran_out(const MoeArgs &A)
+{
+    atomicOr(A.ctl, kRanOut);
+    if (A.status) *A.status = 1;
+}
+// All blocks of the (cooperative) grid meet, each represented by one thread; false where this or any wait before it ran out, here or in a
+// block whose word has come through.
+__device__ __forceinline__ bool arrive_and_poll(const MoeArgs &A, unsigned round, bool arrive)
 {
     if (arrive) {
         __threadfence();
-        atomicAdd(ctl, 1u);
+        atomicAdd(A.ctl, 1u);
     }
     unsigned seen = 0, polls = 0;
     do {
-        asm volatile("ld.acquire.gpu.global.u32 %0, [%1];" : "=r"(seen) : "l"(ctl) : "memory");
-    } while (seen < round && ++polls < kMeetLimit);
+        asm volatile("ld.acquire.gpu.global.u32 %0, [%1];" : "=r"(seen) : "l"(A.ctl) : "memory");
+    } while (seen < round + A.meet_missing && ++polls < A.meet_limit);      // (kRanOut is above any number of arrivals)
     __threadfence();
-    return seen >= round;
+    return seen >= round + A.meet_missing && !(seen & kRanOut);
 }
 template <int ID, int THREADS> __device__ __forceinline__ void bar()
 {
@@ -298,12 +311,15 @@ template <int ID, int THREADS> __device__ __forceinline__ void bar()
 }
 // the multiplying threads (or, before the roles part, all threads) of the block meet the other blocks'
 template <int ID, int THREADS>
-__device__ __forceinline__ bool meet(unsigned *ctl, unsigned &round, int *ok)
+__device__ __forceinline__ bool meet(const MoeArgs &A, unsigned &round, int *ok)
 {
     round += gridDim.x;
     asm volatile("fence.proxy.async;" ::: "memory");      // what was written is read by bulk copies
     bar<ID, THREADS>();
-    if (threadIdx.x == 0) *ok = arrive_and_poll(ctl, round, true);
+    if (threadIdx.x == 0) {
+        *ok = arrive_and_poll(A, round, true);
+        if (!*ok) wait_ran_out(A);
+    }
     bar<ID, THREADS>();
     return *ok != 0;
 }
@@ -426,6 +442,12 @@ __global__ void __launch_bounds__(kMoeBlock, 1) moe_kernel(const __grid_constant
 
     // ---- the choice: one warp per token.  For few tokens each block makes all of it by itself, which saves a meeting.
     const bool by_itself = T <= kMoeWarps;
+    // the block's part of the output, four elements a thread, where a wait ran out
+    auto spoil = [&]() {
+        if (tid >= kMoeThreads) return;
+        for (int i = blockIdx.x * kMoeThreads + tid; i < T * (H / 4); i += gridDim.x * kMoeThreads)
+            reinterpret_cast<uint2 *>(A.out)[i] = make_uint2(0x7FFF7FFFu, 0x7FFF7FFFu);
+    };
     if (tid == 0) {
         for (int i = 0; i < kStages; i++) {
             mbar_init(smem_addr(bars + i), 2 * kCopyWarps);      // full: each copying warp's announcements of weights and of tokens, and their bytes
@@ -445,10 +467,7 @@ __global__ void __launch_bounds__(kMoeBlock, 1) moe_kernel(const __grid_constant
         }
     }
     if (by_itself) __syncthreads();
-    else if (!meet<0, kMoeBlock>(A.ctl, round, &meet_ok)) {
-        if (tid == 0 && A.status) *A.status = 1;
-        return;
-    }
+    else if (!meet<0, kMoeBlock>(A, round, &meet_ok)) return spoil();      // the choices are not there: nothing can be run
 
     // ---- pairs by expert, in pair order within each: off and cnt of every expert (cnt: the end of its pairs), the experts that
     // have any, the chunks of NT tokens before each of those, and which of a token's choices are here.  All blocks arrive at the same.
@@ -719,7 +738,8 @@ __global__ void __launch_bounds__(kMoeBlock, 1) moe_kernel(const __grid_constant
             advance(true, f);
         }
         const unsigned target = round + gridDim.x;
-        if (ok && more(late.c)) ok = arrive_and_poll(A.ctl, target, false);
+        // (where it fails the tokens' rows are copied all the same: the ring's stages stay complete, and the output is spoilt)
+        if (ok && more(late.c) && !arrive_and_poll(A, target, false) && lane == 0) wait_ran_out(A);
         __syncwarp();
         asm volatile("fence.proxy.async;" ::: "memory");
         for (; ok && pos_b < pos; pos_b++) {
@@ -733,15 +753,16 @@ __global__ void __launch_bounds__(kMoeBlock, 1) moe_kernel(const __grid_constant
             filled();
             advance(true, f);
         }
-        // nothing may be in flight when the block ends; after a wait that ran out, the stages without tokens are closed first
+        // Nothing may be in flight when the block ends.  After a wait that ran out (no stage was emptied: the multiplying warps have given up)
+        // the stages without tokens are closed first.
         if (!ok) {
             for (; pos_b < pos; pos_b++) {
                 if (lane == 0) mbar_arrive(full + slot_b * 8);
                 slot_b = slot_b + 1 == kStages ? 0 : slot_b + 1;
             }
-            for (int i = max(0, pos - kStages); i < pos; i++) mbar_wait(full + (i % kStages) * 8, (unsigned)(i / kStages) & 1u);
-            if (lane == 0 && A.status) *A.status = 1;
+            if (lane == 0) wait_ran_out(A);
         }
+        for (int i = max(0, pos - kStages); i < pos && mbar_wait(full + (i % kStages) * 8, (unsigned)(i / kStages) & 1u); i++) {}
         return;
     }
 
@@ -827,7 +848,7 @@ __global__ void __launch_bounds__(kMoeBlock, 1) moe_kernel(const __grid_constant
                     for (int i = 0; i < 4; i++) acc[j][i] = fmaf(sub[x][j][i], i < 2 ? s0 : s1, acc[j][i]);
         }
         __syncwarp();
-        if (lane == 0) mbar_arrive(empty + slot * 8);
+        if (lane == 0 && ok) mbar_arrive(empty + slot * 8);     // a warp that gave up empties no stage: the copies stop
         if (++slot == kStages) {
             slot = 0;
             parity ^= 1u;
@@ -913,8 +934,9 @@ __global__ void __launch_bounds__(kMoeBlock, 1) moe_kernel(const __grid_constant
         }
     }
 
-    // ---- all hidden activations are there
-    ok = meet<3, kMoeThreads>(A.ctl, round, &meet_ok) && ok;
+    // ---- all hidden activations are there (or a wait ran out, which the last meeting hears of)
+    if (!ok && lane == 0) wait_ran_out(A);
+    meet<3, kMoeThreads>(A, round, &meet_ok);
 
     // ---- second product
     for (begin(true, c); more(c); next(true, c)) {
@@ -937,11 +959,8 @@ __global__ void __launch_bounds__(kMoeBlock, 1) moe_kernel(const __grid_constant
             }
         });
     }
-    ok = meet<3, kMoeThreads>(A.ctl, round, &meet_ok) && ok;
-    if (!ok) {
-        if (lane == 0 && A.status) *A.status = 1;
-        return;
-    }
+    if (!ok && lane == 0) wait_ran_out(A);
+    if (!meet<3, kMoeThreads>(A, round, &meet_ok)) return spoil();
 
     // ---- a token's parts, in the order of its choices
     const int quads = H / 4;
@@ -1143,6 +1162,7 @@ extern "C" int pf_moe_forward(const pf_moe_t *m, int32_t T, const void *d_x, int
     a.router = (const uint16_t *)d_router;
     moe_point(a, d_packed);
     a.out = (uint16_t *)d_out; a.ids = d_ids; a.weights = d_weights; a.status = d_status;
+    a.meet_limit = g_meet_limit; a.meet_missing = g_meet_missing;
     cudaStream_t st = (cudaStream_t)stream;
     // Tokens an item takes at most: 8 (a column block of the matrix instruction) where no expert can have more, then 16, and 32 with more
     // than 8 an expert on average: a stage's token rows take room from the ring, and an expert with more tokens than an item is read again,
@@ -1152,4 +1172,12 @@ extern "C" int pf_moe_forward(const pf_moe_t *m, int32_t T, const void *d_x, int
     if ((long long)T * m->top_k <= 8ll * m->n_experts)
         return e4m3 ? moe_launch<true, 16, 5>(a, device, sms, st) : moe_launch<false, 16, 4>(a, device, sms, st);
     return e4m3 ? moe_launch<true, 32, 4>(a, device, sms, st) : moe_launch<false, 32, 4>(a, device, sms, st);
+}
+
+extern "C" int pf_moe_meeting(uint32_t polls, uint32_t missing)
+{
+    if (polls > kMeetLimit || missing > 1) return PF_ERANGE;
+    g_meet_limit = polls ? polls : kMeetLimit;
+    g_meet_missing = missing;
+    return PF_OK;
 }

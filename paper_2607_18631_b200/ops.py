@@ -347,7 +347,8 @@ class MoeLayer:
     def forward(self, x, xq=None, xq_scale=None, *, out=None, status=None, workspace=None, stream=None) -> dict:
         """x: [tokens, H] bf16, 1 .. 512 tokens; xq, xq_scale: the same tokens in 8 bits from pf_add_rms_norm (group 128), which
         e4m3 weights then multiply (the router reads x).  Returns {"out": [tokens, H] bf16, "ids": [tokens, top_k] int32, "weights": [tokens, top_k]
-        fp32}.  status: int32 tensor of one element, see pf_moe_forward."""
+        fp32}.  status: int32 tensor of one element, 0 after a complete call, 1 if a wait inside the kernel ran out; "out" is then NaN, with or
+        without it."""
         L, torch, m = self._L, self._torch, self.m
         if stream is not None:
             with torch.cuda.stream(stream):
