@@ -48,6 +48,10 @@ NOMINAL_HBM_GBS = 7700.0          # HGX B200 data-sheet figure, for context
 # minus that residue.
 FILL_KERNEL_SLICE_DRAM_BYTES = 542_420_224
 FILL_KERNEL_SLICE_CANDIDATES = 46_313_472
+# thread-level instructions the scoring kernel issues per plan that goes through the memory model, the step-time
+# model and the price: smsp__thread_inst_executed.sum with the memory gate lifted minus with the gate on, over the
+# plans the gate had rejected (ncu, profile_case.py --config large_unconstrained --topk-only; summary under profiles/)
+COSTED_PLAN_THREAD_INSTRUCTIONS = 2780
 # thread-level instructions one simulated op needs at least: load the dependency's end, add the hand-over latency,
 # max with the rank's clock, add the duration, store the result, advance the cursor
 SIM_INSTR_PER_OP = 6
@@ -258,14 +262,34 @@ class SearchRig:
     def step(self, stream):
         self.plan.search(self.k, self.s_max, self.k_sim, JITTER_SEED, bufs=self.bufs, stream=stream)
 
+    def timed(self, stream, reps, warm=3):
+        """(ms per call, per-class ms per call) over `reps` calls."""
+        for _ in range(warm):
+            self.step(stream)
+        self.torch.cuda.synchronize()
+        self.plan.timing_enable(True)
+        self.plan.timing_read()
+        a, b = self.torch.cuda.Event(enable_timing=True), self.torch.cuda.Event(enable_timing=True)
+        a.record(stream)
+        for _ in range(reps):
+            self.step(stream)
+        b.record(stream)
+        self.torch.cuda.synchronize()
+        pc = self.plan.timing_read()
+        self.plan.timing_enable(False)
+        return a.elapsed_time(b) / reps, {c: pc[c][0] / reps for c in pc if pc[c][1]}
+
     def close(self):
         self.plan.close()
         self.bufs = None
 
 
 def _config_lines(torch, stream, hbm, peaks):
-    """Device time per call on the benchmark spaces besides the headline one: configs 1-3 and the large space scored
-    alone.  Each line names what bounds it."""
+    """Device time per call on every benchmark space besides the headline one: configs 1-3, the large space scored
+    alone, the unconstrained large space through the whole search (config 5b: 45,116 survivors), the same with the
+    memory gate lifted (the cost-heavy scoring case: 1.17 M plans through the cost model; the simulator tier at its
+    nominal 1e6 survivors).  Each line names what bounds it."""
+    import oracle
     from paper_2607_18631_b200 import Plan
     out = {}
     for name, k in (("tiny", 16), ("mid", 128), ("serve", 128)):
@@ -305,10 +329,58 @@ def _config_lines(torch, stream, hbm, peaks):
     plan.close()
     del o
     torch.cuda.empty_cache()
-    # The large space with the dry-run rules off is not run: its search has ended in an illegal-instruction error in long
-    # runs and once after a few calls here, and the cause has not been found.
-    for label in ("large_unconstrained", "large_unconstrained_gate_lifted"):
-        out[label] = {"unavailable": "the search of this space has ended in an illegal-instruction error, cause not found"}
+    # config 5b and the nominal-size simulator tier
+    for label, lift in (("large_unconstrained", False), ("large_unconstrained_gate_lifted", True)):
+        cfg = make_config("large_unconstrained")
+        if lift:
+            cfg["cluster"]["budget_bytes"] = 10 ** 15
+        rig = SearchRig(torch, cfg, K_TOP, S_MAX, K_SIM)
+        ms, cls = rig.timed(stream, reps=10 if lift else 20)
+        n_surv = int(rig.bufs["surv_count"].item())
+        n_feas = int(((rig.bufs["reason"] & 0x7F) == 0).sum().item())
+        ops, chain = _survivor_shapes(rig.plan, cfg, rig.bufs["surv_idx"][:n_surv].cpu().numpy()[::max(1, n_surv // 20000)])
+        ops *= max(1, n_surv // 20000) if n_surv > 20000 else 1
+        line = {"candidates": rig.N, "call": "pf_search", "ms_per_call": ms, "candidates_per_s": rig.N / (ms * 1e-3),
+                "feasible": n_feas, "survivors": n_surv, "class_ms": cls,
+                "simulator": {"ms": cls.get("simulate", 0.0), "survivors_per_s": n_surv / (cls["simulate"] * 1e-3),
+                              "simulated_ops": ops, "longest_chain_steps": chain,
+                              "alu_frac": SIM_INSTR_PER_OP * ops / peaks["logic"] / (cls["simulate"] * 1e-3)},
+                "bound": "hbm (the fill kernel) beside the latency-bound simulator" if not lift
+                else "alu / latency: the simulator's 1e6 survivors dominate the call"}
+        if lift:
+            # cost-heavy scoring: every feasible plan goes through the memory and step-time model.  ALU bound from
+            # the oracle's operation tally over a sample of the FEASIBLE candidates only (the work the kernel cannot
+            # skip), against the measured issue rates; HBM bound from the dense outputs.
+            oracle.build()
+            orc = oracle.Oracle(cfg)
+            feas = torch.nonzero((rig.bufs["reason"] & 0x7F) == 0).flatten().cpu().numpy()
+            pick = feas[:: max(1, len(feas) // 1500)]
+            io = fo = 0
+            for i in pick:
+                c = oracle.count_ops(orc, int(i), 1)
+                io += c["int_ops"]
+                fo += c["fp_ops"]
+            i_per, f_per = io / len(pick), fo / len(pick)
+            t_alu = n_feas * (i_per / min(peaks["imad"], peaks["logic"]) + f_per / peaks["ffma"])
+            t_hbm = rig.N * BYTES_PER_CANDIDATE / (hbm * 1e9)
+            head_ms = cls.get("score", 0.0)
+            line["cost_heavy_scoring"] = {
+                "feasible_through_cost_model": n_feas, "int_ops_per_feasible": i_per, "fp_ops_per_feasible": f_per,
+                "ops_source": f"oracle operation tally over {len(pick)} sampled feasible candidates",
+                "t_alu_ms": t_alu * 1e3, "t_hbm_ms": t_hbm * 1e3, "score_kernel_ms": head_ms,
+                "note": "the scoring kernel of this call writes the evaluated blocks only; its ALU work is the feasible "
+                        "candidates' cost model plus the rule tables",
+                "alu_frac_of_score_kernel": t_alu * 1e3 / head_ms if head_ms else None,
+                # from the ncu capture summarised under profiles/ (score kernel, cost-heavy slice): what the
+                # compiled kernel issues per plan it takes through the cost model, and the issue-rate bound on that
+                "issued_thread_instructions_per_costed_plan": COSTED_PLAN_THREAD_INSTRUCTIONS,
+                "t_issue_ms": n_feas * COSTED_PLAN_THREAD_INSTRUCTIONS / peaks["logic"] * 1e3,
+                "issue_frac_of_score_kernel": (n_feas * COSTED_PLAN_THREAD_INSTRUCTIONS / peaks["logic"] * 1e3 / head_ms
+                                               if head_ms else None)}
+        out[label] = line
+        rig.close()
+        del rig
+        torch.cuda.empty_cache()
     return out
 
 
