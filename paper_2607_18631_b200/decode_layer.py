@@ -22,23 +22,35 @@ CAP_SLACK = 64       # tokens a sequence may grow by after the context it starts
 
 
 def layer_shape(cfg: dict, plan: dict) -> dict:
-    """What one GPU of a serving plan (a decoded tuple: kv, batch, dpa, ep, tp) holds of a layer."""
+    """What one GPU of a serving plan (a decoded tuple: kv, batch, dpa, ep, tp) holds of a layer, and the tokens of a step.
+
+    tokens: sequences whose attention runs here.  expert_tokens: tokens that the experts here see: with data-parallel attention those of
+    all ep groups, as the serving model counts them.  Shared experts (`shared` of width `shared_ffn`) are split over tp like the rest of
+    the dense weights and see this GPU's own tokens."""
     m, k = cfg["model"], cfg["kern"][plan["kv"]]
     tp, ep, batch = plan["tp"], plan["ep"], plan["batch"]
+
+    def refuse(why):
+        raise PlanfrontError(PF_EINVAL, f"decode_layer: {why}")
     if m["attn_kind"] != 0:
-        raise PlanfrontError(PF_EINVAL, "decode_layer: latent attention has no per-head cache")
+        refuse("latent attention has no per-head cache")
     if m["nh"] % tp or m["E"] % ep or m["nkv"] < 1:
-        raise PlanfrontError(PF_EINVAL, "decode_layer: heads do not divide by tp, or experts by ep")
+        refuse("heads do not divide by tp, or experts by ep")
+    if m["nkv"] % tp and tp % m["nkv"]:
+        refuse(f"{m['nkv']} key / value heads cannot be split over tp {tp}")
+    tokens = batch // ep if plan["dpa"] else batch
+    if tokens < 1:
+        refuse(f"a batch of {batch} leaves GPUs of ep {ep} without a sequence")
     engine = tp * ep if plan["dpa"] else tp          # GPUs of one engine, as the serving model counts them
     moe_tp = max(1, engine // ep)
-    return dict(tokens=batch // ep if plan["dpa"] else batch, hidden=m["H"], heads=m["nh"] // tp, kv_heads=max(1, m["nkv"] // tp), head_dim=m["hd"],
-                experts=m["E"], local=m["E"] // ep, top_k=m["K"], ffn=-(-m["F"] // moe_tp), shared=m["S"] if m["Fs"] == m["F"] else 0,
+    return dict(tokens=tokens, expert_tokens=batch, hidden=m["H"], heads=m["nh"] // tp, kv_heads=max(1, m["nkv"] // tp), head_dim=m["hd"],
+                experts=m["E"], local=m["E"] // ep, top_k=m["K"], ffn=-(-m["F"] // moe_tp), shared=m["S"], shared_ffn=-(-m["Fs"] // tp) if m["S"] else 0,
                 weights="e4m3" if k["wbytes"] == 1 else "bf16")
 
 
 class DecodeLayer:
-    """A layer's weights and cache on the current device, and its decode step.  shape: see layer_shape; context: cached tokens
-    of every sequence at the start."""
+    """A layer's weights and cache on the current device, and its decode step.  shape: see layer_shape (expert_tokens, if left out, is
+    tokens, and shared_ffn is ffn); context: cached tokens of every sequence at the start."""
 
     def __init__(self, shape: dict, context: int, page: int = 64, seed: int = 0):
         import torch
@@ -54,17 +66,30 @@ class DecodeLayer:
 
         self.norm1, self.norm2 = (torch.ones(H, dtype=torch.bfloat16, device=dev) for _ in range(2))
         self.w_qkv, self.w_out = weight((nh + 2 * nkv) * d, H), weight(H, nh * d)
-        n = s["local"] + s["shared"]
-        mats, scales = [], [None] * 3
-        for i, dims in enumerate(((n, s["ffn"], H), (n, s["ffn"], H), (n, H, s["ffn"]))):
-            if s["weights"] == "bf16":
-                mats.append(torch.cat([weight(1, *dims[1:]) for _ in range(n)]))
-                continue
-            mats.append(torch.cat([(torch.randn(1, *dims[1:], generator=g, device=dev) * 112).clamp_(-448, 448).to(torch.float8_e4m3fn).view(torch.uint8)
-                                   for _ in range(n)]).view(torch.float8_e4m3fn))
-            scales[i] = torch.full((n, -(-dims[1] // 128), -(-dims[2] // 128)), dims[2] ** -0.5 / 112, device=dev)
-        self.moe = ops.MoeLayer(weight(s["experts"], H), *mats, top_k=s["top_k"], n_shared=s["shared"], gate_scale=scales[0], up_scale=scales[1],
-                                down_scale=scales[2])
+        s.setdefault("expert_tokens", T)
+        s.setdefault("shared_ffn", s["ffn"])
+        self.router = None
+
+        def layer_of(n, ffn, n_shared):
+            mats, scales = [], [None] * 3
+            for i, dims in enumerate(((n, ffn, H), (n, ffn, H), (n, H, ffn))):
+                if s["weights"] == "bf16":
+                    mats.append(torch.cat([weight(1, *dims[1:]) for _ in range(n)]))
+                    continue
+                mats.append(torch.cat([(torch.randn(1, *dims[1:], generator=g, device=dev) * 112).clamp_(-448, 448).to(torch.float8_e4m3fn).view(torch.uint8)
+                                       for _ in range(n)]).view(torch.float8_e4m3fn))
+                scales[i] = torch.full((n, -(-dims[1] // 128), -(-dims[2] // 128)), dims[2] ** -0.5 / 112, device=dev)
+            if self.router is None:
+                self.router = weight(s["experts"], H)
+            return ops.MoeLayer(self.router, *mats, top_k=s["top_k"], n_shared=n_shared, gate_scale=scales[0], up_scale=scales[1], down_scale=scales[2])
+
+        # shared experts go with the routed ones where they have the same width and tokens, else they are a layer of their own
+        together = not s["shared"] or (s["shared_ffn"] == s["ffn"] and s["expert_tokens"] == T)
+        self.moe = layer_of(s["local"] + (s["shared"] if together else 0), s["ffn"], s["shared"] if together else 0)
+        self.shared = None if together else layer_of(s["shared"], s["shared_ffn"], s["shared"])
+        # the other GPUs' tokens, which an all-gather would bring: they stay the same from step to step
+        others = torch.randn(s["expert_tokens"] - T, H, generator=g, device=dev).to(torch.bfloat16)
+        self.others = ops.pf_add_rms_norm(others, None, self.norm2, y=True) if others.shape[0] else None
         cols = -(-(context + CAP_SLACK) // page)
         self.table = torch.randperm(T * cols, generator=g, device=dev).to(torch.int32).reshape(T, cols)
         self.cache = [torch.empty(T * cols, nkv, page, d, dtype=torch.float8_e4m3fn, device=dev) for _ in range(2)]
@@ -104,9 +129,21 @@ class DecodeLayer:
     def attend(self, q):
         return self.ops.pf_decode_attention(q, *self.cache, *self.scales, self.lengths, self.table)["out"]
 
-    def experts(self, n):
+    def gather(self, n):
+        """The tokens that the experts here see: this GPU's first, then the others'."""
+        if self.others is None:
+            return n
+        whole = {k: self.torch.cat([n[k], self.others[k]]) for k in ("y", "scale")}
+        whole["q"] = self.torch.cat([t["q"].view(self.torch.uint8) for t in (n, self.others)]).view(n["q"].dtype)
+        return whole
+
+    def run(self, layer, n):
         eight = (n["q"], n["scale"]) if self.shape["weights"] == "e4m3" else ()
-        return self.moe.forward(n["y"], *eight)["out"]
+        return layer.forward(n["y"], *eight)["out"]
+
+    def experts(self, n):
+        out = self.run(self.moe, self.gather(n))[:n["y"].shape[0]]
+        return out if self.shared is None else out + self.run(self.shared, n)
 
     def measure(self, repeats: int = 20) -> dict:
         """{part: (microseconds, bytes it cannot do without)} of the attention and the experts, device time of a call."""
@@ -114,10 +151,11 @@ class DecodeLayer:
         x = torch.randn(s["tokens"], s["hidden"], device="cuda").to(torch.bfloat16)
         n = self.ops.pf_add_rms_norm(x, None, self.norm2, y=True)
         q = self.project(x)[0]
-        ids = self.moe.forward(n["y"])["ids"]
-        touched = int(torch.unique(ids[ids < s["local"]]).numel()) + s["shared"]
+        whole = self.gather(n)
+        ids = self.moe.forward(whole["y"])["ids"]
+        touched = int(torch.unique(ids[ids < s["local"]]).numel())
         cache_bytes = int(self.lengths.sum()) * s["kv_heads"] * s["head_dim"] * 2
-        expert_bytes = touched * 3 * s["hidden"] * s["ffn"] * (1 if s["weights"] == "e4m3" else 2)
+        expert_bytes = 3 * s["hidden"] * (touched * s["ffn"] + s["shared"] * s["shared_ffn"]) * (1 if s["weights"] == "e4m3" else 2)
         out = {}
         for name, call, size in (("attention", lambda: self.attend(q), cache_bytes), ("experts", lambda: self.experts(n), expert_bytes)):
             graph = torch.cuda.CUDAGraph()
