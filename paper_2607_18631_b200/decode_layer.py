@@ -3,8 +3,9 @@
 The serving model prices a decode step per layer as the attention (projection weights and cached keys and values over
 HBM) plus the experts (the weights of those that a token chose).  `DecodeLayer` holds one layer as one GPU of a plan
 holds it -- attention heads over tp, experts over ep, expert width over what is left -- with random weights, and runs
-its step with the operators of `ops`; the projections are plain matrix products.  `measure` times the parts, and
+its step with the operators of `ops`; the projections are plain matrix products.  `measure` times the parts out of HBM, and
 `with_measured_hbm` puts the rate they reached into a plan space's cluster, so that the space is ranked again with it.
+(The model's other measured numbers, the efficiencies by tokens an expert, stay as they are.)
 
     python -m paper_2607_18631_b200.decode_layer [--batch N] [--context N]
 
@@ -19,6 +20,7 @@ import copy
 from .binding import PF_EINVAL, PlanfrontError
 
 CAP_SLACK = 64       # tokens a sequence may grow by after the context it starts with
+MIN_RATE_BYTES = 32_000_000   # 5 us at HBM's rate: what less takes is mostly launches and dependent reads
 
 
 def layer_shape(cfg: dict, plan: dict) -> dict:
@@ -146,39 +148,45 @@ class DecodeLayer:
         return out if self.shared is None else out + self.run(self.shared, n)
 
     def measure(self, repeats: int = 20) -> dict:
-        """{part: (microseconds, bytes it cannot do without)} of the attention and the experts, device time of a call."""
+        """{part: (microseconds, bytes it cannot do without)} of the attention and the experts, device time of a call whose cache and weights
+        come from HBM: in front of each, a buffer of four times the L2 is read."""
         torch, s = self.torch, self.shape
         x = torch.randn(s["tokens"], s["hidden"], device="cuda").to(torch.bfloat16)
         n = self.ops.pf_add_rms_norm(x, None, self.norm2, y=True)
-        q = self.project(x)[0]
         whole = self.gather(n)
+        q = self.project(x)[0].contiguous()
         ids = self.moe.forward(whole["y"])["ids"]
         touched = int(torch.unique(ids[ids < s["local"]]).numel())
+        element = 1 if s["weights"] == "e4m3" else 2
         cache_bytes = int(self.lengths.sum()) * s["kv_heads"] * s["head_dim"] * 2
-        expert_bytes = 3 * s["hidden"] * (touched * s["ffn"] + s["shared"] * s["shared_ffn"]) * (1 if s["weights"] == "e4m3" else 2)
+        expert_bytes = 3 * s["hidden"] * (touched * s["ffn"] + s["shared"] * s["shared_ffn"]) * element
+
+        def experts():
+            self.run(self.moe, whole)
+            if self.shared is not None:
+                self.run(self.shared, n)
+        evict = torch.zeros(torch.cuda.get_device_properties(x.device).L2_cache_size, dtype=torch.float32, device=x.device)
         out = {}
-        for name, call, size in (("attention", lambda: self.attend(q), cache_bytes), ("experts", lambda: self.experts(n), expert_bytes)):
-            graph = torch.cuda.CUDAGraph()
+        for name, call, size in (("attention", lambda: self.attend(q), cache_bytes), ("experts", experts, expert_bytes)):
             call()
+            events = [[torch.cuda.Event(enable_timing=True) for _ in range(2)] for _ in range(repeats)]
+            for a, b in events:
+                evict.amax()               # long enough for the host to have the call enqueued
+                a.record()
+                call()
+                b.record()
             torch.cuda.synchronize()
-            with torch.cuda.graph(graph):
-                for _ in range(repeats):
-                    call()
-            graph.replay()
-            a, b = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
-            a.record()
-            graph.replay()
-            b.record()
-            b.synchronize()
-            out[name] = (a.elapsed_time(b) * 1e3 / repeats, size)
-            del graph
+            out[name] = (sum(a.elapsed_time(b) for a, b in events) * 1e3 / repeats, size)
         return out
 
 
 def with_measured_hbm(cfg: dict, parts: dict) -> dict:
-    """The plan space with the HBM rate that the measured parts reached together."""
+    """The plan space with the HBM rate that the measured parts reached together.  Parts of less than MIN_RATE_BYTES measure latency, not a rate, and
+    do not count; without any other the rate stays as it is."""
     new = copy.deepcopy(cfg)
-    new["cluster"]["hbm_bw"] = sum(size for _, size in parts.values()) / (sum(us for us, _ in parts.values()) * 1e-6)
+    large = [part for part in parts.values() if part[1] >= MIN_RATE_BYTES]
+    if large:
+        new["cluster"]["hbm_bw"] = sum(size for _, size in large) / (sum(us for us, _ in large) * 1e-6)
     return new
 
 
@@ -233,7 +241,8 @@ def main(argv=None) -> None:
     torch.cuda.synchronize()
     parts = layer.measure()
     for name, (us, size) in parts.items():
-        print(f"{name:10s} {us:9.1f} us  {size / 1e6:9.1f} MB  {size / us / 1e6:6.2f} TB/s")
+        rate = f"{size / us / 1e6:6.2f} TB/s" if size >= MIN_RATE_BYTES else "(latency)"
+        print(f"{name:10s} {us:9.1f} us  {size / 1e6:9.1f} MB  {rate}")
     again = with_measured_hbm(cfg, parts)
     plan, tput = best_plan(again)
     print(f"with {again['cluster']['hbm_bw'] / 1e12:.2f} TB/s: tp {plan['tp']} ep {plan['ep']}, predicted {tput:.1f} tokens/s/GPU")

@@ -41,3 +41,32 @@ def test_heads_that_do_not_split_are_refused():
             D.layer_shape(space(nh=24, nkv=nkv), dict(BASE, tp=tp))
     with pytest.raises(PlanfrontError):
         D.layer_shape(space(), dict(BASE, batch=2, dpa=1, ep=4))
+
+
+def test_parts_too_small_for_a_rate_do_not_enter_the_cluster():
+    cfg = D.example_space(8, 512)
+    big, tiny = (20.0, 100_000_000), (9.0, 2_500_000)
+    assert D.with_measured_hbm(cfg, {"attention": tiny, "experts": big})["cluster"]["hbm_bw"] == pytest.approx(5e12)
+    assert D.with_measured_hbm(cfg, {"attention": tiny, "experts": tiny})["cluster"]["hbm_bw"] == cfg["cluster"]["hbm_bw"]
+
+
+@pytest.mark.gpu
+def test_measured_parts_come_from_hbm():
+    """A cache of 34 MB, which the L2 would hold: measured as a call is after other work has gone through the L2."""
+    import torch
+    shape = dict(tokens=64, hidden=512, heads=16, kv_heads=4, head_dim=128, experts=4, local=4, top_k=1, ffn=64, shared=0, weights="bf16")
+    layer = D.DecodeLayer(shape, context=500, page=64)
+    parts = layer.measure()
+    assert set(parts) == {"attention", "experts"} and parts["attention"][1] == 64 * 500 * 4 * 128 * 2
+    q = torch.randn(64, 16, 128, device="cuda").to(torch.bfloat16)
+    filler = torch.zeros(1 << 29, dtype=torch.uint8, device="cuda")
+    cold = []
+    for _ in range(10):
+        a, b = (torch.cuda.Event(enable_timing=True) for _ in range(2))
+        filler.view(torch.int32).amax()
+        a.record()
+        layer.attend(q)
+        b.record()
+        torch.cuda.synchronize()
+        cold.append(a.elapsed_time(b) * 1e3)
+    assert parts["attention"][0] > 0.75 * sorted(cold)[5]
