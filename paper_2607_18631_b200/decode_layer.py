@@ -17,7 +17,7 @@ from __future__ import annotations
 import argparse
 import copy
 
-from .binding import PF_EINVAL, PlanfrontError
+from .binding import PF_ECUDA, PF_EINVAL, PlanfrontError
 
 CAP_SLACK = 64       # tokens a sequence may grow by after the context it starts with
 MIN_RATE_BYTES = 32_000_000   # 5 us at HBM's rate: what less takes is mostly launches and dependent reads
@@ -89,6 +89,7 @@ class DecodeLayer:
         together = not s["shared"] or (s["shared_ffn"] == s["ffn"] and s["expert_tokens"] == T)
         self.moe = layer_of(s["local"] + (s["shared"] if together else 0), s["ffn"], s["shared"] if together else 0)
         self.shared = None if together else layer_of(s["shared"], s["shared_ffn"], s["shared"])
+        self.status = torch.zeros(2, dtype=torch.int32, device=dev)        # of the two layers' latest calls
         # the other GPUs' tokens, which an all-gather would bring: they stay the same from step to step
         others = torch.randn(s["expert_tokens"] - T, H, generator=g, device=dev).to(torch.bfloat16)
         self.others = ops.pf_add_rms_norm(others, None, self.norm2, y=True) if others.shape[0] else None
@@ -139,13 +140,18 @@ class DecodeLayer:
         whole["q"] = self.torch.cat([t["q"].view(self.torch.uint8) for t in (n, self.others)]).view(n["q"].dtype)
         return whole
 
-    def run(self, layer, n):
+    def run(self, layer, n, status):
         eight = (n["q"], n["scale"]) if self.shape["weights"] == "e4m3" else ()
-        return layer.forward(n["y"], *eight)["out"]
+        return layer.forward(n["y"], *eight, status=self.status[status:status + 1])["out"]
 
     def experts(self, n):
-        out = self.run(self.moe, self.gather(n))[:n["y"].shape[0]]
-        return out if self.shared is None else out + self.run(self.shared, n)
+        out = self.run(self.moe, self.gather(n), 0)[:n["y"].shape[0]]
+        return out if self.shared is None else out + self.run(self.shared, n, 1)
+
+    def check(self):
+        """Waits for the device; raises if a wait inside a layer's latest call ran out (its output is NaN then)."""
+        if self.status.any().item():
+            raise PlanfrontError(PF_ECUDA, "decode_layer: a wait inside the experts' kernel ran out")
 
     def measure(self, repeats: int = 20) -> dict:
         """{part: (microseconds, bytes it cannot do without)} of the attention and the experts, device time of a call whose cache and weights
@@ -162,9 +168,9 @@ class DecodeLayer:
         expert_bytes = 3 * s["hidden"] * (touched * s["ffn"] + s["shared"] * s["shared_ffn"]) * element
 
         def experts():
-            self.run(self.moe, whole)
+            self.run(self.moe, whole, 0)
             if self.shared is not None:
-                self.run(self.shared, n)
+                self.run(self.shared, n, 1)
         evict = torch.zeros(torch.cuda.get_device_properties(x.device).L2_cache_size, dtype=torch.float32, device=x.device)
         out = {}
         for name, call, size in (("attention", lambda: self.attend(q), cache_bytes), ("experts", experts, expert_bytes)):
@@ -177,6 +183,7 @@ class DecodeLayer:
                 b.record()
             torch.cuda.synchronize()
             out[name] = (sum(a.elapsed_time(b) for a, b in events) * 1e3 / repeats, size)
+        self.check()
         return out
 
 
@@ -238,7 +245,7 @@ def main(argv=None) -> None:
     residual = torch.zeros_like(x)
     for _ in range(a.steps):
         x = layer.step(x, residual)
-    torch.cuda.synchronize()
+    layer.check()
     parts = layer.measure()
     for name, (us, size) in parts.items():
         rate = f"{size / us / 1e6:6.2f} TB/s" if size >= MIN_RATE_BYTES else "(latency)"

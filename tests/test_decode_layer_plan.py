@@ -70,3 +70,22 @@ def test_measured_parts_come_from_hbm():
         torch.cuda.synchronize()
         cold.append(a.elapsed_time(b) * 1e3)
     assert parts["attention"][0] > 0.75 * sorted(cold)[5]
+
+
+@pytest.mark.gpu
+def test_a_wait_that_ran_out_is_raised():
+    import torch
+    from paper_2607_18631_b200.binding import load_library
+    L = load_library()
+    shape = dict(tokens=3, hidden=256, heads=4, kv_heads=2, head_dim=64, experts=4, local=4, top_k=2, ffn=64, shared=0, weights="bf16")
+    layer = D.DecodeLayer(shape, context=5, page=16)
+    x, residual = (torch.randn(3, 256, device="cuda").to(torch.bfloat16) for _ in range(2))
+    assert L.pf_moe_meeting(2000, 1) == 0
+    try:
+        assert torch.isnan(layer.step(x, residual.clone()).float()).all()
+        with pytest.raises(PlanfrontError):
+            layer.check()
+    finally:
+        assert L.pf_moe_meeting(0, 0) == 0
+    layer.step(x, residual)
+    layer.check()
