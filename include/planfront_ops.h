@@ -111,7 +111,7 @@ typedef struct {
  * [n_local + n_shared, ceil(F / 128), ceil(H / 128)], d_down_scale [.., ceil(H / 128), ceil(F / 128)] (NULL with bf16).
  * d_packed: pf_moe_packed_bytes(m) bytes (0 where `m` is not valid), 256-byte aligned; it holds everything that
  * pf_moe_forward needs of the weights.
- * PF_EINVAL: NULL or misaligned pointers, inconsistent pf_moe_t, scales missing or not wanted; PF_ERANGE: more than 2^34 rows. */
+ * PF_EINVAL: NULL or misaligned pointers, inconsistent pf_moe_t, scales missing or not wanted. */
 size_t pf_moe_packed_bytes(const pf_moe_t *m);
 int pf_moe_pack(const pf_moe_t *m, const void *d_gate, const void *d_up, const void *d_down, const float *d_gate_scale,
                 const float *d_up_scale, const float *d_down_scale, void *d_packed, void *stream);

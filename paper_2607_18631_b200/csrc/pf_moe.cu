@@ -21,8 +21,9 @@
 // sum of two bf16 numbers (16 bits of mantissa).  e4m3 weights are widened to fp16, which is exact; tokens and hidden activations
 // are scaled by a power of two per row and rounded to fp16 (11 bits); a weight block's scale is applied to the fp32 sum of
 // its 128 columns.  A hidden row's power of two has to be known before the row is: |h_f| <= |g_f . x| |u_f . x| <= |x|^2 max|g| max|u|
-// (Cauchy-Schwarz; |silu(a)| <= |a|), with the experts' largest row norms from pf_moe_pack.  The bound may lie 2^29 above the largest
-// |h| before fp16's least step costs more than its 11 bits (with random weights it lies a factor H above).
+// (Cauchy-Schwarz; |silu(a)| <= |a|), the maxima over blocks of 128 hidden units, whose sizes pf_moe_pack has evened out.  The bound may lie
+// 2^29 above an |h| before fp16's least step costs it any of its 11 bits; with random weights it lies a factor H above, which leaves
+// 2^16 for gate and up rows of a block that are larger than its others.
 // The legacy matrix instruction is enough: at full HBM speed a scheduler gets a 2 KB slice every 333 cycles, and its products take 70 for up to
 // 8 tokens an expert.  Beyond 16 tokens an expert the reads of token rows from shared memory (4 per product) bound the kernel.
 // Measured (one B200, device time): 1 token, bf16, 6 + 2 of 64 experts of 4096 x 1408 (277 MB): 66 us; 16 tokens, e4m3, 8 of 128, 32 here, 5120 x
@@ -54,7 +55,7 @@ struct MoeArgs {
     int Hk, Fk;                            // H and F rounded up to whole slices: row lengths of the products' inputs
     size_t set_bytes, down_at;             // packed bytes per expert, offset of its down part
     size_t n_up_scales, n_down_scales;     // block scales of one expert's gate (or up) and down matrices
-    size_t packed_bytes;                   // matrices, then gate, up and down scales, then row norms
+    size_t packed_bytes;                   // matrices, then gate, up and down scales, then bounds
     const uint16_t *x;
     int64_t xs;
     const uint8_t *xq;
@@ -62,7 +63,7 @@ struct MoeArgs {
     const uint16_t *router;
     const uint8_t *packed;
     const float *gs, *us, *ds;             // block scales and bounds, behind the packed matrices (e4m3 weights)
-    const float *row_max;                  // [n_sets][2] largest squared row norm of gate and of up
+    const float *row_max;                  // [n_sets][2] squares whose roots' product bounds a hidden unit's size over |x|^2
     uint16_t *out;
     int32_t *ids;
     float *weights;
@@ -118,25 +119,65 @@ __global__ void __launch_bounds__(256) moe_pack_kernel(const pf_moe_t m, int n_s
     }
 }
 
-// largest squared row norms of an expert's gate and up matrices (e4m3 with block scales): one warp per row, maxima over rows
-__global__ void __launch_bounds__(256) moe_row_norm_kernel(const pf_moe_t m, int n_sets, const uint8_t *gate, const uint8_t *up, const float *gs,
-                                                           const float *us, float *row_max)
+// A block of 128 hidden units of an expert (e4m3): its units' sizes are bounded by |x|^2 p, p the product of the block's largest gate and up row
+// norms.  The block's up scales are multiplied by 2^-b and its down scales by 2^b, p = 1.m * 2^b, so that the activations of all
+// blocks come out below 2 |x|^2 and one block's outlier rows take no bits off the others' fp16 numbers.  What is left of the
+// bound, squared (1.m^2, more where b is clamped), goes to the expert's largest.
+__global__ void __launch_bounds__(256) moe_block_norm_kernel(const pf_moe_t m, const uint8_t *gate, const uint8_t *up, const float *gs, float *us, float *ds,
+                                                             float *bound2)
 {
-    const long long row = ((long long)blockIdx.x * blockDim.x + threadIdx.x) / 32;
-    if (row >= (long long)n_sets * m.F * 2) return;
-    const int lane = threadIdx.x & 31, which = (int)(row & 1), f = (int)((row >> 1) % m.F), set = (int)((row >> 1) / m.F);
-    const int kb = (m.H + 127) / 128, fb = (m.F + 127) / 128;
-    const uint8_t *w = (which ? up : gate) + ((size_t)set * m.F + f) * m.H;
-    const float *sc = (which ? us : gs) + ((size_t)set * fb + f / 128) * kb;
-    float ss = 0.f;
-    for (int k = lane * 2; k < m.H; k += 64) {
-        const float2 v = f32x2_of_f16x2(f16x2_of_e4m3x2(*reinterpret_cast<const uint16_t *>(w + k)));
-        const float s = sc[k / 128];
-        ss = fmaf(v.x * s, v.x * s, fmaf(v.y * s, v.y * s, ss));
-    }
+    __shared__ float part[2][8];
+    const int kb = (m.H + 127) / 128, fb = (m.F + 127) / 128, set = blockIdx.x / fb, block = blockIdx.x - set * fb;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, rows = min(128, m.F - block * 128);
+    float *su = us + ((size_t)set * fb + block) * kb, *sd = ds + (size_t)set * kb * fb + block;
+    float top[2] = {0.f, 0.f};
+    bool nan = false;
+    for (int r = warp; r < rows; r += 8)
 #pragma unroll
-    for (int o = 16; o; o >>= 1) ss += __shfl_xor_sync(0xFFFFFFFFu, ss, o);
-    if (lane == 0) atomicMax(reinterpret_cast<unsigned *>(row_max + set * 2 + which), __float_as_uint(ss));   // not negative: bits in the order of the values
+        for (int which = 0; which < 2; which++) {
+            const uint8_t *w = (which ? up : gate) + ((size_t)set * m.F + block * 128 + r) * m.H;
+            const float *sc = which ? su : gs + ((size_t)set * fb + block) * kb;
+            float ss = 0.f;
+            for (int k = lane * 16; k < m.H; k += 512) {
+                const uint4 v = *reinterpret_cast<const uint4 *>(w + k);
+                const uint32_t c[4] = {v.x, v.y, v.z, v.w};
+                float sum = 0.f;
+#pragma unroll
+                for (int i = 0; i < 4; i++) {
+                    const float2 f = f32x2_of_f16x2(f16x2_of_e4m3x2(c[i])), g = f32x2_of_f16x2(f16x2_of_e4m3x2(c[i] >> 16));
+                    sum = fmaf(f.x, f.x, fmaf(f.y, f.y, fmaf(g.x, g.x, fmaf(g.y, g.y, sum))));
+                }
+                const float s = sc[k / 128];
+                ss = fmaf(sum * s, s, ss);
+            }
+#pragma unroll
+            for (int o = 16; o; o >>= 1) ss += __shfl_xor_sync(0xFFFFFFFFu, ss, o);
+            top[which] = fmaxf(top[which], ss);
+            nan |= ss != ss;
+        }
+    if (lane == 0) {
+        part[0][warp] = nan ? __int_as_float(0x7FFFFFFF) : top[0];
+        part[1][warp] = top[1];
+    }
+    __syncthreads();
+    float g2 = 0.f, u2 = 0.f;
+    nan = false;
+#pragma unroll
+    for (int i = 0; i < 8; i++) {
+        nan |= part[0][i] != part[0][i];
+        g2 = fmaxf(g2, part[0][i]);
+        u2 = fmaxf(u2, part[1][i]);
+    }
+    float p = sqrtf(g2) * sqrtf(u2);
+    const int b = p > 0.f && p < INFINITY && !nan ? max(-64, min(64, (int)(__float_as_uint(p) >> 23) - 127)) : 0;
+    const float down = __uint_as_float((uint32_t)(127 - b) << 23), lift = __uint_as_float((uint32_t)(127 + b) << 23);
+    p *= down;
+    if (threadIdx.x == 0 && !nan) atomicMax(reinterpret_cast<unsigned *>(bound2 + set * 2), __float_as_uint(p * p));   // not negative: bits in the order of the values
+    if (threadIdx.x == 0 && block == 0) bound2[set * 2 + 1] = 1.f;
+    for (int k = threadIdx.x; k < kb; k += 256) {
+        su[k] *= down;
+        sd[(size_t)k * fb] *= lift;
+    }
 }
 
 // ------------------------------------------------------------------ router logits, tokens as fp16
@@ -1122,11 +1163,9 @@ extern "C" int pf_moe_pack(const pf_moe_t *m, const void *d_gate, const void *d_
     moe_pack_kernel<true><<<grid, 256, 0, st>>>(*m, a.n_sets, a.f_tiles, a.ks_up, a.ks_down, a.set_bytes, a.down_at, (const uint8_t *)d_gate,
                                                 (const uint8_t *)d_up, (const uint8_t *)d_down, (uint8_t *)d_packed);
     PF_CUDA_TRY(cudaGetLastError(), "moe_pack_kernel launch");
-    const long long warps = (long long)n * m->F * 2;
-    if ((warps + 7) / 8 >= (1ll << 31)) return PF_ERANGE;
-    moe_row_norm_kernel<<<(unsigned)((warps + 7) / 8), 256, 0, st>>>(*m, a.n_sets, (const uint8_t *)d_gate, (const uint8_t *)d_up, d_gate_scale, d_up_scale,
-                                                                     (float *)a.row_max);
-    PF_CUDA_TRY(cudaGetLastError(), "moe_row_norm_kernel launch");
+    moe_block_norm_kernel<<<(unsigned)(n * ((m->F + 127) / 128)), 256, 0, st>>>(*m, (const uint8_t *)d_gate, (const uint8_t *)d_up, a.gs, (float *)a.us,
+                                                                                (float *)a.ds, (float *)a.row_max);
+    PF_CUDA_TRY(cudaGetLastError(), "moe_block_norm_kernel launch");
     count_launch();
     count_launch();
     return PF_OK;
