@@ -3,13 +3,14 @@
  *
  * The serving model of planfront.h prices a decode step as, per layer, max(compute, HBM) of the attention (its
  * weights and the cached keys and values of the running sequences) and of the experts (the weights of those that a
- * token chose), at efficiencies the caller measured.  These are the kernels whose time it prices, for a caller who
- * calibrates the tables on this GPU or checks a ranked plan with the layer itself:
+ * token chose), at efficiencies the caller measured.  Here are the two kernels whose time it prices, and what stands
+ * around them in a layer, for a caller who wants the HBM rate that they reach on this GPU or checks a ranked plan with
+ * the layer itself:
  *
+ *   pf_decode_attention   one query token per sequence against an 8-bit paged cache           (priced)
+ *   pf_moe_forward        router, routed and shared experts of a few tokens                   (priced)
  *   pf_add_rms_norm       residual addition, root-mean-square norm, output in 8 bits with scales
- *   pf_kv_append          new keys and values into an 8-bit paged cache, one scale per page and head
- *   pf_decode_attention   one query token per sequence against that cache
- *   pf_moe_forward        router, routed and shared experts of a few tokens
+ *   pf_kv_append          new keys and values into the cache, one scale per page and head
  *
  * Conventions are those of planfront.h: int32 status codes, "d_" pointers are device memory owned by the caller, the
  * library allocates nothing, all work is enqueued on `stream` and nothing synchronizes.  Every pointer must belong
@@ -39,7 +40,8 @@ enum { PF_DT_BF16 = 0, PF_DT_F16 = 1, PF_DT_F32 = 2, PF_DT_E4M3 = 3 };
  * elements; d_q: [rows, H] contiguous; d_scale: [rows, ceil(H / 128)] or [rows].
  *   d_residual NULL: a = x.  d_weight NULL: 1.  d_sum (a, rounded to dtype), d_y (y, rounded) and the pair d_q /
  *   d_scale may each be NULL.  d_sum may be d_residual or d_x themselves (with the same stride), no other overlap.
- * A NaN or an infinity makes its own row's y and q NaN or zero and no other's.
+ * A NaN or an infinity makes its own row's y and q NaN or zero and no other's.  The mean square is fp32: a row whose
+ * squares add up to more than 2^128 gives y = 0.
  * Any alignment is taken; pointers and strides that are multiples of 16 bytes are read 16 bytes at a time.
  * PF_EINVAL: a NULL d_x, no output at all, d_q without d_scale, another dtype or group, eps < 0 or not finite, a
  * stride below H; PF_ERANGE: H outside 1 .. PF_NORM_MAX_H, rows < 0 or >= 2^31.  rows = 0 does nothing. */
@@ -79,6 +81,8 @@ int pf_kv_append(const pf_kv_cache_t *cache, int32_t dtype, int32_t n_seq, int64
  * read, so what lies there may be NaN.  Tokens on a page outside the cache, or past the table's columns, are left out.
  * A query element that is not finite makes its own head's out and lse NaN (0 and -infinity where all its scores are
  * -infinity) and no other's.
+ * Keys and values are exact, scores, maxima and sums fp32; a token's weight enters the values' sum with 11 bits (fewer below 2^-29 of
+ * the row's largest, none below 2^-40; a page's value scale counts with the weight there), and the denominator with all of them.
  * Scales in the cache have to be positive and finite (below 2^-60 a value scale counts as 2^-60).
  * Several query tokens of one sequence are several rows with the same table row and their own lengths.
  * PF_EINVAL: NULL or misaligned pointers, another dtype, page or hd, n_heads not a multiple of n_kv, sm_scale not
@@ -96,7 +100,10 @@ int pf_decode_attention(const pf_kv_cache_t *cache, int32_t dtype, int32_t n_seq
  *   logits = x . router^T;  a token's top_k experts are those of the largest logits (ties: the lowest index; a NaN
  *   counts as -infinity);  w = softmax over the chosen logits;
  *   out = sum over the token's chosen local experts of w * down(silu(gate . x) * (up . x)), plus the shared experts.
- * A token none of whose experts is local, on a GPU without shared experts, gives zeros. */
+ * A token none of whose experts is local, on a GPU without shared experts, gives zeros.
+ * All sums are fp32.  bf16 weights: tokens as they are, the products' inner activations with 16 bits (two bf16 numbers).  e4m3
+ * weights: tokens and inner activations with 11 bits (fp16 times a power of two a row; inner activations also lose what is below
+ * 2^-37 |x|^2 times the product of the largest gate and up row norms of their block of 128). */
 typedef struct {
     int32_t H, F;                 /* model width (multiple of 16) and expert width (any) */
     int32_t n_experts, first, n_local, n_shared, top_k;

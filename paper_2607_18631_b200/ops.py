@@ -1,7 +1,8 @@
 """The operators of one decode layer (include/planfront_ops.h): argument marshalling only.
 
-What the serving model prices per layer and step -- the norm in front of it, attention over the cached keys and
-values, the experts of a few tokens -- as hand-written CUDA on the current device.  Function names mirror the C ABI.
+What the serving model prices per layer and step -- attention over the cached keys and values, the experts of a few
+tokens -- and the norm and the cache append that go with it, as hand-written CUDA on the current device.  Function names
+mirror the C ABI.
 Tensors stay with the caller; outputs and workspaces that are not passed in come from PyTorch's allocator, on the
 stream the call runs on (`stream`, or the current one).  There is no CPU path.
 
