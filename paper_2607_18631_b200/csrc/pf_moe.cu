@@ -1205,8 +1205,10 @@ extern "C" int pf_moe_forward(const pf_moe_t *m, int32_t T, const void *d_x, int
     cudaStream_t st = (cudaStream_t)stream;
     // Tokens an item takes at most: 8 (a column block of the matrix instruction) where no expert can have more, then 16, and 32 with more
     // than 8 an expert on average: a stage's token rows take room from the ring, and an expert with more tokens than an item is read again,
-    // mostly from the L2.  Measured with 16 and 32 (us): 24 tokens, 6 + 2 of 64 experts, e4m3, 4096 x 1408: 213, 238; 64 tokens: 262, 260; 128
-    // tokens, 8 of 256, 32 here: 335, 334.
+    // mostly from the L2.  Measured with 16 and 32 (us) on either side of the rule's border.  6 + 2 of 64 experts, 4096 x 1408, border at 85 tokens: e4m3
+    // 24 tokens 216, 224; 64: 264, 265; 96: 310, 308; 256: 619, 519; bf16 24: 341, 347; 256: 850, 658.  8 + 1 of 256, 32 here, 7168 x 2048, border
+    // 256: e4m3 32: 200, 222; 128: 328, 328; 256: 445, 433.  8 + 1 of 128, 32 here, 5120 x 1536, border 128: e4m3 32: 152, 157; 192: 277, 259.  2 of
+    // 8, 1024 x 2816, border 32: e4m3 24: 39, 37; 48: 48, 45; 64: 55, 55; 256: 116, 113; bf16 64: 63, 76, the one place where it costs; 192: 116, 103.
     if (T <= 8) return e4m3 ? moe_launch<true, 8, 5>(a, device, sms, st) : moe_launch<false, 8, 5>(a, device, sms, st);
     if ((long long)T * m->top_k <= 8ll * m->n_experts)
         return e4m3 ? moe_launch<true, 16, 5>(a, device, sms, st) : moe_launch<false, 16, 4>(a, device, sms, st);

@@ -9,7 +9,7 @@
 // rows a block goes through several and has the next one's loads in flight while it reduces and stores.
 // 8192 rows of 7168, bf16, residual, all outputs (530 MB): 92 us, 0.88 of the copy rate, with one block of 1024 threads an SM and a run a thread;
 // (before the divisions were replaced by products: 96; 110 with two blocks of 512 and two runs, 119 with a row a block of 256:
-// more rows under way at once mix reads and writes worse).  The schedulers issue in 70 % of the cycles.
+// more rows under way at once mix reads and writes worse).  The schedulers issue in 64 % of the cycles.
 #include <math.h>
 
 #include "pf_ops.cuh"
@@ -230,7 +230,7 @@ template <typename T, bool ALIGNED>
 static void norm_launch(const NormArgs &a, int sms, cudaStream_t st)
 {
     constexpr int W = sizeof(T) == 4 ? 1 : 2;      // fp32 rows take twice the registers
-    // up to a row an SM: the most threads for each (1 x 7168: 2.5 us)
+    // up to a row an SM: the most threads for each (1 x 7168: 2.9 us)
     if (a.rows <= sms && a.H > 2048) {
         if (a.H <= 8192) norm_run<T, 1024, 1, ALIGNED, 1>(a, sms, st);
         else norm_run<T, 1024, 2, ALIGNED, 1>(a, sms, st);
@@ -239,7 +239,10 @@ static void norm_launch(const NormArgs &a, int sms, cudaStream_t st)
     if (a.H <= 1024) norm_run<T, 128, 1, ALIGNED, 8>(a, sms, st);
     else if (a.H <= 2048) norm_run<T, 256, 1, ALIGNED, 4>(a, sms, st);
     else if (a.H <= 4096) norm_run<T, 512, 1, ALIGNED, 2>(a, sms, st);
-    else if (a.H <= 8192 && a.rows <= 4 * sms) norm_run<T, 512, 2, ALIGNED, W>(a, sms, st);      // 509 x 5120: 8.0 us, 8.6 with 1024 threads
+    // 512 threads and two runs a thread against 1024 and one, us at 148 SMs.  16-bit types (two blocks of 512 an SM): 149 x 5120 4.2, 4.7 and 200 x
+    // 5120 4.5, 4.9 with a scale a row, 149 x 7168 4.5, 4.6 and 200 x 7168 4.9, 4.8 with a scale a group; 296 x 7168 5.6, 4.9; 592 x 5120
+    // 8.4, 7.1; 2000 x 7168 32, 24.  fp32 (one block): 149 x 7168 6.4, 6.9; 592 x 7168 13.1, 13.6; 1184 x 7168 27.8, 24.9.
+    else if (a.H <= 8192 && 2 * a.rows <= (sizeof(T) == 4 ? 8 : 3) * sms) norm_run<T, 512, 2, ALIGNED, W>(a, sms, st);
     else if (a.H <= 8192) norm_run<T, 1024, 1, ALIGNED, 1>(a, sms, st);
     else norm_run<T, 1024, 2, ALIGNED, 1>(a, sms, st);
 }
