@@ -74,11 +74,9 @@ def _refuse(what: str):
     raise PlanfrontError(PF_EINVAL, what)
 
 
-def _counts(what, *values):
-    """Counts that have to fit the C call's 32-bit arguments: ctypes would cut them off without a word."""
-    for v in values:
-        if not -(1 << 31) <= v < 1 << 31:
-            raise PlanfrontError(PF_ERANGE, f"{what}: {v} does not fit 32 bits")
+def _cut_off(what):
+    """For counts that do not fit the C call's 32-bit arguments: ctypes would cut them off without a word."""
+    raise PlanfrontError(PF_ERANGE, f"{what}: a count does not fit 32 bits")
 
 
 def _on_device(torch, what, *tensors):
@@ -150,7 +148,8 @@ def pf_add_rms_norm(x, residual=None, weight=None, *, eps: float = 1e-6, group: 
     if x.dim() != 2:
         _refuse(f"{what}: x has to be [rows, H]")
     rows, H = shape = x.shape
-    _counts(what, H, group)
+    if group >> 31 or H >> 31:
+        _cut_off(what)
     if H < 1:
         raise PlanfrontError(PF_ERANGE, f"{what}: rows without elements")
     if weight is not None and (weight.dtype != x.dtype or weight.shape != (H,) or not weight.is_contiguous()):
@@ -221,9 +220,10 @@ def pf_kv_append(k_cache, v_cache, k_scale, v_scale, k, v, cu_new, lengths, tabl
     if dt is None or v.dtype != k.dtype or v.shape != k.shape:
         _refuse(f"{what}: k and v have the same shape and type (bf16 or fp16)")
     n_seq = lengths.shape[0]
-    _counts(what, n_seq, max_new, *table.shape)
     if cu_new.shape != (n_seq + 1,) or table.dim() != 2 or table.shape[0] != n_seq:
         _refuse(f"{what}: cu_new is [sequences + 1], table [sequences, columns]")
+    if (n_seq | max_new | table.shape[1]) >> 31:
+        _cut_off(what)
     if stream is not None:
         _used_on(stream, k_cache, v_cache, k_scale, v_scale, k, v, cu_new, lengths, table)
     status = L.pf_kv_append(c, dt, n_seq, k.shape[0], max_new, k.data_ptr(), _heads(k, what, c.n_kv, c.hd), v.data_ptr(), _heads(v, what, c.n_kv, c.hd),
@@ -253,10 +253,11 @@ def pf_decode_attention(q, k_cache, v_cache, k_scale, v_scale, lengths, table, *
     if dt is None or len(shape) != 3:
         _refuse(f"{what}: q has to be [sequences, heads, head_dim] of bf16 or fp16")
     n_seq, heads, _ = shape
-    _counts(what, n_seq, heads, *table.shape)
     hd = c.hd
     if lengths.shape != (n_seq,) or table.dim() != 2 or table.shape[0] != n_seq:
         _refuse(f"{what}: lengths is [sequences], table [sequences, columns]")
+    if (n_seq | heads | table.shape[1]) >> 31:
+        _cut_off(what)
     res = {}
     if out is None:
         out = _like(torch, q)
@@ -316,7 +317,8 @@ class MoeLayer:
                 _refuse(f"{what}: block scales come with float8 weights, and only with them")
             if t is not None and (t.dtype != torch.float32 or t.shape != shape or not t.is_contiguous()):
                 _refuse(f"{what}: expected contiguous fp32 block scales of shape {shape}")
-        _counts(what, H, F, E, n, first_expert, n_shared, top_k)
+        if any(v >> 31 for v in (H, F, E, n, first_expert, n_shared, top_k)):
+            _cut_off(what)
         self.m = PfMoe(H, F, E, first_expert, n - n_shared, n_shared, top_k, wtype)
         size = L.pf_moe_packed_bytes(self.m)
         if size == 0:
