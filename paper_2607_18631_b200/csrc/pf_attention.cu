@@ -17,7 +17,7 @@
 // are the rows.  So with up to 8 heads a key head, and with one, no more than the unused columns is computed in vain (heads as rows: twice
 // the products, accumulators and exponentials, 62 us instead of 53 for one sequence of 131071 tokens, 8 key and 64 query heads of 128).
 // Measured (one B200, device time of both kernels): that sequence (269 MB) 57 us, of which the copies alone take 45; 48 ragged sequences up to 8192
-// tokens, 32 / 8 heads (418 MB) 86 us, copies alone 68; 777 tokens, 16 heads of 64: 9.7 us.
+// tokens, 32 / 8 heads (418 MB) 86 us, copies alone 68; 64 / 4 heads (209 MB) 71 us; 777 tokens, 16 heads of 64: 9.6 us.
 // Bytes are widened to fp16, which is exact; queries are scaled by a power of two a head into fp16's range.  Scores, maxima and
 // sums are fp32.
 // The value scale joins the exponent: with p_t = exp2(s_t + log2 vs - z), the values' sum is plain and the denominator

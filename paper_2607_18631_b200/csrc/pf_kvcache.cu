@@ -7,8 +7,8 @@
 // 2^-n, which loses nothing but what underflows e4m3, so the cache does not depend on how a sequence was cut into calls
 // beyond that.  A unit is worked on by R rows of HD / 8 lanes, a lane holding 8 neighbouring elements (one 16-byte load,
 // one 8-byte store): R = 1 for single tokens (16 to 32 units a block), R = 128 / (HD / 8) for prompts (a unit a block).  The values are
-// read twice, the second time from the caches: keeping them in registers cost more blocks than it saved (27.6 us instead of 20.6 for 6 prompts of up to
-// 4096 tokens, 94 MB).  256 single tokens of 32 heads of 128: 5.9 us, a chain of four dependent reads.
+// read twice, the second time from the caches: keeping them in registers cost more blocks than it saved (27.6 us instead of 21.1 for 6 prompts of up to
+// 4096 tokens, 94 MB).  256 single tokens of 32 heads of 128: 6.2 us, a chain of four reads.
 #include "pf_ops.cuh"
 
 namespace pf {

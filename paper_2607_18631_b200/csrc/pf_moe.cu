@@ -27,7 +27,7 @@
 // The legacy matrix instruction is enough: at full HBM speed a scheduler gets a 2 KB slice every 333 cycles, and its products take 70 for up to
 // 8 tokens an expert.  Beyond 16 tokens an expert the reads of token rows from shared memory (4 per product) bound the kernel.
 // Measured (one B200, device time): 1 token, bf16, 6 + 2 of 64 experts of 4096 x 1408 (277 MB): 66 us; 16 tokens, e4m3, 8 of 128, 32 here, 5120 x
-// 1536 (511 MB): 121 us; 128 tokens, e4m3, 8 of 256, 32 here, 7168 x 2048 (1436 MB): 334 us.  Of the 66 us the streams of the two products take 44
+// 1536 (511 MB): 122 us; 128 tokens, e4m3, 8 of 256, 32 here, 7168 x 2048 (1436 MB): 337 us.  Of the 66 us the streams of the two products take 44
 // (6.3 TB/s), the router's kernel 5, the choice and the sorting of pairs 5, the meetings 8.
 #include <atomic>
 #include <type_traits>
