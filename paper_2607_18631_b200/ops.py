@@ -89,11 +89,16 @@ def _on_device(torch, what, *tensors):
 
 
 def _stream(torch, dev, stream):
-    return stream.cuda_stream if stream is not None else torch._C._cuda_getCurrentRawStream(dev)
+    if stream is None:
+        return torch._C._cuda_getCurrentRawStream(dev)
+    if stream.device_index != dev:
+        _refuse(f"the stream belongs to cuda:{stream.device_index}, the current device is cuda:{dev}")
+    return stream.cuda_stream
 
 
-def _used_on(stream, *tensors):
-    """The allocator is not to hand these tensors' memory out again before the work now enqueued on `stream` is done."""
+def _used_on(torch, stream, *tensors):
+    """A stream of the current device; the allocator is not to hand these tensors' memory out again before the work now enqueued there is done."""
+    _stream(torch, torch._C._cuda_getDevice(), stream)
     for t in tensors:
         if t is not None:
             t.record_stream(stream)
@@ -137,8 +142,8 @@ def pf_add_rms_norm(x, residual=None, weight=None, *, eps: float = 1e-6, group: 
     unless q=False."""
     L, torch = _ready or _lib()
     if stream is not None:      # the caching allocator hands memory out per stream
+        _used_on(torch, stream, x, residual, weight, sum_out)
         with torch.cuda.stream(stream):
-            _used_on(stream, x, residual, weight, sum_out)
             return pf_add_rms_norm(x, residual, weight, eps=eps, group=group, y=y, q=q, sum_out=sum_out)
     what = "pf_add_rms_norm"
     dev = _on_device(torch, what, x, residual, weight, sum_out)
@@ -225,7 +230,7 @@ def pf_kv_append(k_cache, v_cache, k_scale, v_scale, k, v, cu_new, lengths, tabl
     if (n_seq | max_new | table.shape[1]) >> 31:
         _cut_off(what)
     if stream is not None:
-        _used_on(stream, k_cache, v_cache, k_scale, v_scale, k, v, cu_new, lengths, table)
+        _used_on(torch, stream, k_cache, v_cache, k_scale, v_scale, k, v, cu_new, lengths, table)
     status = L.pf_kv_append(c, dt, n_seq, k.shape[0], max_new, k.data_ptr(), _heads(k, what, c.n_kv, c.hd), v.data_ptr(), _heads(v, what, c.n_kv, c.hd),
                             _int32(torch, what, cu_new, 1), _int32(torch, what, lengths, 1), _int32(torch, what, table, 2), table.shape[1],
                             _stream(torch, dev, stream))
@@ -242,8 +247,8 @@ def pf_decode_attention(q, k_cache, v_cache, k_scale, v_scale, lengths, table, *
     zeros and -inf."""
     L, torch = _ready or _lib()
     if stream is not None:
+        _used_on(torch, stream, q, k_cache, v_cache, k_scale, v_scale, lengths, table, out, workspace)
         with torch.cuda.stream(stream):
-            _used_on(stream, q, k_cache, v_cache, k_scale, v_scale, lengths, table, out, workspace)
             return pf_decode_attention(q, k_cache, v_cache, k_scale, v_scale, lengths, table, sm_scale=sm_scale, lse=lse, out=out, workspace=workspace)
     what = "pf_decode_attention"
     dev = _on_device(torch, what, q, k_cache, v_cache, k_scale, v_scale, lengths, table, out, workspace)
@@ -326,10 +331,9 @@ class MoeLayer:
         self._L, self._torch, self._dev = L, torch, dev
         self.router = router
         if stream is not None:
+            _used_on(torch, stream, gate, up, down, gate_scale, up_scale, down_scale)
             stream.wait_stream(torch.cuda.current_stream())
         with contextlib.nullcontext() if stream is None else torch.cuda.stream(stream):
-            if stream is not None:
-                _used_on(stream, gate, up, down, gate_scale, up_scale, down_scale)
             self.packed = torch.empty(size, dtype=torch.uint8, device=router.device)
             self._home = _stream(torch, dev, None)         # the packing's stream
             _check(L.pf_moe_pack(self.m, gate.data_ptr(), up.data_ptr(), down.data_ptr(), _ptr(gate_scale), _ptr(up_scale), _ptr(down_scale),
@@ -342,7 +346,7 @@ class MoeLayer:
         used there."""
         torch = self._torch
         stream = torch.cuda.current_stream()
-        _used_on(stream, self.packed, self.router)
+        _used_on(torch, stream, self.packed, self.router)
         if not torch.cuda.is_current_stream_capturing():
             stream.wait_event(self._pack_done)
             self._visited.add(raw)
@@ -354,8 +358,8 @@ class MoeLayer:
         without it."""
         L, torch, m = self._L, self._torch, self.m
         if stream is not None:
+            _used_on(torch, stream, x, xq, xq_scale, out, status, workspace)
             with torch.cuda.stream(stream):
-                _used_on(stream, x, xq, xq_scale, out, status, workspace)
                 return self.forward(x, xq, xq_scale, out=out, status=status, workspace=workspace)
         what = "pf_moe_forward"
         dev = _on_device(torch, what, x, xq, xq_scale, out, status, workspace, self.packed)

@@ -65,3 +65,20 @@ def test_counts_that_do_not_fit_32_bits_are_refused():
     w = [torch.randn(*s, device="cuda").to(torch.bfloat16) for s in ((8, 128), (8, 32, 128), (8, 32, 128), (8, 128, 32))]
     for kw in (dict(top_k=big + 2), dict(top_k=2, first_expert=big), dict(top_k=2, n_shared=-big)):
         refused(lambda: ops.MoeLayer(*w, **kw))
+
+
+def test_a_stream_of_another_device_is_refused():
+    import torch
+    from paper_2607_18631_b200 import ops
+
+    class Elsewhere:
+        device_index, cuda_stream = torch.cuda.current_device() + 1, 0
+    layer, x = moe_layer()
+    d = lambda *x: torch.tensor(x, dtype=torch.int32, device="cuda")  # noqa: E731
+    cache = [torch.zeros(4, 2, 16, 64, device="cuda").to(torch.float8_e4m3fn) for _ in range(2)] + [torch.ones(4, 2, device="cuda") for _ in range(2)]
+    k, table = torch.randn(3, 2, 64, device="cuda").to(torch.bfloat16), d(0, 1).reshape(1, 2)
+    w = [torch.randn(*s, device="cuda").to(torch.bfloat16) for s in ((8, 128), (8, 32, 128), (8, 32, 128), (8, 128, 32))]
+    for call in (lambda: ops.pf_add_rms_norm(x, stream=Elsewhere()), lambda: ops.pf_kv_append(*cache, k, k, d(0, 3), d(0), table, max_new=3, stream=Elsewhere()),
+                 lambda: ops.pf_decode_attention(k[:1], *cache, d(3), table, stream=Elsewhere()), lambda: layer.forward(x, stream=Elsewhere()),
+                 lambda: ops.MoeLayer(*w, top_k=2, stream=Elsewhere())):
+        refused(call)
