@@ -11,6 +11,9 @@
  *   pf_moe_forward        router, routed and shared experts of a few tokens                   (priced)
  *   pf_add_rms_norm       residual addition, root-mean-square norm, output in 8 bits with scales
  *   pf_kv_append          new keys and values into the cache, one scale per page and head
+ *   pf_rope               rotary positions of query or key heads, and their gradient
+ *   pf_kv_append_rope     the append with the rotation on the way
+ *   pf_prefix_attention   pf_decode_attention for sequences that share long prefixes
  *
  * Conventions are those of planfront.h: int32 status codes, "d_" pointers are device memory owned by the caller, the
  * library allocates nothing, all work is enqueued on `stream` and nothing synchronizes.  Every pointer must belong
@@ -94,6 +97,58 @@ int pf_decode_attention(const pf_kv_cache_t *cache, int32_t dtype, int32_t n_seq
                         int64_t q_stride, const int32_t *d_len, const int32_t *d_table, int32_t table_cols, float sm_scale,
                         void *d_out, int64_t out_stride, float *d_lse, void *d_workspace, size_t workspace_bytes,
                         void *stream);
+
+/* Rotary positions.  Pair i of a head's first `rot` elements, i < rot / 2, at position p becomes
+ *   (a, b) -> amplitude * (a cos t - b sin t, b cos t + a sin t),   t = p * freq[i] radians;
+ * pair i is elements i and i + rot / 2 (PF_ROPE_HALF) or 2 i and 2 i + 1 (PF_ROPE_INTERLEAVED); elements from `rot` on stay as they are.
+ * d_phase: rot / 2 words, freq[i] as a fraction of a turn times 2^64 (pf_rotary_phases), so that angles are exact to 2^-32 turns at every
+ * 32-bit position, negative ones included.  An element that is not finite spoils its own pair only. */
+enum { PF_ROPE_HALF = 0, PF_ROPE_INTERLEAVED = 1 };
+#define PF_ROPE_MAX_HD 1024
+#define PF_ROPE_MAX_HEADS 65535
+typedef struct {
+    int32_t rot, layout;      /* rot: even, 0 .. hd */
+    float amplitude;          /* finite; 1 but for some long-context scalings */
+    const uint64_t *d_phase;
+} pf_rotary_t;
+/* Host: phase[i] = round(frac(freq[i] / (2 pi)) * 2^64), i < n.  PF_EINVAL: NULL, a frequency that is not finite; PF_ERANGE: n < 0. */
+int pf_rotary_phases(int32_t n, const double *freq, uint64_t *phase);
+
+/* y[t, h] = rotation of x[t, h] to position d_pos[t], or, where `transposed` is not 0, the transposed matrix times x[t, h]: the gradient with
+ * respect to x, given the gradient with respect to y.  Heads of hd contiguous elements of `dtype` (PF_DT_BF16, F16, F32; 32-bit arithmetic, rounded once); strides of a token
+ * and of a head in elements, in either order.  d_y may be d_x with the same strides, no other overlap.  Any alignment is taken; with hd and rot
+ * multiples of 16, and pointers and strides multiples of 16 bytes, 16 bytes are moved at a time.
+ * PF_EINVAL: NULL or misaligned pointers, another dtype or layout, rot odd or above hd, heads or tokens that overlap; PF_ERANGE: counts out of
+ * range.  tokens = 0 or heads = 0 does nothing. */
+int pf_rope(const pf_rotary_t *rotary, int32_t transposed, int32_t dtype, int64_t tokens, int32_t heads, int32_t hd, const void *d_x, int64_t x_token,
+            int64_t x_head, const int32_t *d_pos, void *d_y, int64_t y_token, int64_t y_head, void *stream);
+
+/* pf_kv_append with keys rotated on the way: from `dtype` to 32 bits, rotated, and rounded once, to e4m3; scales are chosen over the rotated
+ * keys.  The queries of the same tokens, n_heads heads a row of d_q, are rotated into d_q_out (d_q itself, with the same stride, allowed; n_heads = 0: none).
+ * Token j of sequence b has position d_pos[d_cu_new[b] + j] or, where d_pos is NULL, d_len[b] + j; its place in the cache is d_len[b] + j
+ * either way.  A query row is written if its token is one of the first max_new of a sequence, whether or not the table has a place for its key;
+ * other rows of d_q_out are left as they were.  rotary->rot is a multiple of 16.  d_cu_new does not decrease.
+ * Otherwise as pf_kv_append, which see. */
+int pf_kv_append_rope(const pf_kv_cache_t *cache, const pf_rotary_t *rotary, int32_t dtype, int32_t n_seq, int64_t n_new, int32_t max_new,
+                      int32_t n_heads, const void *d_q, int64_t q_stride, void *d_q_out, int64_t q_out_stride, const void *d_k, int64_t k_stride,
+                      const void *d_v, int64_t v_stride, const int32_t *d_cu_new, const int32_t *d_len, const int32_t *d_table,
+                      int32_t table_cols, const int32_t *d_pos, void *stream);
+
+/* Single-token attention of sequences that share prefixes: sequences d_cu_seqs[g] .. d_cu_seqs[g + 1] - 1 see, in front of their own d_len[b]
+ * cached tokens (table row b), the d_prefix_len[g] tokens on the pages of prefix table row g.  A prefix is read once for all rows of its group that fit a
+ * tile of 256 (sequences times query heads of a key head), not once a sequence.
+ *   out[b, h] = softmax over both of sm_scale * q[b, h] . K[t], times V[t]
+ * d_cu_seqs: n_groups + 1 offsets that do not decrease (NULL, with one group: all sequences); a sequence in no group sees its own tokens only.  Prefixes of any length, and tables, lengths,
+ * missing pages, scales, q, out and lse otherwise as in pf_decode_attention.  A row that sees no token gives zeros and -infinity.
+ * A prefix token's weight enters the values' sum with 11 bits (fewer below 2^-21 of the row's largest, none below 2^-32).
+ * A wait inside the kernel that runs out makes the rows that it concerns NaN.
+ * PF_EINVAL, PF_ERANGE (also: n_groups above PF_PREFIX_MAX_GROUPS), PF_EWORKSPACE as there.  n_groups = 0: no sequence has a prefix. */
+#define PF_PREFIX_MAX_GROUPS 1024
+size_t pf_prefix_attention_workspace(const pf_kv_cache_t *cache, int32_t n_seq, int32_t n_heads, int32_t n_groups, int32_t prefix_cols);
+int pf_prefix_attention(const pf_kv_cache_t *cache, int32_t dtype, int32_t n_seq, int32_t n_heads, const void *d_q, int64_t q_stride,
+                        const int32_t *d_len, const int32_t *d_table, int32_t table_cols, int32_t n_groups, const int32_t *d_cu_seqs,
+                        const int32_t *d_prefix_len, const int32_t *d_prefix_table, int32_t prefix_cols, float sm_scale, void *d_out,
+                        int64_t out_stride, float *d_lse, void *d_workspace, size_t workspace_bytes, void *stream);
 
 /* One mixture-of-experts layer as this GPU holds it: experts [first, first + n_local) of n_experts, and n_shared
  * experts that every token takes with weight 1 (indices n_local .. n_local + n_shared - 1 of the weight tensors).

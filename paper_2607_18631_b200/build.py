@@ -9,7 +9,7 @@ CSRC = os.path.join(HERE, "csrc")
 INCLUDE = os.path.join(os.path.dirname(HERE), "include")
 LIB = os.path.join(HERE, "libplanfront.so")
 SOURCES = ["pf_api.cu", "pf_score.cu", "pf_select.cu", "pf_simulate.cu", "pf_search.cu", "pf_aggregate.cu", "pf_report.cu", "pf_compact.cu",
-           "pf_norm.cu", "pf_kvcache.cu", "pf_attention.cu", "pf_moe.cu"]
+           "pf_norm.cu", "pf_kvcache.cu", "pf_attention.cu", "pf_moe.cu", "pf_rope.cu", "pf_prefix.cu"]
 # the roofline probes of the benchmark: a library of their own, not part of the scoring ABI
 PROBE_LIB = os.path.join(HERE, "libplanfront_probe.so")
 # the same library with every device-side index range-checked (-DPF_BOUNDS_CHECK): for the checked test run
@@ -25,7 +25,7 @@ def _newest_source() -> float:
 def _compile(lib: str, sources, verbose: bool, defines=()) -> None:
     nvcc = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")
     cmd = [nvcc, "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
-           "-I" + INCLUDE, "-Xcompiler", "-fPIC", "-shared", "-o", lib]
+           "-I" + INCLUDE, "-Xcompiler", "-fPIC", "-shared", "--threads", "0", "-o", lib]
     cmd += ["-D" + d for d in defines]
     if verbose:
         cmd += ["-Xptxas", "-v"]

@@ -23,17 +23,6 @@ struct AppendArgs {
     int64_t units;    // n_seq * units_per_seq * n_kv * 2
 };
 
-// the exponent of the least power of two >= amax / 448, in [-100, 118]; amax >= 0, infinity included
-__device__ __forceinline__ int scale_exponent(float amax)
-{
-    if (!(amax > 0.f)) return -100;
-    const uint32_t b = __float_as_uint(amax);
-    // amax = 1.m * 2^(E - 127), 448 = 1.75 * 2^8; a subnormal amax reads E = 0 and lands below the floor either way
-    const int e = (int)(b >> 23) - 127 - 8 + ((b & 0x7FFFFFu) > 0x600000u ? 1 : 0);
-    return max(-100, min(118, e));
-}
-__device__ __forceinline__ float pow2f(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }   // -126 <= e <= 127
-
 template <typename T, int HD, int R>
 __global__ void __launch_bounds__(R == 1 ? 256 : 128) append_kernel(const AppendArgs A)
 {

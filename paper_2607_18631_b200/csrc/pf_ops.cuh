@@ -63,6 +63,18 @@ template <typename T> __device__ __forceinline__ uint32_t pair_of_f32(float a, f
 template <> __device__ __forceinline__ uint32_t pair_of_f32<Bf16>(float a, float b) { return bf16x2_of(a, b); }
 template <> __device__ __forceinline__ uint32_t pair_of_f32<F16>(float a, float b) { return f16x2_of(a, b); }
 
+// ------------------------------------------------------------------ the cache's scales
+// the exponent of the least power of two >= amax / 448, in [-100, 118]; amax >= 0, infinity included
+__device__ __forceinline__ int scale_exponent(float amax)
+{
+    if (!(amax > 0.f)) return -100;
+    const uint32_t b = __float_as_uint(amax);
+    // amax = 1.m * 2^(E - 127), 448 = 1.75 * 2^8; a subnormal amax reads E = 0 and lands below the floor either way
+    const int e = (int)(b >> 23) - 127 - 8 + ((b & 0x7FFFFFu) > 0x600000u ? 1 : 0);
+    return max(-100, min(118, e));
+}
+__device__ __forceinline__ float pow2f(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }   // -126 <= e <= 127
+
 // ------------------------------------------------------------------ asynchronous copies, global -> shared
 __device__ __forceinline__ uint32_t smem_addr(const void *p) { return (uint32_t)__cvta_generic_to_shared(p); }
 // 16 bytes, of which the first `bytes` (0 or 16) are read and the rest are zero; past L1

@@ -1,7 +1,7 @@
 """The operators of one decode layer (include/planfront_ops.h): argument marshalling only.
 
-What the serving model prices per layer and step -- attention over the cached keys and values, the experts of a few
-tokens -- and the norm and the cache append that go with it, as hand-written CUDA on the current device.  Function names
+What the serving model prices per layer and step -- attention over the cached keys and values, shared prefixes among them, the experts of a few
+tokens -- and the norm, the rotary positions and the cache append that go with it, as hand-written CUDA on the current device.  Function names
 mirror the C ABI.
 Tensors stay with the caller; outputs and workspaces that are not passed in come from PyTorch's allocator, on the
 stream the call runs on (`stream`, or the current one).  There is no CPU path.
@@ -20,7 +20,8 @@ import math
 from .binding import PF_EINVAL, PF_ERANGE, PF_OK, PlanfrontError, _check, _torch, i32, i64, load_library
 
 EXPORTS = ("pf_add_rms_norm", "pf_kv_append", "pf_decode_attention_workspace", "pf_decode_attention",
-           "pf_moe_packed_bytes", "pf_moe_pack", "pf_moe_workspace", "pf_moe_forward")
+           "pf_moe_packed_bytes", "pf_moe_pack", "pf_moe_workspace", "pf_moe_forward", "pf_rotary_phases", "pf_rope", "pf_kv_append_rope",
+           "pf_prefix_attention_workspace", "pf_prefix_attention")
 DT_BF16, DT_F16, DT_F32, DT_E4M3 = 0, 1, 2, 3
 SCALE_GROUP = 128
 MOE_MAX_TOKENS = 512
@@ -34,6 +35,10 @@ class PfKvCache(C.Structure):
 
 class PfMoe(C.Structure):
     _fields_ = [(n, i32) for n in ("H", "F", "n_experts", "first", "n_local", "n_shared", "top_k", "wtype")]
+
+
+class PfRotary(C.Structure):
+    _fields_ = [("rot", i32), ("layout", i32), ("amplitude", C.c_float), ("d_phase", _vp)]
 
 
 _ready = None
@@ -55,16 +60,20 @@ def _lib():
 
 def declare(L):
     """Declare the argument types of planfront_ops.h on a loaded library."""
-    cache, moe = C.POINTER(PfKvCache), C.POINTER(PfMoe)
+    cache, moe, rotary = C.POINTER(PfKvCache), C.POINTER(PfMoe), C.POINTER(PfRotary)
     f32 = C.c_float
     for name, args in (("pf_add_rms_norm", [i32, i64, i32, _vp, i64, _vp, i64, _vp, f32, i32, _vp, i64, _vp, i64, _vp, _vp, _vp]),
                        ("pf_kv_append", [cache, i32, i32, i64, i32, _vp, i64, _vp, i64, _vp, _vp, _vp, i32, _vp]),
                        ("pf_decode_attention", [cache, i32, i32, i32, _vp, i64, _vp, _vp, i32, f32, _vp, i64, _vp, _vp, _sz, _vp]),
                        ("pf_moe_pack", [moe] + [_vp] * 8),
+                       ("pf_rotary_phases", [i32, C.POINTER(C.c_double), C.POINTER(C.c_uint64)]),
+                       ("pf_rope", [rotary, i32, i32, i64, i32, i32, _vp, i64, i64, _vp, _vp, i64, i64, _vp]),
+                       ("pf_kv_append_rope", [cache, rotary, i32, i32, i64, i32, i32] + [_vp, i64] * 4 + [_vp, _vp, _vp, i32, _vp, _vp]),
+                       ("pf_prefix_attention", [cache, i32, i32, i32, _vp, i64, _vp, _vp, i32, i32, _vp, _vp, _vp, i32, f32, _vp, i64, _vp, _vp, _sz, _vp]),
                        ("pf_moe_forward", [moe, i32, _vp, i64] + [_vp] * 8 + [_vp, _sz, _vp])):
         fn = getattr(L, name)
         fn.restype, fn.argtypes = C.c_int, args
-    for name, args in (("pf_decode_attention_workspace", [cache, i32, i32]), ("pf_moe_packed_bytes", [moe]), ("pf_moe_workspace", [moe, i32])):
+    for name, args in (("pf_decode_attention_workspace", [cache, i32, i32]), ("pf_prefix_attention_workspace", [cache, i32, i32, i32, i32]), ("pf_moe_packed_bytes", [moe]), ("pf_moe_workspace", [moe, i32])):
         fn = getattr(L, name)
         fn.restype, fn.argtypes = _sz, args
     return L
@@ -287,6 +296,185 @@ def pf_decode_attention(q, k_cache, v_cache, k_scale, v_scale, lengths, table, *
     if status != PF_OK:
         _check(status, what)
     return res
+
+
+def pf_prefix_attention(q, k_cache, v_cache, k_scale, v_scale, lengths, table, prefix_lengths, prefix_table, cu_seqs=None, *, sm_scale: float | None = None,
+                        lse: bool = False, out=None, workspace=None, stream=None) -> dict:
+    """pf_decode_attention of sequences that share prefixes: sequences cu_seqs[g] .. cu_seqs[g + 1] - 1 (all, without cu_seqs) see the
+    prefix_lengths[g] tokens on the pages prefix_table[g] in front of their own lengths[b] tokens, and a prefix is read once for its group.
+
+    prefix_lengths: [groups], prefix_table: [groups, columns], cu_seqs: [groups + 1], int32, not decreasing; a sequence in no group sees its own tokens
+    only.  Everything else, and what comes back, as in pf_decode_attention."""
+    L, torch = _ready or _lib()
+    if stream is not None:
+        _used_on(torch, stream, q, k_cache, v_cache, k_scale, v_scale, lengths, table, prefix_lengths, prefix_table, cu_seqs, out, workspace)
+        with torch.cuda.stream(stream):
+            return pf_prefix_attention(q, k_cache, v_cache, k_scale, v_scale, lengths, table, prefix_lengths, prefix_table, cu_seqs, sm_scale=sm_scale, lse=lse,
+                                       out=out, workspace=workspace)
+    what = "pf_prefix_attention"
+    dev = _on_device(torch, what, q, k_cache, v_cache, k_scale, v_scale, lengths, table, prefix_lengths, prefix_table, cu_seqs, out, workspace)
+    c = _cache(torch, what, k_cache, v_cache, k_scale, v_scale)
+    dt = _dtypes.get(q.dtype)
+    shape = q.shape
+    if dt is None or len(shape) != 3:
+        _refuse(f"{what}: q has to be [sequences, heads, head_dim] of bf16 or fp16")
+    n_seq, heads, _ = shape
+    hd = c.hd
+    if lengths.shape != (n_seq,) or table.dim() != 2 or table.shape[0] != n_seq:
+        _refuse(f"{what}: lengths is [sequences], table [sequences, columns]")
+    n_groups = prefix_lengths.numel()
+    if prefix_lengths.shape != (n_groups,) or prefix_table.dim() != 2 or prefix_table.shape[0] != n_groups:
+        _refuse(f"{what}: prefix_lengths is [groups], prefix_table [groups, columns]")
+    if (cu_seqs is None and n_groups > 1) or (cu_seqs is not None and cu_seqs.shape != (n_groups + 1,)):
+        _refuse(f"{what}: cu_seqs is [groups + 1]; without it there is one group")
+    cols = prefix_table.shape[1]
+    if (n_seq | heads | table.shape[1] | n_groups | cols) >> 31:
+        _cut_off(what)
+    res = {}
+    if out is None:
+        out = _like(torch, q)
+    elif out.dtype != q.dtype or out.shape != shape:
+        _refuse(f"{what}: out has q's shape and type")
+    res["out"] = out
+    lse_ptr = None
+    if lse:
+        res["lse"] = t = _matrix(torch, n_seq, heads, torch.float32, q.device)
+        lse_ptr = t.data_ptr()
+    if workspace is None:
+        size = L.pf_prefix_attention_workspace(c, n_seq, heads, n_groups, cols)
+        workspace = torch.empty(size, dtype=torch.uint8, device=q.device)
+    else:
+        size = _work_bytes(workspace, what)
+    status = L.pf_prefix_attention(c, dt, n_seq, heads, q.data_ptr(), _heads(q, what, heads, hd), _int32(torch, what, lengths, 1), _int32(torch, what, table, 2),
+                                   table.shape[1], n_groups, None if cu_seqs is None else _int32(torch, what, cu_seqs, 1), _int32(torch, what, prefix_lengths, 1),
+                                   _int32(torch, what, prefix_table, 2), cols, 1.0 / math.sqrt(hd) if sm_scale is None else sm_scale, out.data_ptr(),
+                                   _heads(out, what, heads, hd), lse_ptr, workspace.data_ptr(), size, _stream(torch, dev, None))
+    if status != PF_OK:
+        _check(status, what)
+    return res
+
+
+class Rotary:
+    """Frequencies of rotary positions, laid out once on the current device.
+
+    Pair i of `rot` rotated elements turns by base^(-2 i / rot) radians a position, changed for contexts longer than the trained ones by `scaling`:
+    "linear": divided by `factor`; "base": base times factor^(rot / (rot - 2)); "parts": with r turns within `original`
+    positions, pairs of r >= high stay, pairs of r <= low are divided by `factor`, and in between the two are mixed linearly in r.  `frequencies`: rot / 2 numbers to use
+    instead.  layout: "half" (pairs i, i + rot / 2) or "interleaved" (pairs 2 i, 2 i + 1).  amplitude: factor of rotated elements."""
+
+    def __init__(self, rot: int, *, layout: str = "half", base: float = 10000.0, scaling: str = "none", factor: float = 1.0, original: int = 8192, low: float = 1.0,
+                 high: float = 32.0, amplitude: float = 1.0, frequencies=None):
+        L, torch = _ready or _lib()
+        self.frequencies = rotary_frequencies(rot, base=base, scaling=scaling, factor=factor, original=original, low=low, high=high) if frequencies is None else [float(f) for f in frequencies]
+        if layout not in ("half", "interleaved") or not math.isfinite(amplitude):
+            _refuse(f"Rotary: layout {layout!r}, amplitude {amplitude}")
+        if rot < 0 or rot % 2 or rot >> 31 or len(self.frequencies) != rot // 2:
+            _refuse(f"Rotary: {rot} rotated elements, {len(self.frequencies)} frequencies")
+        n = rot // 2
+        phase = (C.c_uint64 * n)()
+        _check(L.pf_rotary_phases(n, (C.c_double * n)(*self.frequencies), phase), "pf_rotary_phases")
+        self.rot, self.layout, self.amplitude = rot, layout, amplitude
+        self.phase = torch.tensor([p - (1 << 64) if p >> 63 else p for p in phase], dtype=torch.int64, device="cuda")      # waits for the copy
+        self.r = PfRotary(rot, int(layout == "interleaved"), amplitude, self.phase.data_ptr() if n else None)
+
+
+def rotary_frequencies(rot: int, *, base: float = 10000.0, scaling: str = "none", factor: float = 1.0, original: int = 8192, low: float = 1.0, high: float = 32.0) -> list:
+    """Radians a position of rot / 2 pairs; see Rotary."""
+    if rot < 0 or rot % 2 or not (base > 0 and math.isfinite(base) and factor > 0 and math.isfinite(factor)):
+        _refuse(f"Rotary: rot {rot}, base {base}, factor {factor}")
+    if scaling not in ("none", "linear", "base", "parts") or (scaling == "parts" and not low < high):
+        _refuse(f"Rotary: scaling {scaling!r}, low {low}, high {high}")
+    if scaling == "base" and rot > 2:
+        base *= factor ** (rot / (rot - 2))
+    f = [base ** (-2 * i / rot) for i in range(rot // 2)]
+    if scaling == "linear":
+        return [x / factor for x in f]
+    if scaling == "parts":
+        keep = [min(1.0, max(0.0, (original * x / (2 * math.pi) - low) / (high - low))) for x in f]
+        return [x * (k + (1 - k) / factor) for x, k in zip(f, keep)]
+    return f
+
+
+def _strided_heads(t, what):
+    """[tokens, heads, hd] with contiguous heads; returns the strides of a token and of a head."""
+    if t.dim() != 3 or (t.stride(2) != 1 and t.shape[2] > 1):
+        _refuse(f"{what}: expected [tokens, heads, head_dim] with contiguous heads, got shape {tuple(t.shape)}, strides {t.stride()}")
+    return t.stride(0), t.stride(1)
+
+
+def pf_rope(x, positions, rotary: Rotary, *, transposed: bool = False, out=None, stream=None):
+    """Heads rotated to their tokens' positions: [tokens, heads, head_dim] bf16, fp16 or fp32, heads contiguous, tokens and heads at any stride.
+
+    positions: [tokens] int32.  transposed: the transposed rotation, which takes the gradient with respect to the result to
+    that with respect to x.  out: like x (x itself allowed); returned."""
+    L, torch = _ready or _lib()
+    if stream is not None:
+        _used_on(torch, stream, x, positions, rotary.phase, out)
+        with torch.cuda.stream(stream):
+            return pf_rope(x, positions, rotary, transposed=transposed, out=out)
+    what = "pf_rope"
+    dev = _on_device(torch, what, x, positions, rotary.phase, out)
+    dt = _dtypes.get(x.dtype)
+    if dt is None or x.dim() != 3:
+        _refuse(f"{what}: x has to be [tokens, heads, head_dim] of bf16, fp16 or fp32")
+    tokens, heads, hd = shape = x.shape
+    if positions.shape != (tokens,):
+        _refuse(f"{what}: positions is [tokens]")
+    if (heads | hd) >> 31:
+        _cut_off(what)
+    if out is None:
+        out = _like(torch, x)
+    elif out.dtype != x.dtype or out.shape != shape:
+        _refuse(f"{what}: out has x's shape and type")
+    status = L.pf_rope(rotary.r, int(transposed), dt, tokens, heads, hd, x.data_ptr(), *_strided_heads(x, what), _int32(torch, what, positions, 1), out.data_ptr(),
+                       *_strided_heads(out, what), _stream(torch, dev, None))
+    if status != PF_OK:
+        _check(status, what)
+    return out
+
+
+def pf_kv_append_rope(k_cache, v_cache, k_scale, v_scale, q, k, v, cu_new, lengths, table, rotary: Rotary, *, max_new: int, positions=None, q_out=None, stream=None):
+    """pf_kv_append with the keys rotated on the way into the cache (rounded once, to 8 bits), and the queries of the same tokens rotated.
+
+    q: [new tokens, heads, head_dim] of k's type, or None; returned rotated (in q_out, where given; q itself allowed).  Rows of tokens that are in no sequence are left as
+    they were (of a new q_out: undefined).  positions: [new tokens] int32, or None: lengths[b] + j for token j of sequence b, as if nothing but the
+    sequence's own tokens came before it; behind a shared prefix, its length is to be added.  Everything else as in pf_kv_append."""
+    L, torch = _ready or _lib()
+    if stream is not None:
+        _used_on(torch, stream, k_cache, v_cache, k_scale, v_scale, q, k, v, cu_new, lengths, table, positions, q_out, rotary.phase)
+        with torch.cuda.stream(stream):
+            return pf_kv_append_rope(k_cache, v_cache, k_scale, v_scale, q, k, v, cu_new, lengths, table, rotary, max_new=max_new, positions=positions, q_out=q_out)
+    what = "pf_kv_append_rope"
+    dev = _on_device(torch, what, k_cache, v_cache, k_scale, v_scale, q, k, v, cu_new, lengths, table, positions, q_out, rotary.phase)
+    c = _cache(torch, what, k_cache, v_cache, k_scale, v_scale)
+    dt = _dtypes.get(k.dtype)
+    if dt is None or v.dtype != k.dtype or v.shape != k.shape:
+        _refuse(f"{what}: k and v have the same shape and type (bf16 or fp16)")
+    n_seq, n_new = lengths.shape[0], k.shape[0]
+    if cu_new.shape != (n_seq + 1,) or table.dim() != 2 or table.shape[0] != n_seq:
+        _refuse(f"{what}: cu_new is [sequences + 1], table [sequences, columns]")
+    if positions is not None and positions.shape != (n_new,):
+        _refuse(f"{what}: positions is [new tokens]")
+    heads, q_ptr, q_stride, o_ptr, o_stride = 0, None, 0, None, 0
+    if q is not None:
+        if q.dim() != 3 or q.dtype != k.dtype or q.shape[0] != n_new:
+            _refuse(f"{what}: q is [new tokens, heads, head_dim] of k's type")
+        heads = q.shape[1]
+        if q_out is None:
+            q_out = _like(torch, q)
+        elif q_out.dtype != q.dtype or q_out.shape != q.shape:
+            _refuse(f"{what}: q_out has q's shape and type")
+        q_ptr, q_stride, o_ptr, o_stride = q.data_ptr(), _heads(q, what, heads, c.hd), q_out.data_ptr(), _heads(q_out, what, heads, c.hd)
+    elif q_out is not None:
+        _refuse(f"{what}: q_out without q")
+    if (n_seq | max_new | table.shape[1] | heads) >> 31:
+        _cut_off(what)
+    status = L.pf_kv_append_rope(c, rotary.r, dt, n_seq, n_new, max_new, heads, q_ptr, q_stride, o_ptr, o_stride, k.data_ptr(), _heads(k, what, c.n_kv, c.hd),
+                                 v.data_ptr(), _heads(v, what, c.n_kv, c.hd), _int32(torch, what, cu_new, 1), _int32(torch, what, lengths, 1),
+                                 _int32(torch, what, table, 2), table.shape[1], None if positions is None else _int32(torch, what, positions, 1), _stream(torch, dev, None))
+    if status != PF_OK:
+        _check(status, what)
+    return q_out
 
 
 class MoeLayer:
