@@ -9,6 +9,7 @@
 #include <math.h>
 
 #include "pf_attention.cuh"
+#include "pf_tcgen.cuh"
 
 namespace pf {
 
@@ -16,11 +17,14 @@ constexpr int kRows = 256;               // rows of a task
 constexpr int kTok = 128;                // tokens of a tile
 constexpr int kMostTiles = 512;          // tiles of a piece at most: 32-bit sums do not run over more than 65536 tokens
 constexpr int kLeastTiles = 4;           // a piece takes no fewer while others have none
+constexpr unsigned kWaitLimit = 500000, kDrainLimit = 500000;      // polls of 2 us: a second
+constexpr float kSetLift = 7.f;          // log2 of the largest weight when a row's reference is set; it may grow to kLift
 
 struct PrefixArgs {
     AttnArgs a;
     const int32_t *cu, *plen, *ptable;
     int n_groups, pcols;
+    unsigned wait_limit;                 // polls of a wait inside the kernel
     long long n_slots;
     float *slots;                        // [n_slots] x (kRows x HD values, kRows references, kRows sums)
 };
@@ -98,94 +102,451 @@ __device__ __forceinline__ int last_at(const V *list, int n, V x)
     return lo;
 }
 
-// A stretch of one task: tiles [tile, end) of task `task` (number `no` within its group)
+// A stretch of tiles [tile, end) of one task
 struct Stretch {
     Group g;
-    int kv, row0, rows, tile, end, group;
+    int group, kv, row0, rows;           // the task's rows are row0 .. row0 + rows - 1 of the group
+    int tile, end;
     long long slot;
+    // few rows: both streams go through the same rows, and take turns with the tiles
+    __device__ __forceinline__ bool turns() const { return rows <= 128; }
+    __device__ __forceinline__ int tiles_of(int stream) const { return turns() ? (end - tile + 1 - stream) / 2 : end - tile; }
+};
+// the stretches of this block's pieces, one behind the other
+struct Walk {
+    long long total, u, u_end;
+    int n_pieces, piece;
+    __device__ __forceinline__ Walk(long long all) : total(all), u(0), u_end(0), n_pieces(pieces_of(all, gridDim.x)), piece((int)blockIdx.x - (int)gridDim.x) {}
+    __device__ __forceinline__ bool next(const PrefixArgs &P, const long long *units, const int *tasks, Stretch &s)
+    {
+        if (u >= u_end) {
+            piece += gridDim.x;
+            if (piece >= n_pieces) return false;
+            u = first_tile(total, n_pieces, piece);
+            u_end = first_tile(total, n_pieces, piece + 1);
+        }
+        s.group = last_at(units, P.n_groups, u);
+        s.g = group_of(P, s.group);
+        const long long r = u - units[s.group];
+        const int no = (int)(r / s.g.tiles);
+        s.tile = (int)(r - (long long)no * s.g.tiles);
+        s.end = (int)min((long long)s.g.tiles, s.tile + (u_end - u));
+        s.kv = no / s.g.row_tiles;
+        s.row0 = (no - s.kv * s.g.row_tiles) * kRows;
+        s.rows = min(kRows, s.g.rows - s.row0);
+        s.slot = (long long)tasks[s.group] + no + piece;
+        u += s.end - s.tile;
+        return true;
+    }
 };
 
-template <typename T, int HD>
-__global__ void __launch_bounds__(512, 1) prefix_kernel(const __grid_constant__ PrefixArgs P)
+constexpr int kSoftWarps = 8, kWidenWarps = 4;          // two streams of four warps that own the rows; warps that bring the cache's bytes
+constexpr int kPrefixThreads = 32 * (kSoftWarps + kWidenWarps + 1);
+template <int HD> struct PrefixShape {
+    static constexpr int kHalves = HD / 64;             // 128-byte columns of an fp16 row
+    static constexpr int kOperand = kHalves * 16384;    // 128 rows of HD fp16
+    static constexpr int kQ = 0, kK = 2 * kOperand, kV = 4 * kOperand, kBytes = 6 * kOperand;
+};
+// barriers, 8 bytes each
+enum { B_KFULL = 0, B_KEMPTY = 2, B_VFULL = 4, B_VEMPTY = 6, B_QFULL = 8, B_SFULL = 10, B_PFULL = 12, B_OFULL = 14, B_DRAIN = 16, B_COUNT = 17 };
+
+// 16-byte chunk c of row r of an operand's 128-byte column
+__device__ __forceinline__ uint32_t operand_at(int r, int c) { return (uint32_t)(r * 128 + ((c ^ (r & 7)) << 4)); }
+__device__ __forceinline__ void sts128(uint32_t a, uint32_t x, uint32_t y, uint32_t z, uint32_t w)
 {
+    asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(a), "r"(x), "r"(y), "r"(z), "r"(w) : "memory");
+}
+
+struct PrefixRoom {                     // what the roles share
+    uint32_t smem, bars, tmem;
+    volatile int *gave_up;
+    unsigned limit;
+    __device__ __forceinline__ bool wait(int bar, unsigned parity) const { return bar_wait(bars + 8 * bar, parity & 1u, limit, gave_up); }
+    __device__ __forceinline__ bool wait_warp(int bar, unsigned parity) const { return __all_sync(0xFFFFFFFFu, wait(bar, parity)); }      // one answer for all lanes
+    __device__ __forceinline__ void arrive(int bar) const { bar_arrive(bars + 8 * bar); }
+};
+
+// ---- the cache's bytes -> fp16 operands.  256 threads, 16 bytes each at a time; a tile's bytes are asked for while the one in front is widened
+template <int HD>
+__device__ __forceinline__ void widen_role(const PrefixArgs &P, const PrefixRoom &R, Walk walk, const long long *units, const int *tasks)
+{
+    using S = PrefixShape<HD>;
     const AttnArgs &A = P.a;
-    extern __shared__ __align__(128) uint8_t smem[];
-    float *ks = reinterpret_cast<float *>(smem), *vs = ks + 32 * HD, *lv = vs + 32 * HD;
-    long long *units = reinterpret_cast<long long *>(lv + 32);
+    constexpr int LPR = HD / 16, RPP = 32 * kWidenWarps / LPR, N = kTok / RPP;      // lanes a row, rows a pass, passes
+    const int tid = threadIdx.x - 32 * kSoftWarps, lane = tid & 31;
+    const int r0 = tid / LPR, c = tid % LPR;
+    // a lane's 16 dims are chunks 2c and 2c + 1 of the row's fp16 form; lanes of the second column store them the other way round: no bank twice
+    const uint32_t column = (uint32_t)(c / 4) * 16384u;
+    const int c0 = 2 * (c % 4) + (c / 4), c1 = 2 * (c % 4) + 1 - (c / 4);
+    const int64_t page_bytes = (int64_t)A.c.page * HD;
+    const int page_log2 = 31 - __clz(A.c.page);
+    unsigned n = 0;                                     // tiles so far
+    Stretch s;
+    while (walk.next(P, units, tasks, s)) {
+        const int32_t *row = P.ptable + (int64_t)s.group * P.pcols;
+        uint4 k[N], v[N];
+        int64_t at[N];                                  // of the next tile: offset of the lane's bytes, -1 where there is no token
+        auto find = [&](int tile) {
+#pragma unroll
+            for (int i = 0; i < N; i++) {
+                const int tok = tile * kTok + r0 + i * RPP;
+                int page = -1;
+                if (tile < s.end && tok < s.g.len) page = row[tok >> page_log2];
+                at[i] = page < 0 || page >= A.c.n_pages ? -1 : ((int64_t)page * A.c.n_kv + s.kv) * page_bytes + (tok & (A.c.page - 1)) * HD + c * 16;
+            }
+        };
+        auto fetch = [&](const uint8_t *from, uint4 (&x)[N]) {
+#pragma unroll
+            for (int i = 0; i < N; i++) x[i] = at[i] >= 0 ? __ldg(reinterpret_cast<const uint4 *>(from + at[i])) : make_uint4(0u, 0u, 0u, 0u);
+        };
+        auto put = [&](uint32_t to, const uint4 (&x)[N]) {
+#pragma unroll
+            for (int i = 0; i < N; i++) {
+                uint32_t w[8];
+                widen4(x[i].x, w[0], w[1]);
+                widen4(x[i].y, w[2], w[3]);
+                widen4(x[i].z, w[4], w[5]);
+                widen4(x[i].w, w[6], w[7]);
+                const int r = r0 + i * RPP;
+                const bool swap = c / 4;
+                const uint32_t at0 = to + column;
+                sts128(at0 + operand_at(r, c0), swap ? w[4] : w[0], swap ? w[5] : w[1], swap ? w[6] : w[2], swap ? w[7] : w[3]);
+                sts128(at0 + operand_at(r, c1), swap ? w[0] : w[4], swap ? w[1] : w[5], swap ? w[2] : w[6], swap ? w[3] : w[7]);
+            }
+            publish_shared();
+            __syncwarp();
+        };
+        find(s.tile);
+        fetch(A.c.d_k, k);
+        fetch(A.c.d_v, v);
+        for (int t = s.tile; t < s.end; t++, n++) {
+            const int stage = n & 1;
+            const unsigned free = ((n >> 1) & 1u) ^ 1u;
+            find(t + 1);
+            if (!R.wait_warp(B_KEMPTY + stage, free)) return;
+            put(R.smem + S::kK + stage * S::kOperand, k);
+            if (lane == 0) R.arrive(B_KFULL + stage);
+            fetch(A.c.d_k, k);
+            if (!R.wait_warp(B_VEMPTY + stage, free)) return;
+            put(R.smem + S::kV + stage * S::kOperand, v);
+            if (lane == 0) R.arrive(B_VFULL + stage);
+            fetch(A.c.d_v, v);
+        }
+    }
+}
+
+// ---- the products, by one thread.  Tensor memory: 128 columns of scores of either stream, which weights replace, then HD columns of values of either
+template <int HD>
+__device__ __forceinline__ void product_role(const PrefixArgs &P, const PrefixRoom &R, Walk walk, const long long *units, const int *tasks)
+{
+    using S = PrefixShape<HD>;
+    constexpr uint32_t kScores = mma_shape(kTok, false), kValues = mma_shape(HD, true);
+    unsigned n = 0, runs = 0, weights[2] = {0, 0};      // tiles and stretches so far; each stream's tiles of weights
+    auto scores = [&](int j, int stage) {
+        const uint64_t q = operand_along(R.smem + S::kQ + j * S::kOperand), k = operand_along(R.smem + S::kK + stage * S::kOperand);
+#pragma unroll
+        for (int i = 0; i < HD / 16; i++) {
+            const uint32_t on = (i / 4) * 1024 + (i % 4) * 2;        // in 16 bytes
+            mma_shared(R.tmem + j * 128, q + on, k + on, kScores, i > 0);
+        }
+        mma_commit(R.bars + 8 * (B_SFULL + j));
+    };
+    auto values = [&](int j, int stage, bool first) {
+        const uint64_t v = operand_across(R.smem + S::kV + stage * S::kOperand, 16384u);
+#pragma unroll
+        for (int i = 0; i < kTok / 16; i++) mma_tmem(R.tmem + 256 + j * HD, R.tmem + j * 128 + 8 * i, v + i * 128, kValues, !(first && i == 0));
+    };
+    auto weights_ready = [&](int j) {
+        if (!R.wait(B_PFULL + j, weights[j]++)) return false;
+        tmem_after_sync();
+        return true;
+    };
+    Stretch s;
+    while (walk.next(P, units, tasks, s)) {
+        const int m = s.end - s.tile;
+        const bool turns = s.turns();
+        if (!R.wait(B_QFULL, runs) || !R.wait(B_QFULL + 1, runs)) return;
+        runs++;
+        const unsigned base = n;
+        const int lag = turns ? 2 : 1;
+        // step i: the scores of tile i, behind the values of the tile `lag` in front, whose weights lie where the scores go
+        for (int i = 0; i < m + lag; i++) {
+            const unsigned kt = base + i, vt = base + i - lag;
+            if (i < m && !R.wait(B_KFULL + (kt & 1), kt >> 1)) return;
+            if (i >= lag && !R.wait(B_VFULL + (vt & 1), vt >> 1)) return;
+            for (int j = turns ? i & 1 : 0; j < (turns ? (i & 1) + 1 : 2); j++) {
+                if (i >= lag) {
+                    if (!weights_ready(j)) return;
+                    values(j, vt & 1, i < 2 * lag);
+                    if (i + lag >= m + lag) mma_commit(R.bars + 8 * (B_OFULL + j));
+                }
+                if (i < m) scores(j, kt & 1);
+            }
+            if (i >= lag) mma_commit(R.bars + 8 * (B_VEMPTY + (vt & 1)));
+            if (i < m) mma_commit(R.bars + 8 * (B_KEMPTY + (kt & 1)));
+        }
+        if (turns && m == 1) mma_commit(R.bars + 8 * (B_OFULL + 1));      // a stream without a tile keeps step too
+        n += m;
+    }
+}
+
+// ---- the rows: thread r of a stream owns row r of its 128
+template <typename T, int HD>
+__device__ __forceinline__ bool rows_run(const PrefixArgs &P, const PrefixRoom &R, const Stretch &s, int j, unsigned &tiles, float (&zl)[2])
+{
+    using S = PrefixShape<HD>;
+    const AttnArgs &A = P.a;
+    const int warp = threadIdx.x / 32 % 4, lane = threadIdx.x & 31, r = 32 * warp + lane;
+    const int at = s.row0 + (s.turns() ? 0 : 128 * j) + r;
+    const bool live = at < s.g.rows;
+    const bool any = s.row0 + (s.turns() ? 0 : 128 * j) + 32 * warp < s.g.rows;       // of the warp
+    const int count = s.tiles_of(j);
+    const uint32_t lanes = (uint32_t)(32 * warp) << 16, score = R.tmem + lanes + j * 128, value = R.tmem + lanes + 256 + j * HD;
+    // The query row, as in the kernel of a sequence's own tokens: its largest finite element goes to [2^13, 2^14), and the power of two and the sign of
+    // sm_scale to the factor of the scores.
+    float up;
+    {
+        uint4 raw[HD / 8];
+        const uint16_t *src = A.q + (int64_t)(s.g.first + at / A.group) * A.qs + (int64_t)(s.kv * A.group + at % A.group) * HD;
+        float top = 0.f;
+#pragma unroll
+        for (int i = 0; i < HD / 8; i++) {
+            raw[i] = live ? *reinterpret_cast<const uint4 *>(src + 8 * i) : make_uint4(0u, 0u, 0u, 0u);
+            const uint32_t w[4] = {raw[i].x, raw[i].y, raw[i].z, raw[i].w};
+#pragma unroll
+            for (int x = 0; x < 4; x++) {
+                const float2 f = pair_to_f32<T>(w[x]);
+                top = fmaxf(top, fmaxf(fabsf(f.x) < INFINITY ? fabsf(f.x) : 0.f, fabsf(f.y) < INFINITY ? fabsf(f.y) : 0.f));
+            }
+        }
+        int e = top > 0.f ? ((int)(__float_as_uint(top) >> 23) - 127) : 0;
+        e = max(-100, e) - 13;
+        const float down = A.scale_log2 < 0.f ? -exp2f((float)-e) : exp2f((float)-e);
+        up = fabsf(A.scale_log2) * exp2f((float)e);
+        const uint32_t q = R.smem + S::kQ + j * S::kOperand;
+#pragma unroll
+        for (int i = 0; i < HD / 8; i++) {
+            const uint32_t w[4] = {raw[i].x, raw[i].y, raw[i].z, raw[i].w};
+            uint32_t o[4];
+#pragma unroll
+            for (int x = 0; x < 4; x++) {
+                const float2 f = pair_to_f32<T>(w[x]);
+                o[x] = f16x2_of(f.x * down, f.y * down);
+            }
+            sts128(q + (i / 8) * 16384 + operand_at(r, i % 8), o[0], o[1], o[2], o[3]);
+        }
+        publish_shared();
+        __syncwarp();
+        if (lane == 0) R.arrive(B_QFULL + j);
+    }
+    float &z = zl[0], &l = zl[1];
+    float l32 = 0.f;                                    // sums in two levels, as there
+    z = -INFINITY;
+    l = 0.f;
+    const int step = s.turns() ? 2 : 1;
+    // lane x < 8: scales of the x-th 16 tokens' page of a tile; missing pages and 16 tokens behind the end: lv -infinity
+    const int32_t *row = P.ptable + (int64_t)s.group * P.pcols;
+    int page = -1;
+    float ks = 0.f, vs = -1.f, next_ks = 0.f, next_vs = -1.f;
+    auto find = [&](int tile) {
+        const int tok = tile * kTok + 16 * lane;
+        page = lane < 8 && tile < s.end && tok < s.g.len ? row[tok >> (31 - __clz(A.c.page))] : -1;
+    };
+    auto fetch = [&]() {
+        const bool there = page >= 0 && page < A.c.n_pages;
+        const int64_t ph = (int64_t)page * A.c.n_kv + s.kv;
+        next_ks = there ? __ldg(A.c.d_k_scale + ph) : 0.f;
+        next_vs = there ? __ldg(A.c.d_v_scale + ph) : -1.f;
+    };
+    int tile = s.tile + (s.turns() ? j : 0);
+    find(tile);
+    fetch();
+    find(tile + step);
+    for (int i = 0; i < count; i++, tile += step, tiles++) {
+        ks = next_ks;
+        vs = next_vs;
+        fetch();
+        find(tile + 2 * step);
+        const float v = fmaxf(vs, 8.673617379884035e-19f);      // 2^-60
+        const float my_lv = vs < 0.f ? -INFINITY : __log2f(v), my_iv = __fdividef(1.f, v);
+        if (!R.wait_warp(B_SFULL + j, tiles)) return false;
+        tmem_after_sync();
+        if (any) {
+            const int left = s.g.len - tile * kTok;
+            float top = -INFINITY;
+#pragma unroll
+            for (int c = 0; c < 4; c++) {
+                uint32_t x[32];
+                tmem_ld32(score + 32 * c, x);
+                tmem_wait_ld(x);
+#pragma unroll
+                for (int h = 0; h < 2; h++) {
+                    const float f = up * __shfl_sync(0xFFFFFFFFu, ks, 2 * c + h), lv = __shfl_sync(0xFFFFFFFFu, my_lv, 2 * c + h);
+                    float m = -INFINITY;
+                    if (32 * c + 16 * h + 16 <= left) {
+#pragma unroll
+                        for (int k = 0; k < 16; k++) m = fmaxf(m, __uint_as_float(x[16 * h + k]));
+                    } else {
+#pragma unroll
+                        for (int k = 0; k < 16; k++) m = fmaxf(m, 32 * c + 16 * h + k < left ? __uint_as_float(x[16 * h + k]) : -INFINITY);
+                    }
+                    top = fmaxf(top, fmaf(m, f, lv));
+                }
+            }
+            // A new reference where a weight would pass 2^15; it brings the largest to 2^7, so that the next one is far off.
+            if (__any_sync(0xFFFFFFFFu, __fsub_ru(top, kLift) > z)) {
+                const float n = __fsub_ru(top, kLift) > z ? __fsub_ru(top, kSetLift) : z;
+                const float a = n == -INFINITY ? 1.f : ex2(z - n);
+                z = n;
+                l *= a;
+                l32 *= a;
+                if (i > 0) {                            // this stream's products in front are done: their end came before the scores'
+#pragma unroll
+                    for (int c = 0; c < HD / 32; c++) {
+                        uint32_t x[32];
+                        tmem_ld32(value + 32 * c, x);
+                        tmem_wait_ld(x);
+#pragma unroll
+                        for (int k = 0; k < 32; k++) x[k] = __float_as_uint(__uint_as_float(x[k]) * a);
+                        tmem_st32(value + 32 * c, x);
+                    }
+                }
+            }
+            const float ref = z == -INFINITY ? 0.f : z;
+#pragma unroll
+            for (int c = 0; c < 4; c++) {
+                uint32_t x[32], p[16];
+                tmem_ld32(score + 32 * c, x);
+                tmem_wait_ld(x);
+#pragma unroll
+                for (int h = 0; h < 2; h++) {
+                    const float f = up * __shfl_sync(0xFFFFFFFFu, ks, 2 * c + h), lv = __shfl_sync(0xFFFFFFFFu, my_lv, 2 * c + h) - ref;
+                    const float iv = __shfl_sync(0xFFFFFFFFu, my_iv, 2 * c + h);
+                    float sum = 0.f;
+#pragma unroll
+                    for (int k = 0; k < 16; k += 2) {
+                        float e0 = ex2(fmaf(__uint_as_float(x[16 * h + k]), f, lv)), e1 = ex2(fmaf(__uint_as_float(x[16 * h + k + 1]), f, lv));
+                        if (32 * c + 16 * h + 16 > left) {
+                            if (32 * c + 16 * h + k >= left) e0 = 0.f;
+                            if (32 * c + 16 * h + k + 1 >= left) e1 = 0.f;
+                        }
+                        sum += e0 + e1;
+                        p[8 * h + k / 2] = f16x2_of(e0, e1);
+                    }
+                    l32 = fmaf(sum, iv, l32);
+                }
+                tmem_st16(score + 16 * c, p);           // over scores that have been read
+            }
+            tmem_wait_st();
+            if ((i & 31) == 31) {
+                l += l32;
+                l32 = 0.f;
+            }
+        }
+        tmem_before_sync();
+        __syncwarp();
+        if (lane == 0) R.arrive(B_PFULL + j);
+    }
+    l += l32;
+    return true;
+}
+
+template <typename T, int HD>
+__device__ __forceinline__ void rows_role(const PrefixArgs &P, const PrefixRoom &R, Walk walk, const long long *units, const int *tasks)
+{
+    const int j = threadIdx.x / 128, warp = threadIdx.x / 32 % 4, lane = threadIdx.x & 31, r = 32 * warp + lane;
+    unsigned runs = 0, tiles = 0;                       // stretches, and tiles of this stream, so far
+    bool good = true;
+    Stretch s;
+    while (walk.next(P, units, tasks, s)) {
+        float zl[2] = {0.f, __int_as_float(0x7FC00000)};
+        const int count = s.tiles_of(j);
+        if (good) good = rows_run<T, HD>(P, R, s, j, tiles, zl);
+        if (good) good = R.wait_warp(B_OFULL + j, runs);
+        runs++;
+        if (!good) zl[1] = __int_as_float(0x7FC00000);  // a wait ran out: these rows are NaN
+        const int row = s.turns() ? r : 128 * j + r;
+        const bool live = row < s.rows && s.slot < P.n_slots;
+        float *to = P.slots + s.slot * (kRows * (HD + 2));
+        const int place = 128 * j + r;
+        if (live) {
+            to[kRows * HD + place] = zl[0];
+            to[kRows * (HD + 1) + place] = zl[1];
+        }
+        if (good && count) {
+            tmem_after_sync();
+#pragma unroll
+            for (int c = 0; c < HD / 32; c++) {
+                uint32_t x[32];
+                tmem_ld32(R.tmem + ((uint32_t)(32 * warp) << 16) + 256 + j * HD + 32 * c, x);
+                tmem_wait_ld(x);
+                if (live)
+#pragma unroll
+                    for (int k = 0; k < 32; k += 4)
+                        *reinterpret_cast<uint4 *>(to + place * HD + 32 * c + k) = make_uint4(x[k], x[k + 1], x[k + 2], x[k + 3]);
+            }
+            tmem_before_sync();
+        } else if (live) {
+            for (int k = 0; k < HD; k += 4) *reinterpret_cast<uint4 *>(to + place * HD + k) = make_uint4(0u, 0u, 0u, 0u);
+        }
+    }
+}
+
+template <typename T, int HD>
+__global__ void __launch_bounds__(kPrefixThreads, 1) prefix_kernel(const __grid_constant__ PrefixArgs P)
+{
+    using S = PrefixShape<HD>;
+    extern __shared__ __align__(1024) uint8_t prefix_smem[];
+    uint8_t *room = prefix_smem + (-smem_addr(prefix_smem) & 1023u);      // operands begin at multiples of 1024
+    __shared__ __align__(8) uint64_t bars[B_COUNT];
+    __shared__ uint32_t tmem_at;
+    __shared__ int gave_up;
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    long long *units = reinterpret_cast<long long *>(room + S::kBytes);
     int *tasks = reinterpret_cast<int *>(units + P.n_groups + 1);
     group_prefix(P, units, tasks);
     const long long total = units[P.n_groups];
-    if (total == 0) return;
-    const int n_pieces = pieces_of(total, gridDim.x);
-    const int row = threadIdx.x >> 1, part = threadIdx.x & 1;
-    constexpr int D = HD / 2;
-    for (int piece = blockIdx.x; piece < n_pieces; piece += gridDim.x) {
-        long long u = first_tile(total, n_pieces, piece);
-        const long long u_end = first_tile(total, n_pieces, piece + 1);
-        while (u < u_end) {
-            const int gi = last_at(units, P.n_groups, u);
-            const Group g = group_of(P, gi);
-            const long long r = u - units[gi];
-            const int no = (int)(r / g.tiles), tile0 = (int)(r - (long long)no * g.tiles);
-            const int end = (int)min((long long)g.tiles, tile0 + (u_end - u));
-            const int kv = no / g.row_tiles, rt = no - kv * g.row_tiles;
-            const int at = rt * kRows + row;
-            const bool live = at < g.rows;
-            float q[D], o[D], z = -INFINITY, l = 0.f;
-#pragma unroll
-            for (int i = 0; i < D; i++) q[i] = 0.f, o[i] = 0.f;
-            if (live) {
-                const uint16_t *src = A.q + (int64_t)(g.first + at / A.group) * A.qs + (int64_t)(kv * A.group + at % A.group) * HD + part * D;
-#pragma unroll
-                for (int i = 0; i < D; i += 2) {
-                    const float2 f = pair_to_f32<T>(*reinterpret_cast<const uint32_t *>(src + i));
-                    q[i] = f.x * A.scale_log2;
-                    q[i + 1] = f.y * A.scale_log2;
-                }
-            }
-            for (int tok0 = tile0 * kTok; tok0 < min(g.len, end * kTok); tok0 += 32) {
-                __syncthreads();
-                for (int i = threadIdx.x; i < 32 * HD / 4; i += blockDim.x) {
-                    const int t = i / (HD / 4), e = i % (HD / 4) * 4, tok = tok0 + t;
-                    int page = tok < g.len ? P.ptable[(int64_t)gi * P.pcols + tok / A.c.page] : -1;
-                    if (page >= A.c.n_pages) page = -1;
-                    const int64_t ph = (int64_t)page * A.c.n_kv + kv, from = (ph * A.c.page + tok % A.c.page) * HD + e;
-                    const uint32_t k = page < 0 ? 0u : *reinterpret_cast<const uint32_t *>(A.c.d_k + from), v = page < 0 ? 0u : *reinterpret_cast<const uint32_t *>(A.c.d_v + from);
-                    const float fk = page < 0 ? 0.f : A.c.d_k_scale[ph], fv = page < 0 ? 0.f : A.c.d_v_scale[ph];
-                    const float2 k0 = f32x2_of_f16x2(f16x2_of_e4m3x2(k)), k1 = f32x2_of_f16x2(f16x2_of_e4m3x2(k >> 16));
-                    const float2 v0 = f32x2_of_f16x2(f16x2_of_e4m3x2(v)), v1 = f32x2_of_f16x2(f16x2_of_e4m3x2(v >> 16));
-                    *reinterpret_cast<float4 *>(ks + t * HD + e) = make_float4(k0.x * fk, k0.y * fk, k1.x * fk, k1.y * fk);
-                    *reinterpret_cast<float4 *>(vs + t * HD + e) = make_float4(v0.x * fv, v0.y * fv, v1.x * fv, v1.y * fv);
-                    if (e == 0) lv[t] = page < 0 ? -INFINITY : 0.f;
-                }
-                __syncthreads();
-                for (int t = 0; t < 32; t++) {
-                    float s = 0.f;
-#pragma unroll
-                    for (int i = 0; i < D; i++) s = fmaf(q[i], ks[t * HD + part * D + i], s);
-                    s += __shfl_xor_sync(0xFFFFFFFFu, s, 1);
-                    s += lv[t];
-                    const float n = fmaxf(z, s);
-                    const float f = n == -INFINITY ? 1.f : exp2f(z - n), p = exp2f(s - (n == -INFINITY ? 0.f : n));
-                    z = n;
-                    l = fmaf(l, f, p);
-#pragma unroll
-                    for (int i = 0; i < D; i++) o[i] = fmaf(o[i], f, p * vs[t * HD + part * D + i]);
-                }
-            }
-            const long long slot = tasks[gi] + no + piece;
-            if (live && slot < P.n_slots) {
-                float *to = P.slots + slot * (kRows * (HD + 2));
-#pragma unroll
-                for (int i = 0; i < D; i++) to[row * HD + part * D + i] = o[i];
-                if (part == 0) {
-                    to[kRows * HD + row] = z;
-                    to[kRows * (HD + 1) + row] = l;
-                }
-            }
-            u += end - tile0;
+    if (total == 0 || (int)blockIdx.x >= pieces_of(total, gridDim.x)) return;
+    const int warp = threadIdx.x >> 5;
+    PrefixRoom R{smem_addr(room), smem_addr(bars), 0u, &gave_up, P.wait_limit};
+    if (threadIdx.x == 0) {
+        gave_up = 0;
+        for (int i = 0; i < 2; i++) {
+            bar_init(R.bars + 8 * (B_KFULL + i), kWidenWarps);
+            bar_init(R.bars + 8 * (B_VFULL + i), kWidenWarps);
+            bar_init(R.bars + 8 * (B_KEMPTY + i), 1);
+            bar_init(R.bars + 8 * (B_VEMPTY + i), 1);
+            bar_init(R.bars + 8 * (B_QFULL + i), 4);
+            bar_init(R.bars + 8 * (B_SFULL + i), 1);
+            bar_init(R.bars + 8 * (B_PFULL + i), 4);
+            bar_init(R.bars + 8 * (B_OFULL + i), 1);
         }
+        bar_init(R.bars + 8 * B_DRAIN, 1);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
+    if (warp == kSoftWarps + kWidenWarps) tmem_alloc(smem_addr(&tmem_at), 512);
+    tmem_before_sync();
+    __syncthreads();
+    tmem_after_sync();
+    R.tmem = tmem_at;
+    const Walk walk(total);
+    if (warp < kSoftWarps) {
+        rows_role<T, HD>(P, R, walk, units, tasks);
+    } else if (warp < kSoftWarps + kWidenWarps) {
+        widen_role<HD>(P, R, walk, units, tasks);
+    } else {
+        if ((threadIdx.x & 31) == 0) {
+            product_role<HD>(P, R, walk, units, tasks);
+            // whatever was begun is done before the block gives its memory back
+            mma_commit(R.bars + 8 * B_DRAIN);
+            int alone = 0;
+            bar_wait(R.bars + 8 * B_DRAIN, 0, kDrainLimit, &alone);
+        }
+        __syncwarp();
+    }
+    tmem_before_sync();
+    __syncthreads();
+    if (warp == kSoftWarps + kWidenWarps) tmem_free(R.tmem, 512);
 }
 
 // ------------------------------------------------------------------ the join
@@ -225,19 +586,21 @@ __global__ void __launch_bounds__(256) prefix_join_kernel(const __grid_constant_
         }
         // parts of its group's prefix
         long long slot = 0;
-        int n_pre = 0, at = 0;
+        int n_pre = 0, at = 0, both = 1;          // parts of a slot
         if (total) {
             const int gi = P.cu ? last_at(P.cu, P.n_groups, b) : 0;
             const Group g = group_of(P, gi);
             if (g.tiles && b >= g.first && b < g.first + g.rows / A.group) {
                 at = (b - g.first) * A.group + gh;
                 const int no = kv * g.row_tiles + at / kRows;
+                both = g.rows - at / kRows * kRows <= 128 ? 2 : 1;
                 at %= kRows;
                 const long long begin = units[gi] + (long long)no * g.tiles;
                 const int p0 = piece_of(total, n_pieces, begin);
                 n_pre = piece_of(total, n_pieces, begin + g.tiles - 1) - p0 + 1;
                 slot = (long long)tasks[gi] + no + p0;
                 if (slot + n_pre > P.n_slots) n_pre = 0;
+                n_pre *= both;
             }
         }
         const int n = n_own + n_pre;
@@ -258,10 +621,11 @@ __global__ void __launch_bounds__(256) prefix_join_kernel(const __grid_constant_
                 z = p[S::kHeads * HD + own_row];
                 l = p[S::kHeads * (HD + 1) + own_row];
             } else if (i < n) {
-                const float *p = P.slots + (slot + i - n_own) * (kRows * (HD + 2));
-                from = p + at * HD;
-                z = p[kRows * HD + at];
-                l = p[kRows * (HD + 1) + at];
+                const int no = i - n_own, place = both == 2 ? at + 128 * (no & 1) : at;
+                const float *p = P.slots + (slot + (both == 2 ? no >> 1 : no)) * (kRows * (HD + 2));
+                from = p + place * HD;
+                z = p[kRows * HD + place];
+                l = p[kRows * (HD + 1) + place];
             }
             float most = fmaxf(top, z);
 #pragma unroll
@@ -320,11 +684,11 @@ static int prefix_launch(PrefixArgs p, int device, int sms, cudaStream_t st)
     a.row_blocks = (a.group + S::kHeads - 1) / S::kHeads;
     a.jobs_per_seq = a.c.n_kv * a.row_blocks;
     const size_t groups = (size_t)(p.n_groups + 1) * 12, own = ((size_t)a.n_seq + 1) * 4;
-    const size_t smem0 = 2 * 32 * HD * 4 + 128 + groups, smem1 = (size_t)S::kWarps * S::kWarpBytes + own, smem2 = groups + own;
+    const size_t smem0 = 1024 + PrefixShape<HD>::kBytes + groups, smem1 = (size_t)S::kWarps * S::kWarpBytes + own, smem2 = groups + own;
     PF_CUDA_TRY(ensure_dynamic_smem((const void *)prefix_kernel<T, HD>, device, smem0), "prefix_kernel shared memory");
     PF_CUDA_TRY(ensure_dynamic_smem((const void *)attention_kernel<T, HD, NB, true>, device, smem1), "attention_kernel shared memory");
     PF_CUDA_TRY(ensure_dynamic_smem((const void *)prefix_join_kernel<T, HD, NB>, device, smem2), "prefix_join_kernel shared memory");
-    prefix_kernel<T, HD><<<sms, 512, smem0, st>>>(p);
+    prefix_kernel<T, HD><<<sms, kPrefixThreads, smem0, st>>>(p);
     PF_CUDA_TRY(cudaGetLastError(), "prefix_kernel launch");
     count_launch();
     PF_CUDA_TRY(launch_chained(attention_kernel<T, HD, NB, true>, dim3(sms), dim3(S::kWarps * 32), smem1, st, a), "attention_kernel launch");
@@ -393,6 +757,7 @@ extern "C" int pf_prefix_attention(const pf_kv_cache_t *cache, int32_t dtype, in
     p.cu = d_cu_seqs; p.plen = d_prefix_len; p.ptable = d_prefix_table;
     p.n_groups = n_groups; p.pcols = prefix_cols; p.n_slots = z.n_slots;
     p.slots = (float *)(ws + z.slots);
+    p.wait_limit = kWaitLimit;
     cudaStream_t st = (cudaStream_t)stream;
     return dtype == PF_DT_BF16 ? prefix_launch<Bf16>(p, device, sms, st) : prefix_launch<F16>(p, device, sms, st);
 }
