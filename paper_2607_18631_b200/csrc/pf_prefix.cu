@@ -140,8 +140,13 @@ struct Walk {
     }
 };
 
-constexpr int kSoftWarps = 8, kWidenWarps = 4;          // two streams of four warps that own the rows; warps that bring the cache's bytes
-constexpr int kPrefixThreads = 32 * (kSoftWarps + kWidenWarps + 1);
+// Four groups of four warps: two streams that own the rows, one that brings the cache's bytes, and one of which a thread issues the products.  Registers go
+// where they are needed: 256 x 184 + 128 x 104 + 128 x 40 = 512 x 128, what the block is launched with.
+constexpr int kSoftWarps = 8, kWidenWarps = 4;
+constexpr int kPrefixThreads = 512, kSoftRegs = 184, kWidenRegs = 104, kProductRegs = 40;
+static_assert(kSoftRegs * 256 + kWidenRegs * 128 + kProductRegs * 128 <= kPrefixThreads * 128, "no group waits for registers that nobody gives back");
+template <int N> __device__ __forceinline__ void take_registers() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N)); }
+template <int N> __device__ __forceinline__ void leave_registers() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N)); }
 template <int HD> struct PrefixShape {
     static constexpr int kHalves = HD / 64;             // 128-byte columns of an fp16 row
     static constexpr int kOperand = kHalves * 16384;    // 128 rows of HD fp16
@@ -166,71 +171,75 @@ struct PrefixRoom {                     // what the roles share
     __device__ __forceinline__ void arrive(int bar) const { bar_arrive(bars + 8 * bar); }
 };
 
-// ---- the cache's bytes -> fp16 operands.  256 threads, 16 bytes each at a time; a tile's bytes are asked for while the one in front is widened
+// ---- the cache's bytes -> fp16 operands.  Two warps bring keys, two bring values; a thread holds the 16-byte pieces of a whole tile that it asked for when
+// it had widened those of the one in front.  Eight neighbouring lanes have four pieces of each of two rows, so that their stores meet no bank twice.
 template <int HD>
 __device__ __forceinline__ void widen_role(const PrefixArgs &P, const PrefixRoom &R, Walk walk, const long long *units, const int *tasks)
 {
     using S = PrefixShape<HD>;
     const AttnArgs &A = P.a;
-    constexpr int LPR = HD / 16, RPP = 32 * kWidenWarps / LPR, N = kTok / RPP;      // lanes a row, rows a pass, passes
-    const int tid = threadIdx.x - 32 * kSoftWarps, lane = tid & 31;
-    const int r0 = tid / LPR, c = tid % LPR;
-    // a lane's 16 dims are chunks 2c and 2c + 1 of the row's fp16 form; lanes of the second column store them the other way round: no bank twice
-    const uint32_t column = (uint32_t)(c / 4) * 16384u;
-    const int c0 = 2 * (c % 4) + (c / 4), c1 = 2 * (c % 4) + 1 - (c / 4);
-    const int64_t page_bytes = (int64_t)A.c.page * HD;
+    constexpr int ROWS = 32 / (HD / 16);                // rows of a warp's pass
+    constexpr int N = kTok / (2 * ROWS), PER16 = 16 / (2 * ROWS);      // passes, and passes of 16 tokens
+    const int lane = threadIdx.x & 31, w = threadIdx.x / 32 - kSoftWarps, values = w >> 1;
+    const int c = HD == 128 ? (lane & 3) + (lane >> 4) * 4 : lane & 3, r0 = (w & 1) * ROWS + (HD == 128 ? (lane >> 2) & 3 : lane >> 2);
+    const uint8_t *from = (values ? A.c.d_v : A.c.d_k) + r0 * HD + c * 16;
+    const uint32_t to = R.smem + (values ? S::kV : S::kK) + (uint32_t)(c >> 2) * 16384u;
+    const uint32_t to0 = to + operand_at(r0, 2 * (c & 3)), to1 = to + operand_at(r0, 2 * (c & 3) + 1);
+    const int full = values ? B_VFULL : B_KFULL, empty = values ? B_VEMPTY : B_KEMPTY;
     const int page_log2 = 31 - __clz(A.c.page);
     unsigned n = 0;                                     // tiles so far
     Stretch s;
     while (walk.next(P, units, tasks, s)) {
         const int32_t *row = P.ptable + (int64_t)s.group * P.pcols;
-        uint4 k[N], v[N];
-        int64_t at[N];                                  // of the next tile: offset of the lane's bytes, -1 where there is no token
+        uint4 x[N];
+        int page;                                       // lane i < 8: page of the i-th 16 tokens of the next tile, negative: none
         auto find = [&](int tile) {
+            const int tok = tile * kTok + 16 * lane;
+            page = lane < 8 && tile < s.end && tok < s.g.len ? row[tok >> page_log2] : -1;
+        };
+        auto fetch = [&](int tile) {
+            const int64_t at = page < 0 || page >= A.c.n_pages ? -1 : (((int64_t)page * A.c.n_kv + s.kv) * A.c.page + ((16 * lane) & (A.c.page - 1))) * HD;
+            const int left = s.g.len - tile * kTok - r0;
+            if (__all_sync(0xFFFFFFFFu, (at >= 0 || lane >= 8) && left >= kTok)) {
 #pragma unroll
-            for (int i = 0; i < N; i++) {
-                const int tok = tile * kTok + r0 + i * RPP;
-                int page = -1;
-                if (tile < s.end && tok < s.g.len) page = row[tok >> page_log2];
-                at[i] = page < 0 || page >= A.c.n_pages ? -1 : ((int64_t)page * A.c.n_kv + s.kv) * page_bytes + (tok & (A.c.page - 1)) * HD + c * 16;
+                for (int g = 0; g < 8; g++) {
+                    const uint8_t *src = from + __shfl_sync(0xFFFFFFFFu, at, g);
+#pragma unroll
+                    for (int i = 0; i < PER16; i++) x[g * PER16 + i] = __ldg(reinterpret_cast<const uint4 *>(src + i * 2 * ROWS * HD));
+                }
+            } else {
+#pragma unroll
+                for (int g = 0; g < 8; g++) {
+                    const int64_t base = __shfl_sync(0xFFFFFFFFu, at, g);
+#pragma unroll
+                    for (int i = 0; i < PER16; i++) {
+                        const bool there = base >= 0 && (g * PER16 + i) * 2 * ROWS < left;
+                        x[g * PER16 + i] = there ? __ldg(reinterpret_cast<const uint4 *>(from + base + i * 2 * ROWS * HD)) : make_uint4(0u, 0u, 0u, 0u);
+                    }
+                }
             }
         };
-        auto fetch = [&](const uint8_t *from, uint4 (&x)[N]) {
-#pragma unroll
-            for (int i = 0; i < N; i++) x[i] = at[i] >= 0 ? __ldg(reinterpret_cast<const uint4 *>(from + at[i])) : make_uint4(0u, 0u, 0u, 0u);
-        };
-        auto put = [&](uint32_t to, const uint4 (&x)[N]) {
+        find(s.tile);
+        fetch(s.tile);
+        for (int t = s.tile; t < s.end; t++, n++) {
+            const int stage = n & 1;
+            find(t + 1);
+            if (!R.wait_warp(empty + stage, ((n >> 1) & 1u) ^ 1u)) return;
 #pragma unroll
             for (int i = 0; i < N; i++) {
-                uint32_t w[8];
-                widen4(x[i].x, w[0], w[1]);
-                widen4(x[i].y, w[2], w[3]);
-                widen4(x[i].z, w[4], w[5]);
-                widen4(x[i].w, w[6], w[7]);
-                const int r = r0 + i * RPP;
-                const bool swap = c / 4;
-                const uint32_t at0 = to + column;
-                sts128(at0 + operand_at(r, c0), swap ? w[4] : w[0], swap ? w[5] : w[1], swap ? w[6] : w[2], swap ? w[7] : w[3]);
-                sts128(at0 + operand_at(r, c1), swap ? w[0] : w[4], swap ? w[1] : w[5], swap ? w[2] : w[6], swap ? w[3] : w[7]);
+                uint32_t h[8];
+                widen4(x[i].x, h[0], h[1]);
+                widen4(x[i].y, h[2], h[3]);
+                widen4(x[i].z, h[4], h[5]);
+                widen4(x[i].w, h[6], h[7]);
+                const uint32_t on = stage * S::kOperand + i * 2 * ROWS * 128;
+                sts128(to0 + on, h[0], h[1], h[2], h[3]);
+                sts128(to1 + on, h[4], h[5], h[6], h[7]);
             }
             publish_shared();
             __syncwarp();
-        };
-        find(s.tile);
-        fetch(A.c.d_k, k);
-        fetch(A.c.d_v, v);
-        for (int t = s.tile; t < s.end; t++, n++) {
-            const int stage = n & 1;
-            const unsigned free = ((n >> 1) & 1u) ^ 1u;
-            find(t + 1);
-            if (!R.wait_warp(B_KEMPTY + stage, free)) return;
-            put(R.smem + S::kK + stage * S::kOperand, k);
-            if (lane == 0) R.arrive(B_KFULL + stage);
-            fetch(A.c.d_k, k);
-            if (!R.wait_warp(B_VEMPTY + stage, free)) return;
-            put(R.smem + S::kV + stage * S::kOperand, v);
-            if (lane == 0) R.arrive(B_VFULL + stage);
-            fetch(A.c.d_v, v);
+            if (lane == 0) R.arrive(full + stage);
+            fetch(t + 1);
         }
     }
 }
@@ -289,6 +298,8 @@ __device__ __forceinline__ void product_role(const PrefixArgs &P, const PrefixRo
         n += m;
     }
 }
+
+__device__ __forceinline__ float score_of(const uint32_t (&x)[4][32], int k) { return __uint_as_float(x[k / 32][k % 32]); }
 
 // ---- the rows: thread r of a stream owns row r of its 128
 template <typename T, int HD>
@@ -373,25 +384,28 @@ __device__ __forceinline__ bool rows_run(const PrefixArgs &P, const PrefixRoom &
         tmem_after_sync();
         if (any) {
             const int left = s.g.len - tile * kTok;
+            uint32_t x[4][32];                          // the row's scores
+#pragma unroll
+            for (int c = 0; c < 4; c++) tmem_ld32(score + 32 * c, x[c]);
+            // factor of each 16 tokens' scores; never 0, which times -infinity would be no number
+            auto factor = [&](int g) { return fmaxf(up * __shfl_sync(0xFFFFFFFFu, ks, g), 1.1754944e-38f); };
+#pragma unroll
+            for (int c = 0; c < 4; c++) tmem_wait_ld(x[c]);
+            if (left < kTok) {
+#pragma unroll
+                for (int k = 0; k < kTok; k++)
+                    if (k >= left) x[k / 32][k % 32] = 0xFF800000u;      // -infinity: weight 0
+            }
             float top = -INFINITY;
 #pragma unroll
-            for (int c = 0; c < 4; c++) {
-                uint32_t x[32];
-                tmem_ld32(score + 32 * c, x);
-                tmem_wait_ld(x);
+            for (int g = 0; g < 8; g++) {
+                float m0 = -INFINITY, m1 = -INFINITY;
 #pragma unroll
-                for (int h = 0; h < 2; h++) {
-                    const float f = up * __shfl_sync(0xFFFFFFFFu, ks, 2 * c + h), lv = __shfl_sync(0xFFFFFFFFu, my_lv, 2 * c + h);
-                    float m = -INFINITY;
-                    if (32 * c + 16 * h + 16 <= left) {
-#pragma unroll
-                        for (int k = 0; k < 16; k++) m = fmaxf(m, __uint_as_float(x[16 * h + k]));
-                    } else {
-#pragma unroll
-                        for (int k = 0; k < 16; k++) m = fmaxf(m, 32 * c + 16 * h + k < left ? __uint_as_float(x[16 * h + k]) : -INFINITY);
-                    }
-                    top = fmaxf(top, fmaf(m, f, lv));
+                for (int k = 0; k < 16; k += 4) {
+                    m0 = fmaxf(m0, fmaxf(score_of(x, 16 * g + k), score_of(x, 16 * g + k + 1)));
+                    m1 = fmaxf(m1, fmaxf(score_of(x, 16 * g + k + 2), score_of(x, 16 * g + k + 3)));
                 }
+                top = fmaxf(top, fmaf(fmaxf(m0, m1), factor(g), __shfl_sync(0xFFFFFFFFu, my_lv, g)));
             }
             // A new reference where a weight would pass 2^15; it brings the largest to 2^7, so that the next one is far off.
             if (__any_sync(0xFFFFFFFFu, __fsub_ru(top, kLift) > z)) {
@@ -401,41 +415,36 @@ __device__ __forceinline__ bool rows_run(const PrefixArgs &P, const PrefixRoom &
                 l *= a;
                 l32 *= a;
                 if (i > 0) {                            // this stream's products in front are done: their end came before the scores'
+#pragma unroll 1
+                    for (int c = 0; c < HD / 16; c++) {
+                        uint32_t o[16];
+                        tmem_ld16(value + 16 * c, o);
+                        tmem_wait_ld(o);
 #pragma unroll
-                    for (int c = 0; c < HD / 32; c++) {
-                        uint32_t x[32];
-                        tmem_ld32(value + 32 * c, x);
-                        tmem_wait_ld(x);
-#pragma unroll
-                        for (int k = 0; k < 32; k++) x[k] = __float_as_uint(__uint_as_float(x[k]) * a);
-                        tmem_st32(value + 32 * c, x);
+                        for (int k = 0; k < 16; k++) o[k] = __float_as_uint(__uint_as_float(o[k]) * a);
+                        tmem_st16(value + 16 * c, o);
                     }
                 }
             }
             const float ref = z == -INFINITY ? 0.f : z;
 #pragma unroll
             for (int c = 0; c < 4; c++) {
-                uint32_t x[32], p[16];
-                tmem_ld32(score + 32 * c, x);
-                tmem_wait_ld(x);
+                uint32_t w[16];
 #pragma unroll
                 for (int h = 0; h < 2; h++) {
-                    const float f = up * __shfl_sync(0xFFFFFFFFu, ks, 2 * c + h), lv = __shfl_sync(0xFFFFFFFFu, my_lv, 2 * c + h) - ref;
-                    const float iv = __shfl_sync(0xFFFFFFFFu, my_iv, 2 * c + h);
-                    float sum = 0.f;
+                    const int g = 2 * c + h;
+                    const float f = factor(g), shift = __shfl_sync(0xFFFFFFFFu, my_lv, g) - ref;
+                    float s0 = 0.f, s1 = 0.f;
 #pragma unroll
                     for (int k = 0; k < 16; k += 2) {
-                        float e0 = ex2(fmaf(__uint_as_float(x[16 * h + k]), f, lv)), e1 = ex2(fmaf(__uint_as_float(x[16 * h + k + 1]), f, lv));
-                        if (32 * c + 16 * h + 16 > left) {
-                            if (32 * c + 16 * h + k >= left) e0 = 0.f;
-                            if (32 * c + 16 * h + k + 1 >= left) e1 = 0.f;
-                        }
-                        sum += e0 + e1;
-                        p[8 * h + k / 2] = f16x2_of(e0, e1);
+                        const float e0 = ex2(fmaf(score_of(x, 16 * g + k), f, shift)), e1 = ex2(fmaf(score_of(x, 16 * g + k + 1), f, shift));
+                        s0 += e0;
+                        s1 += e1;
+                        w[8 * h + k / 2] = f16x2_of(e0, e1);
                     }
-                    l32 = fmaf(sum, iv, l32);
+                    l32 = fmaf(s0 + s1, __shfl_sync(0xFFFFFFFFu, my_iv, g), l32);
                 }
-                tmem_st16(score + 16 * c, p);           // over scores that have been read
+                tmem_st16(score + 16 * c, w);           // over scores that have been read
             }
             tmem_wait_st();
             if ((i & 31) == 31) {
@@ -512,8 +521,8 @@ __global__ void __launch_bounds__(kPrefixThreads, 1) prefix_kernel(const __grid_
     if (threadIdx.x == 0) {
         gave_up = 0;
         for (int i = 0; i < 2; i++) {
-            bar_init(R.bars + 8 * (B_KFULL + i), kWidenWarps);
-            bar_init(R.bars + 8 * (B_VFULL + i), kWidenWarps);
+            bar_init(R.bars + 8 * (B_KFULL + i), kWidenWarps / 2);
+            bar_init(R.bars + 8 * (B_VFULL + i), kWidenWarps / 2);
             bar_init(R.bars + 8 * (B_KEMPTY + i), 1);
             bar_init(R.bars + 8 * (B_VEMPTY + i), 1);
             bar_init(R.bars + 8 * (B_QFULL + i), 4);
@@ -531,11 +540,14 @@ __global__ void __launch_bounds__(kPrefixThreads, 1) prefix_kernel(const __grid_
     R.tmem = tmem_at;
     const Walk walk(total);
     if (warp < kSoftWarps) {
+        take_registers<kSoftRegs>();
         rows_role<T, HD>(P, R, walk, units, tasks);
     } else if (warp < kSoftWarps + kWidenWarps) {
+        leave_registers<kWidenRegs>();
         widen_role<HD>(P, R, walk, units, tasks);
     } else {
-        if ((threadIdx.x & 31) == 0) {
+        leave_registers<kProductRegs>();
+        if (threadIdx.x == 32 * (kSoftWarps + kWidenWarps)) {
             product_role<HD>(P, R, walk, units, tasks);
             // whatever was begun is done before the block gives its memory back
             mma_commit(R.bars + 8 * B_DRAIN);
