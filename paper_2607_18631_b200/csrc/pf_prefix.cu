@@ -152,6 +152,7 @@ template <int HD> struct PrefixShape {
     static constexpr int kOperand = kHalves * 16384;    // 128 rows of HD fp16
     static constexpr int kQ = 0, kK = 2 * kOperand, kV = 4 * kOperand, kBytes = 6 * kOperand;
 };
+constexpr uint32_t kTmem = 0;            // tensor memory: a block takes all 512 columns, which begin at 0
 // barriers, 8 bytes each
 enum { B_KFULL = 0, B_KEMPTY = 2, B_VFULL = 4, B_VEMPTY = 6, B_QFULL = 8, B_SFULL = 10, B_PFULL = 12, B_OFULL = 14, B_DRAIN = 16, B_COUNT = 17 };
 
@@ -163,7 +164,7 @@ __device__ __forceinline__ void sts128(uint32_t a, uint32_t x, uint32_t y, uint3
 }
 
 struct PrefixRoom {                     // what the roles share
-    uint32_t smem, bars, tmem;
+    uint32_t smem, bars;
     volatile int *gave_up;
     unsigned limit;
     __device__ __forceinline__ bool wait(int bar, unsigned parity) const { return bar_wait(bars + 8 * bar, parity & 1u, limit, gave_up); }
@@ -244,29 +245,41 @@ __device__ __forceinline__ void widen_role(const PrefixArgs &P, const PrefixRoom
     }
 }
 
-// ---- the products, by one thread.  Tensor memory: 128 columns of scores of either stream, which weights replace, then HD columns of values of either
+// ---- the products, by one warp, of which one thread issues them; the others go the same way, so that the operands' addresses are a warp's, not a thread's.
+// (With one thread going through all this, their computation took longer than the products.)
+// Tensor memory: 128 columns of scores of either stream, which weights replace, then HD columns of values of either
 template <int HD>
 __device__ __forceinline__ void product_role(const PrefixArgs &P, const PrefixRoom &R, Walk walk, const long long *units, const int *tasks)
 {
     using S = PrefixShape<HD>;
     constexpr uint32_t kScores = mma_shape(kTok, false), kValues = mma_shape(HD, true);
+    const uint32_t tmem = kTmem, smem = R.smem, bars = R.bars;
+    const bool one = elected();
     unsigned n = 0, runs = 0, weights[2] = {0, 0};      // tiles and stretches so far; each stream's tiles of weights
+    auto commit = [&](int bar) {
+        if (one) mma_commit(bars + 8 * bar);
+    };
     auto scores = [&](int j, int stage) {
-        const uint64_t q = operand_along(R.smem + S::kQ + j * S::kOperand), k = operand_along(R.smem + S::kK + stage * S::kOperand);
+        const uint32_t q = operand_along(smem + S::kQ + j * S::kOperand), k = operand_along(smem + S::kK + stage * S::kOperand), d = tmem + j * 128;
+        if (one) {
 #pragma unroll
-        for (int i = 0; i < HD / 16; i++) {
-            const uint32_t on = (i / 4) * 1024 + (i % 4) * 2;        // in 16 bytes
-            mma_shared(R.tmem + j * 128, q + on, k + on, kScores, i > 0);
+            for (int i = 0; i < HD / 16; i++) {
+                const uint32_t on = (i / 4) * 1024 + (i % 4) * 2;        // in 16 bytes
+                mma_shared(d, q + on, k + on, kScores, i > 0);
+            }
+            mma_commit(bars + 8 * (B_SFULL + j));
         }
-        mma_commit(R.bars + 8 * (B_SFULL + j));
     };
     auto values = [&](int j, int stage, bool first) {
-        const uint64_t v = operand_across(R.smem + S::kV + stage * S::kOperand, 16384u);
+        const uint32_t v = operand_across(smem + S::kV + stage * S::kOperand, 16384u), d = tmem + 256 + j * HD, w = tmem + j * 128;
+        if (one) {
 #pragma unroll
-        for (int i = 0; i < kTok / 16; i++) mma_tmem(R.tmem + 256 + j * HD, R.tmem + j * 128 + 8 * i, v + i * 128, kValues, !(first && i == 0));
+            for (int i = 0; i < kTok / 16; i++) mma_tmem(d, w + 8 * i, v + i * 128, kValues, i > 0 || !first);
+        }
     };
     auto weights_ready = [&](int j) {
-        if (!R.wait(B_PFULL + j, weights[j]++)) return false;
+        const unsigned turn = j ? weights[1]++ : weights[0]++;
+        if (!R.wait_warp(B_PFULL + j, turn)) return false;
         tmem_after_sync();
         return true;
     };
@@ -274,27 +287,27 @@ __device__ __forceinline__ void product_role(const PrefixArgs &P, const PrefixRo
     while (walk.next(P, units, tasks, s)) {
         const int m = s.end - s.tile;
         const bool turns = s.turns();
-        if (!R.wait(B_QFULL, runs) || !R.wait(B_QFULL + 1, runs)) return;
+        if (!R.wait_warp(B_QFULL, runs) || !R.wait_warp(B_QFULL + 1, runs)) return;
         runs++;
         const unsigned base = n;
         const int lag = turns ? 2 : 1;
         // step i: the scores of tile i, behind the values of the tile `lag` in front, whose weights lie where the scores go
         for (int i = 0; i < m + lag; i++) {
             const unsigned kt = base + i, vt = base + i - lag;
-            if (i < m && !R.wait(B_KFULL + (kt & 1), kt >> 1)) return;
-            if (i >= lag && !R.wait(B_VFULL + (vt & 1), vt >> 1)) return;
+            if (i < m && !R.wait_warp(B_KFULL + (kt & 1), kt >> 1)) return;
+            if (i >= lag && !R.wait_warp(B_VFULL + (vt & 1), vt >> 1)) return;
             for (int j = turns ? i & 1 : 0; j < (turns ? (i & 1) + 1 : 2); j++) {
                 if (i >= lag) {
                     if (!weights_ready(j)) return;
                     values(j, vt & 1, i < 2 * lag);
-                    if (i + lag >= m + lag) mma_commit(R.bars + 8 * (B_OFULL + j));
+                    if (i >= m) commit(B_OFULL + j);
                 }
                 if (i < m) scores(j, kt & 1);
             }
-            if (i >= lag) mma_commit(R.bars + 8 * (B_VEMPTY + (vt & 1)));
-            if (i < m) mma_commit(R.bars + 8 * (B_KEMPTY + (kt & 1)));
+            if (i >= lag) commit(B_VEMPTY + (vt & 1));
+            if (i < m) commit(B_KEMPTY + (kt & 1));
         }
-        if (turns && m == 1) mma_commit(R.bars + 8 * (B_OFULL + 1));      // a stream without a tile keeps step too
+        if (turns && m == 1) commit(B_OFULL + 1);       // a stream without a tile keeps step too
         n += m;
     }
 }
@@ -312,7 +325,7 @@ __device__ __forceinline__ bool rows_run(const PrefixArgs &P, const PrefixRoom &
     const bool live = at < s.g.rows;
     const bool any = s.row0 + (s.turns() ? 0 : 128 * j) + 32 * warp < s.g.rows;       // of the warp
     const int count = s.tiles_of(j);
-    const uint32_t lanes = (uint32_t)(32 * warp) << 16, score = R.tmem + lanes + j * 128, value = R.tmem + lanes + 256 + j * HD;
+    const uint32_t lanes = (uint32_t)(32 * warp) << 16, score = kTmem + lanes + j * 128, value = kTmem + lanes + 256 + j * HD;
     // The query row, as in the kernel of a sequence's own tokens: its largest finite element goes to [2^13, 2^14), and the power of two and the sign of
     // sm_scale to the factor of the scores.
     float up;
@@ -487,7 +500,7 @@ __device__ __forceinline__ void rows_role(const PrefixArgs &P, const PrefixRoom 
 #pragma unroll
             for (int c = 0; c < HD / 32; c++) {
                 uint32_t x[32];
-                tmem_ld32(R.tmem + ((uint32_t)(32 * warp) << 16) + 256 + j * HD + 32 * c, x);
+                tmem_ld32(kTmem + ((uint32_t)(32 * warp) << 16) + 256 + j * HD + 32 * c, x);
                 tmem_wait_ld(x);
                 if (live)
 #pragma unroll
@@ -517,7 +530,7 @@ __global__ void __launch_bounds__(kPrefixThreads, 1) prefix_kernel(const __grid_
     const long long total = units[P.n_groups];
     if (total == 0 || (int)blockIdx.x >= pieces_of(total, gridDim.x)) return;
     const int warp = threadIdx.x >> 5;
-    PrefixRoom R{smem_addr(room), smem_addr(bars), 0u, &gave_up, P.wait_limit};
+    PrefixRoom R{smem_addr(room), smem_addr(bars), &gave_up, P.wait_limit};
     if (threadIdx.x == 0) {
         gave_up = 0;
         for (int i = 0; i < 2; i++) {
@@ -537,7 +550,6 @@ __global__ void __launch_bounds__(kPrefixThreads, 1) prefix_kernel(const __grid_
     tmem_before_sync();
     __syncthreads();
     tmem_after_sync();
-    R.tmem = tmem_at;
     const Walk walk(total);
     if (warp < kSoftWarps) {
         take_registers<kSoftRegs>();
@@ -547,18 +559,18 @@ __global__ void __launch_bounds__(kPrefixThreads, 1) prefix_kernel(const __grid_
         widen_role<HD>(P, R, walk, units, tasks);
     } else {
         leave_registers<kProductRegs>();
-        if (threadIdx.x == 32 * (kSoftWarps + kWidenWarps)) {
+        if (warp == kSoftWarps + kWidenWarps) {
             product_role<HD>(P, R, walk, units, tasks);
             // whatever was begun is done before the block gives its memory back
-            mma_commit(R.bars + 8 * B_DRAIN);
+            __syncwarp();
+            if (elected()) mma_commit(R.bars + 8 * B_DRAIN);
             int alone = 0;
             bar_wait(R.bars + 8 * B_DRAIN, 0, kDrainLimit, &alone);
         }
-        __syncwarp();
     }
     tmem_before_sync();
     __syncthreads();
-    if (warp == kSoftWarps + kWidenWarps) tmem_free(R.tmem, 512);
+    if (warp == kSoftWarps + kWidenWarps) tmem_free(tmem_at, 512);
 }
 
 // ------------------------------------------------------------------ the join

@@ -76,24 +76,29 @@ __device__ __forceinline__ void tmem_st16(uint32_t addr, const uint32_t (&r)[16]
 // Operands in shared memory are rows of 128 bytes, eight of them 1024, whose 16-byte chunks are permuted by the row's number (chunk ^ (row & 7)), at
 // addresses that are multiples of 1024.  Either the summed index runs along a row (64 elements; a step of 16 is 32 bytes on), or the
 // rows are the summed index (`across`: 64 columns of B a row; a step of 16 is 2048 bytes on; the next 64 columns are `apart` bytes on).
-__device__ __forceinline__ uint64_t operand_along(uint32_t addr)
-{
-    return (uint64_t)((addr & 0x3FFFF) >> 4) | (uint64_t)1 << 16 | (uint64_t)(1024 >> 4) << 32 | (uint64_t)1 << 46 | (uint64_t)2 << 61;
-}
-__device__ __forceinline__ uint64_t operand_across(uint32_t addr, uint32_t apart)
-{
-    return (uint64_t)((addr & 0x3FFFF) >> 4) | (uint64_t)(apart >> 4) << 16 | (uint64_t)(1024 >> 4) << 32 | (uint64_t)1 << 46 | (uint64_t)2 << 61;
-}
+// A descriptor's lower word holds the address and `apart`, in 16 bytes; its upper word is the same for all.
+__device__ __forceinline__ uint32_t operand_along(uint32_t addr) { return ((addr & 0x3FFFF) >> 4) | 1u << 16; }
+__device__ __forceinline__ uint32_t operand_across(uint32_t addr, uint32_t apart) { return ((addr & 0x3FFFF) >> 4) | (apart >> 4) << 16; }
+constexpr uint32_t kOperandHigh = (1024u >> 4) | 1u << 14 | 2u << 29;      // eight rows on: 1024 bytes; version 1; chunks permuted within 128 bytes
 __host__ __device__ constexpr uint32_t mma_shape(int n, bool b_across) { return 1u << 4 | (b_across ? 1u << 16 : 0u) | (uint32_t)(n / 8) << 17 | (uint32_t)(128 / 16) << 24; }
 // by one thread; `add`: 0 sets D
-__device__ __forceinline__ void mma_shared(uint32_t d, uint64_t a, uint64_t b, uint32_t shape, uint32_t add)
+__device__ __forceinline__ void mma_shared(uint32_t d, uint32_t a, uint32_t b, uint32_t shape, uint32_t add)
 {
-    asm volatile("{\n.reg .pred p;\nsetp.ne.b32 p, %4, 0;\ntcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}" ::"r"(d), "l"(a), "l"(b), "r"(shape), "r"(add) : "memory");
+    asm volatile("{\n.reg .pred p;\n.reg .b64 a, b;\nsetp.ne.b32 p, %4, 0;\nmov.b64 a, {%1, %5};\nmov.b64 b, {%2, %5};\n"
+                 "tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %3, p;\n}" ::"r"(d), "r"(a), "r"(b), "r"(shape), "r"(add), "r"(kOperandHigh) : "memory");
 }
 // A from tensor memory: a lane a row, 16 elements in 8 columns
-__device__ __forceinline__ void mma_tmem(uint32_t d, uint32_t a, uint64_t b, uint32_t shape, uint32_t add)
+__device__ __forceinline__ void mma_tmem(uint32_t d, uint32_t a, uint32_t b, uint32_t shape, uint32_t add)
 {
-    asm volatile("{\n.reg .pred p;\nsetp.ne.b32 p, %4, 0;\ntcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}" ::"r"(d), "r"(a), "l"(b), "r"(shape), "r"(add) : "memory");
+    asm volatile("{\n.reg .pred p;\n.reg .b64 b;\nsetp.ne.b32 p, %4, 0;\nmov.b64 b, {%2, %5};\n"
+                 "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], b, %3, p;\n}" ::"r"(d), "r"(a), "r"(b), "r"(shape), "r"(add), "r"(kOperandHigh) : "memory");
+}
+// one lane of a whole warp, the same one each time
+__device__ __forceinline__ bool elected()
+{
+    uint32_t yes;
+    asm volatile("{\n.reg .pred p;\nelect.sync _|p, 0xFFFFFFFF;\nselp.u32 %0, 1, 0, p;\n}" : "=r"(yes));
+    return yes;
 }
 // the barrier gets an arrival when all of this thread's matrix instructions so far are done
 __device__ __forceinline__ void mma_commit(uint32_t bar)
