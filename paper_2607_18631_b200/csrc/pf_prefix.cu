@@ -141,9 +141,9 @@ struct Walk {
 };
 
 // Four groups of four warps: two streams that own the rows, one that brings the cache's bytes, and one of which a thread issues the products.  Registers go
-// where they are needed: 256 x 184 + 128 x 104 + 128 x 40 = 512 x 128, what the block is launched with.
+// where they are needed: 256 x 184 + 128 x 96 + 128 x 48 = 512 x 128, what the block is launched with.
 constexpr int kSoftWarps = 8, kWidenWarps = 4;
-constexpr int kPrefixThreads = 512, kSoftRegs = 184, kWidenRegs = 104, kProductRegs = 40;
+constexpr int kPrefixThreads = 512, kSoftRegs = 184, kWidenRegs = 96, kProductRegs = 48;
 static_assert(kSoftRegs * 256 + kWidenRegs * 128 + kProductRegs * 128 <= kPrefixThreads * 128, "no group waits for registers that nobody gives back");
 template <int N> __device__ __forceinline__ void take_registers() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N)); }
 template <int N> __device__ __forceinline__ void leave_registers() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N)); }
@@ -154,7 +154,7 @@ template <int HD> struct PrefixShape {
 };
 constexpr uint32_t kTmem = 0;            // tensor memory: a block takes all 512 columns, which begin at 0
 // barriers, 8 bytes each
-enum { B_KFULL = 0, B_KEMPTY = 2, B_VFULL = 4, B_VEMPTY = 6, B_QFULL = 8, B_SFULL = 10, B_PFULL = 12, B_OFULL = 14, B_DRAIN = 16, B_COUNT = 17 };
+enum { B_KFULL = 0, B_KEMPTY = 2, B_VFULL = 4, B_VEMPTY = 6, B_QFULL = 8, B_SFULL = 10, B_PFULL = 12, B_OFULL = 14, B_PHALF = 16, B_DRAIN = 18, B_COUNT = 19 };
 
 // 16-byte chunk c of row r of an operand's 128-byte column
 __device__ __forceinline__ uint32_t operand_at(int r, int c) { return (uint32_t)(r * 128 + ((c ^ (r & 7)) << 4)); }
@@ -193,15 +193,48 @@ __device__ __forceinline__ void widen_role(const PrefixArgs &P, const PrefixRoom
     while (walk.next(P, units, tasks, s)) {
         const int32_t *row = P.ptable + (int64_t)s.group * P.pcols;
         uint4 x[N];
-        int page;                                       // lane i < 8: page of the i-th 16 tokens of the next tile, negative: none
-        auto find = [&](int tile) {
+        auto page_of = [&](int tile) {                  // lane i < 8: page of the tile's i-th 16 tokens, negative: none
             const int tok = tile * kTok + 16 * lane;
-            page = lane < 8 && tile < s.end && tok < s.g.len ? row[tok >> page_log2] : -1;
+            return lane < 8 && tile < s.end && tok < s.g.len ? row[tok >> page_log2] : -1;
         };
-        auto fetch = [&](int tile) {
-            const int64_t at = page < 0 || page >= A.c.n_pages ? -1 : (((int64_t)page * A.c.n_kv + s.kv) * A.c.page + ((16 * lane) & (A.c.page - 1))) * HD;
-            const int left = s.g.len - tile * kTok - r0;
-            if (__all_sync(0xFFFFFFFFu, (at >= 0 || lane >= 8) && left >= kTok)) {
+        auto place_of = [&](int page) {                 // and where they begin in the cache, negative: nowhere
+            return page < 0 || page >= A.c.n_pages ? (int64_t)-1 : (((int64_t)page * A.c.n_kv + s.kv) * A.c.page + ((16 * lane) & (A.c.page - 1))) * HD;
+        };
+        auto load = [&](const uint8_t *src, bool there) { return there ? __ldg(reinterpret_cast<const uint4 *>(src)) : make_uint4(0u, 0u, 0u, 0u); };
+        int64_t at = place_of(page_of(s.tile));
+        int left = s.g.len - s.tile * kTok - r0;
+#pragma unroll
+        for (int g = 0; g < 8; g++) {
+            const int64_t base = __shfl_sync(0xFFFFFFFFu, at, g);
+#pragma unroll
+            for (int i = 0; i < PER16; i++) x[g * PER16 + i] = load(from + base + i * 2 * ROWS * HD, base >= 0 && (g * PER16 + i) * 2 * ROWS < left);
+        }
+        int page = page_of(s.tile + 1);
+        for (int t = s.tile; t < s.end; t++, n++) {
+            const int stage = n & 1;
+            at = place_of(page);
+            left -= kTok;
+            const bool whole = __all_sync(0xFFFFFFFFu, (at >= 0 || lane >= 8) && left >= kTok);      // of the next tile
+            page = page_of(t + 2);
+            if (!R.wait_warp(empty + stage, ((n >> 1) & 1u) ^ 1u)) return;
+#pragma unroll
+            for (int g = 0; g < 8; g++) {
+#pragma unroll
+                for (int i = g * PER16; i < (g + 1) * PER16; i++) {
+                    uint32_t h[8];
+                    widen4(x[i].x, h[0], h[1]);
+                    widen4(x[i].y, h[2], h[3]);
+                    widen4(x[i].z, h[4], h[5]);
+                    widen4(x[i].w, h[6], h[7]);
+                    const uint32_t on = stage * S::kOperand + i * 2 * ROWS * 128;
+                    sts128(to0 + on, h[0], h[1], h[2], h[3]);
+                    sts128(to1 + on, h[4], h[5], h[6], h[7]);
+                }
+            }
+            publish_shared();
+            __syncwarp();
+            if (lane == 0) R.arrive(full + stage);
+            if (whole) {
 #pragma unroll
                 for (int g = 0; g < 8; g++) {
                     const uint8_t *src = from + __shfl_sync(0xFFFFFFFFu, at, g);
@@ -213,34 +246,9 @@ __device__ __forceinline__ void widen_role(const PrefixArgs &P, const PrefixRoom
                 for (int g = 0; g < 8; g++) {
                     const int64_t base = __shfl_sync(0xFFFFFFFFu, at, g);
 #pragma unroll
-                    for (int i = 0; i < PER16; i++) {
-                        const bool there = base >= 0 && (g * PER16 + i) * 2 * ROWS < left;
-                        x[g * PER16 + i] = there ? __ldg(reinterpret_cast<const uint4 *>(from + base + i * 2 * ROWS * HD)) : make_uint4(0u, 0u, 0u, 0u);
-                    }
+                    for (int i = 0; i < PER16; i++) x[g * PER16 + i] = load(from + base + i * 2 * ROWS * HD, base >= 0 && (g * PER16 + i) * 2 * ROWS < left);
                 }
             }
-        };
-        find(s.tile);
-        fetch(s.tile);
-        for (int t = s.tile; t < s.end; t++, n++) {
-            const int stage = n & 1;
-            find(t + 1);
-            if (!R.wait_warp(empty + stage, ((n >> 1) & 1u) ^ 1u)) return;
-#pragma unroll
-            for (int i = 0; i < N; i++) {
-                uint32_t h[8];
-                widen4(x[i].x, h[0], h[1]);
-                widen4(x[i].y, h[2], h[3]);
-                widen4(x[i].z, h[4], h[5]);
-                widen4(x[i].w, h[6], h[7]);
-                const uint32_t on = stage * S::kOperand + i * 2 * ROWS * 128;
-                sts128(to0 + on, h[0], h[1], h[2], h[3]);
-                sts128(to1 + on, h[4], h[5], h[6], h[7]);
-            }
-            publish_shared();
-            __syncwarp();
-            if (lane == 0) R.arrive(full + stage);
-            fetch(t + 1);
         }
     }
 }
@@ -270,17 +278,22 @@ __device__ __forceinline__ void product_role(const PrefixArgs &P, const PrefixRo
             mma_commit(bars + 8 * (B_SFULL + j));
         }
     };
+    // a stream's values, as soon as either half of its weights is there
     auto values = [&](int j, int stage, bool first) {
         const uint32_t v = operand_across(smem + S::kV + stage * S::kOperand, 16384u), d = tmem + 256 + j * HD, w = tmem + j * 128;
+        const unsigned turn = j ? weights[1]++ : weights[0]++;
+        if (!R.wait_warp(B_PHALF + j, turn)) return false;
+        tmem_after_sync();
         if (one) {
 #pragma unroll
-            for (int i = 0; i < kTok / 16; i++) mma_tmem(d, w + 8 * i, v + i * 128, kValues, i > 0 || !first);
+            for (int i = 0; i < kTok / 32; i++) mma_tmem(d, w + 8 * i, v + i * 128, kValues, i > 0 || !first);
         }
-    };
-    auto weights_ready = [&](int j) {
-        const unsigned turn = j ? weights[1]++ : weights[0]++;
         if (!R.wait_warp(B_PFULL + j, turn)) return false;
         tmem_after_sync();
+        if (one) {
+#pragma unroll
+            for (int i = kTok / 32; i < kTok / 16; i++) mma_tmem(d, w + 8 * i, v + i * 128, kValues, 1);
+        }
         return true;
     };
     Stretch s;
@@ -298,8 +311,7 @@ __device__ __forceinline__ void product_role(const PrefixArgs &P, const PrefixRo
             if (i >= lag && !R.wait_warp(B_VFULL + (vt & 1), vt >> 1)) return;
             for (int j = turns ? i & 1 : 0; j < (turns ? (i & 1) + 1 : 2); j++) {
                 if (i >= lag) {
-                    if (!weights_ready(j)) return;
-                    values(j, vt & 1, i < 2 * lag);
+                    if (!values(j, vt & 1, i < 2 * lag)) return;
                     if (i >= m) commit(B_OFULL + j);
                 }
                 if (i < m) scores(j, kt & 1);
@@ -312,7 +324,39 @@ __device__ __forceinline__ void product_role(const PrefixArgs &P, const PrefixRo
     }
 }
 
-__device__ __forceinline__ float score_of(const uint32_t (&x)[4][32], int k) { return __uint_as_float(x[k / 32][k % 32]); }
+// ---- two fp32 numbers at a time: half the instructions
+struct Two { uint64_t v; };
+__device__ __forceinline__ Two two(float lo, float hi) { Two r; asm("mov.b64 %0, {%1, %2};" : "=l"(r.v) : "f"(lo), "f"(hi)); return r; }
+__device__ __forceinline__ void apart(Two a, float &lo, float &hi) { asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(a.v)); }
+__device__ __forceinline__ Two fma2(Two a, Two b, Two c) { Two r; asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.v) : "l"(a.v), "l"(b.v), "l"(c.v)); return r; }
+__device__ __forceinline__ Two add2(Two a, Two b) { Two r; asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v)); return r; }
+// 2^a without the special-function unit, which computes 16 a cycle and SM where a tile asks for 16384: a = n + f, n whole, |f| <= 1/2, and the
+// polynomial of degree 4 that is nearest to 2^f there (relative error 2.6e-6, found by exchange).  Below 2^-126 (-infinity): 2^-126.  No NaN comes out.
+__device__ __forceinline__ void pow2_two(Two a, float &lo, float &hi)
+{
+    float x, y;
+    apart(a, x, y);
+    a = two(fmaxf(x, -126.f), fmaxf(y, -126.f));
+    const float big = 12582912.f;                       // 1.5 * 2^23: what is added to it is rounded to a whole number
+    const Two m = add2(a, two(big, big)), n = add2(m, two(-big, -big)), f = fma2(n, two(-1.f, -1.f), a);
+    Two r = fma2(f, two(0.009570102207362652f, 0.009570102207362652f), two(0.05591785907745361f, 0.05591785907745361f));
+    r = fma2(r, f, two(0.240247443318367f, 0.240247443318367f));
+    r = fma2(r, f, two(0.6931217908859253f, 0.6931217908859253f));
+    r = fma2(r, f, two(0.9999992847442627f, 0.9999992847442627f));
+    float mx, my;
+    apart(m, mx, my);
+    apart(r, x, y);
+    lo = __uint_as_float(__float_as_uint(x) + (__float_as_uint(mx) << 23));
+    hi = __uint_as_float(__float_as_uint(y) + (__float_as_uint(my) << 23));
+}
+// largest of three, NaN if one of them is
+__device__ __forceinline__ float max3(float a, float b, float c)
+{
+    float r;
+    asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+    return r;
+}
+__device__ __forceinline__ float score_of(const uint32_t (&x)[8][16], int k) { return __uint_as_float(x[k / 16][k % 16]); }
 
 // ---- the rows: thread r of a stream owns row r of its 128
 template <typename T, int HD>
@@ -397,29 +441,34 @@ __device__ __forceinline__ bool rows_run(const PrefixArgs &P, const PrefixRoom &
         tmem_after_sync();
         if (any) {
             const int left = s.g.len - tile * kTok;
-            uint32_t x[4][32];                          // the row's scores
+            uint32_t x[8][16];                          // the row's scores
 #pragma unroll
-            for (int c = 0; c < 4; c++) tmem_ld32(score + 32 * c, x[c]);
+            for (int c = 0; c < 8; c++) tmem_ld16(score + 16 * c, x[c]);
             // factor of each 16 tokens' scores; never 0, which times -infinity would be no number
             auto factor = [&](int g) { return fmaxf(up * __shfl_sync(0xFFFFFFFFu, ks, g), 1.1754944e-38f); };
 #pragma unroll
-            for (int c = 0; c < 4; c++) tmem_wait_ld(x[c]);
+            for (int c = 0; c < 8; c++) tmem_wait_ld(x[c]);
             if (left < kTok) {
 #pragma unroll
                 for (int k = 0; k < kTok; k++)
-                    if (k >= left) x[k / 32][k % 32] = 0xFF800000u;      // -infinity: weight 0
+                    if (k >= left) x[k / 16][k % 16] = 0xFF800000u;      // -infinity: weight 0
             }
             float top = -INFINITY;
 #pragma unroll
             for (int g = 0; g < 8; g++) {
-                float m0 = -INFINITY, m1 = -INFINITY;
+                float m0 = score_of(x, 16 * g), m1 = score_of(x, 16 * g + 1);
 #pragma unroll
-                for (int k = 0; k < 16; k += 4) {
-                    m0 = fmaxf(m0, fmaxf(score_of(x, 16 * g + k), score_of(x, 16 * g + k + 1)));
-                    m1 = fmaxf(m1, fmaxf(score_of(x, 16 * g + k + 2), score_of(x, 16 * g + k + 3)));
+                for (int k = 2; k < 14; k += 4) {
+                    m0 = max3(m0, score_of(x, 16 * g + k), score_of(x, 16 * g + k + 1));
+                    m1 = max3(m1, score_of(x, 16 * g + k + 2), score_of(x, 16 * g + k + 3));
                 }
-                top = fmaxf(top, fmaf(fmaxf(m0, m1), factor(g), __shfl_sync(0xFFFFFFFFu, my_lv, g)));
+                m0 = max3(m0, m1, score_of(x, 16 * g + 14));
+                m0 = max3(m0, m0, score_of(x, 16 * g + 15));
+                const float most = fmaf(m0, factor(g), __shfl_sync(0xFFFFFFFFu, my_lv, g));
+                top = max3(top, top, most);
             }
+            // a score that is no number, or infinite, makes the row NaN, whichever way its weight is computed
+            if (!(top < INFINITY)) l = __int_as_float(0x7FC00000);
             // A new reference where a weight would pass 2^15; it brings the largest to 2^7, so that the next one is far off.
             if (__any_sync(0xFFFFFFFFu, __fsub_ru(top, kLift) > z)) {
                 const float n = __fsub_ru(top, kLift) > z ? __fsub_ru(top, kSetLift) : z;
@@ -447,23 +496,41 @@ __device__ __forceinline__ bool rows_run(const PrefixArgs &P, const PrefixRoom &
                 for (int h = 0; h < 2; h++) {
                     const int g = 2 * c + h;
                     const float f = factor(g), shift = __shfl_sync(0xFFFFFFFFu, my_lv, g) - ref;
-                    float s0 = 0.f, s1 = 0.f;
+                    const Two ff = two(f, f), ss = two(shift, shift);
+                    Two sum = two(0.f, 0.f);
 #pragma unroll
-                    for (int k = 0; k < 16; k += 2) {
-                        const float e0 = ex2(fmaf(score_of(x, 16 * g + k), f, shift)), e1 = ex2(fmaf(score_of(x, 16 * g + k + 1), f, shift));
-                        s0 += e0;
-                        s1 += e1;
-                        w[8 * h + k / 2] = f16x2_of(e0, e1);
+                    for (int k = 0; k < 8; k++) {
+                        const Two a = fma2(two(score_of(x, 16 * g + 2 * k), score_of(x, 16 * g + 2 * k + 1)), ff, ss);
+                        float e0, e1;
+                        if (k % 4 == 3) {               // a quarter: the special-function unit and the others take about as long
+                            pow2_two(a, e0, e1);
+                        } else {
+                            apart(a, e0, e1);
+                            e0 = ex2(e0);
+                            e1 = ex2(e1);
+                        }
+                        sum = add2(sum, two(e0, e1));
+                        w[8 * h + k] = f16x2_of(e0, e1);
                     }
+                    float s0, s1;
+                    apart(sum, s0, s1);
                     l32 = fmaf(s0 + s1, __shfl_sync(0xFFFFFFFFu, my_iv, g), l32);
                 }
                 tmem_st16(score + 16 * c, w);           // over scores that have been read
+                if (c == 1) {                           // half of the weights: their products may begin
+                    tmem_wait_st();
+                    tmem_before_sync();
+                    __syncwarp();
+                    if (lane == 0) R.arrive(B_PHALF + j);
+                }
             }
             tmem_wait_st();
             if ((i & 31) == 31) {
                 l += l32;
                 l32 = 0.f;
             }
+        } else if (lane == 0) {
+            R.arrive(B_PHALF + j);
         }
         tmem_before_sync();
         __syncwarp();
@@ -541,6 +608,7 @@ __global__ void __launch_bounds__(kPrefixThreads, 1) prefix_kernel(const __grid_
             bar_init(R.bars + 8 * (B_QFULL + i), 4);
             bar_init(R.bars + 8 * (B_SFULL + i), 1);
             bar_init(R.bars + 8 * (B_PFULL + i), 4);
+            bar_init(R.bars + 8 * (B_PHALF + i), 4);
             bar_init(R.bars + 8 * (B_OFULL + i), 1);
         }
         bar_init(R.bars + 8 * B_DRAIN, 1);
