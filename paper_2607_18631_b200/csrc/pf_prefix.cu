@@ -16,6 +16,7 @@ namespace pf {
 constexpr int kRows = 256;               // rows of a task
 constexpr int kTok = 128;                // tokens of a tile
 constexpr int kMostTiles = 512;          // tiles of a piece at most: 32-bit sums do not run over more than 65536 tokens
+constexpr int kAhead = 4;                // tiles that are under way from HBM to the L2
 constexpr int kLeastTiles = 4;           // a piece takes no fewer while others have none
 constexpr unsigned kWaitLimit = 500000, kDrainLimit = 500000;      // polls of 2 us: a second
 constexpr float kSetLift = 7.f;          // log2 of the largest weight when a row's reference is set; it may grow to kLift
@@ -26,6 +27,7 @@ struct PrefixArgs {
     int n_groups, pcols;
     unsigned wait_limit;                 // polls of a wait inside the kernel
     long long n_slots;
+    uint32_t *status;                    // [blocks], written by those with work
     float *slots;                        // [n_slots] x (kRows x HD values, kRows references, kRows sums)
 };
 
@@ -45,11 +47,11 @@ __device__ __forceinline__ Group group_of(const PrefixArgs &P, int g)
     return r;
 }
 
-// Tiles and tasks of the groups in front of each group, by the whole block.  units, tasks: n_groups + 1 words
-__device__ __forceinline__ void group_prefix(const PrefixArgs &P, long long *units, int *tasks)
+// Tiles and tasks of the groups in front of each group, by the whole block.  units, tasks: n_groups + 1 words; scratch: 100
+__device__ __forceinline__ void group_prefix(const PrefixArgs &P, long long *units, int *tasks, int *scratch)
 {
-    __shared__ long long warp_units[32];
-    __shared__ int warp_tasks[32];
+    int *warp_tasks = scratch;
+    long long *warp_units = reinterpret_cast<long long *>(scratch + 32 + ((uintptr_t)scratch & 4 ? 1 : 0));
     const int nt = blockDim.x, tid = threadIdx.x, lane = tid & 31, nw = (nt + 31) >> 5;
     long long base_u = 0;
     int base_t = 0;
@@ -90,6 +92,8 @@ __device__ __forceinline__ int pieces_of(long long total, int blocks)
     const long long per = (total + (long long)blocks * kMostTiles - 1) / ((long long)blocks * kMostTiles);
     return (int)(per * blocks);
 }
+// pieces of a block, which follow one another
+__device__ __forceinline__ int pieces_each(int n_pieces, int blocks) { return (n_pieces + blocks - 1) / blocks; }
 // the last entry of a rising list of n + 1 words whose value is at most x
 template <typename V>
 __device__ __forceinline__ int last_at(const V *list, int n, V x)
@@ -102,45 +106,20 @@ __device__ __forceinline__ int last_at(const V *list, int n, V x)
     return lo;
 }
 
-// A stretch of tiles [tile, end) of one task
-struct Stretch {
-    Group g;
-    int group, kv, row0, rows;           // the task's rows are row0 .. row0 + rows - 1 of the group
-    int tile, end;
+// A stretch of tiles [tile, end) of one task: what the roles of a block work on together
+struct __align__(16) Stretch {
+    int group, first, members, len;      // the group, its first sequence, its rows, and its tokens
+    int kv, row0, rows, tile;            // the task's rows are row0 .. row0 + rows - 1 of the group
+    int end, pad;                        // (end = tile: there are no more)
     long long slot;
     // few rows: both streams go through the same rows, and take turns with the tiles
     __device__ __forceinline__ bool turns() const { return rows <= 128; }
     __device__ __forceinline__ int tiles_of(int stream) const { return turns() ? (end - tile + 1 - stream) / 2 : end - tile; }
 };
-// the stretches of this block's pieces, one behind the other
-struct Walk {
-    long long total, u, u_end;
-    int n_pieces, piece;
-    __device__ __forceinline__ Walk(long long all) : total(all), u(0), u_end(0), n_pieces(pieces_of(all, gridDim.x)), piece((int)blockIdx.x - (int)gridDim.x) {}
-    __device__ __forceinline__ bool next(const PrefixArgs &P, const long long *units, const int *tasks, Stretch &s)
-    {
-        if (u >= u_end) {
-            piece += gridDim.x;
-            if (piece >= n_pieces) return false;
-            u = first_tile(total, n_pieces, piece);
-            u_end = first_tile(total, n_pieces, piece + 1);
-        }
-        s.group = last_at(units, P.n_groups, u);
-        s.g = group_of(P, s.group);
-        const long long r = u - units[s.group];
-        const int no = (int)(r / s.g.tiles);
-        s.tile = (int)(r - (long long)no * s.g.tiles);
-        s.end = (int)min((long long)s.g.tiles, s.tile + (u_end - u));
-        s.kv = no / s.g.row_tiles;
-        s.row0 = (no - s.kv * s.g.row_tiles) * kRows;
-        s.rows = min(kRows, s.g.rows - s.row0);
-        s.slot = (long long)tasks[s.group] + no + piece;
-        u += s.end - s.tile;
-        return true;
-    }
-};
+static_assert(sizeof(Stretch) == 48, "as the roles read it");
 
-// Four groups of four warps: two streams that own the rows, one that brings the cache's bytes, and one of which a thread issues the products.  Registers go
+// Four groups of four warps: two streams that own the rows, one that widens the cache's bytes, and one of which a warp issues the products, two copy from the cache and one
+// plans.  Registers go
 // where they are needed: 256 x 184 + 128 x 96 + 128 x 48 = 512 x 128, what the block is launched with.
 constexpr int kSoftWarps = 8, kWidenWarps = 4;
 constexpr int kPrefixThreads = 512, kSoftRegs = 184, kWidenRegs = 96, kProductRegs = 48;
@@ -150,11 +129,17 @@ template <int N> __device__ __forceinline__ void leave_registers() { asm volatil
 template <int HD> struct PrefixShape {
     static constexpr int kHalves = HD / 64;             // 128-byte columns of an fp16 row
     static constexpr int kOperand = kHalves * 16384;    // 128 rows of HD fp16
-    static constexpr int kQ = 0, kK = 2 * kOperand, kV = 4 * kOperand, kBytes = 6 * kOperand;
+    static constexpr int kQ = 0, kK = 2 * kOperand, kV = 4 * kOperand;
+    static constexpr int kRing = 6 * kOperand;          // bytes of the cache under way: a tile of keys and one of values
+    static constexpr int kScales = kRing + 2 * kTok * HD;        // of eight tiles, for each 16 tokens: key scale, log2 and inverse of the value scale
+    static constexpr int kHave = kScales + 8 * 128;     // which runs of a half tile were copied, of keys and of values
+    static constexpr int kPlan = kHave + 16;     // two stretches
+    static constexpr int kBars = kPlan + 2 * 48, kBytes = kBars + 288;
+    static_assert(kBytes <= 227 * 1024, "fits an SM");
 };
 constexpr uint32_t kTmem = 0;            // tensor memory: a block takes all 512 columns, which begin at 0
 // barriers, 8 bytes each
-enum { B_KFULL = 0, B_KEMPTY = 2, B_VFULL = 4, B_VEMPTY = 6, B_QFULL = 8, B_SFULL = 10, B_PFULL = 12, B_OFULL = 14, B_PHALF = 16, B_DRAIN = 18, B_COUNT = 19 };
+enum { B_KFULL = 0, B_KEMPTY = 2, B_VFULL = 4, B_VEMPTY = 6, B_QFULL = 8, B_SFULL = 10, B_PHALF = 12, B_PFULL = 14, B_OFULL = 16, B_DRAIN = 18, B_KRAW = 19, B_VRAW = 21, B_KREAD = 23, B_VREAD = 25, B_PLAN = 27, B_DONE = 29, B_COUNT = 31 };
 
 // 16-byte chunk c of row r of an operand's 128-byte column
 __device__ __forceinline__ uint32_t operand_at(int r, int c) { return (uint32_t)(r * 128 + ((c ^ (r & 7)) << 4)); }
@@ -164,91 +149,229 @@ __device__ __forceinline__ void sts128(uint32_t a, uint32_t x, uint32_t y, uint3
 }
 
 struct PrefixRoom {                     // what the roles share
-    uint32_t smem, bars;
-    volatile int *gave_up;
+    uint32_t smem, bars, gave_up;
     unsigned limit;
+    int run_log2;
     __device__ __forceinline__ bool wait(int bar, unsigned parity) const { return bar_wait(bars + 8 * bar, parity & 1u, limit, gave_up); }
     __device__ __forceinline__ bool wait_warp(int bar, unsigned parity) const { return __all_sync(0xFFFFFFFFu, wait(bar, parity)); }      // one answer for all lanes
     __device__ __forceinline__ void arrive(int bar) const { bar_arrive(bars + 8 * bar); }
+    // the run-th stretch, by a whole warp, which says done() of it afterwards; false: there is none
+    __device__ __forceinline__ bool next(const Stretch *plan, unsigned run, Stretch &s) const
+    {
+        if (!wait_warp(B_PLAN + (run & 1), run >> 1)) return false;
+        s = plan[run & 1];
+        return s.end > s.tile;
+    }
+    __device__ __forceinline__ void done(unsigned run) const
+    {
+        __syncwarp();
+        if ((threadIdx.x & 31) == 0) arrive(B_DONE + (run & 1));
+    }
 };
 
-// ---- the cache's bytes -> fp16 operands.  Two warps bring keys, two bring values; a thread holds the 16-byte pieces of a whole tile that it asked for when
-// it had widened those of the one in front.  Eight neighbouring lanes have four pieces of each of two rows, so that their stores meet no bank twice.
+// ---- one thread finds the block's stretches, one ahead: pieces follow one another, so where the first begins is looked up once (`units`, `tasks`: before the others
+// overwrite them), and from there it goes on by itself
+struct Walk {
+    Group g;
+    int group, task, no, tile, piece, last, n_pieces;   // task: number of the group's first
+    long long total;
+    __device__ __forceinline__ bool begin(const PrefixArgs &P, const long long *units, const int *tasks)
+    {
+        total = units[P.n_groups];
+        n_pieces = total ? pieces_of(total, gridDim.x) : 0;
+        const int per = pieces_each(n_pieces, gridDim.x);
+        piece = blockIdx.x * per;
+        last = min(n_pieces, piece + per);
+        if (piece >= last) return false;
+        const long long u = first_tile(total, n_pieces, piece);
+        group = last_at(units, P.n_groups, u);
+        g = group_of(P, group);
+        task = tasks[group];
+        no = (int)((u - units[group]) / g.tiles);
+        tile = (int)((u - units[group]) - (long long)no * g.tiles);
+        return true;
+    }
+};
+__device__ __forceinline__ void plan_role(const PrefixArgs &P, const PrefixRoom &R, Walk k, Stretch *plan)
+{
+    unsigned run = 0;
+    auto room = [&]() { return R.wait(B_DONE + (run & 1), (run >> 1) ^ 1u); };
+    for (; k.piece < k.last; k.piece++) {
+        int left = (int)(first_tile(k.total, k.n_pieces, k.piece + 1) - first_tile(k.total, k.n_pieces, k.piece));
+        while (left > 0) {
+            while (k.no >= (k.g.tiles ? k.g.row_tiles * P.a.c.n_kv : 0)) {
+                if (k.g.tiles) k.task += k.g.row_tiles * P.a.c.n_kv;
+                k.no = 0;
+                if (++k.group >= P.n_groups) return;    // (not reached: the list ends with the last piece)
+                k.g = group_of(P, k.group);
+            }
+            Stretch s;
+            s.group = k.group; s.first = k.g.first; s.members = k.g.rows; s.len = k.g.len;
+            s.kv = k.no / k.g.row_tiles;
+            s.row0 = (k.no - s.kv * k.g.row_tiles) * kRows;
+            s.rows = min(kRows, k.g.rows - s.row0);
+            s.tile = k.tile;
+            s.end = min(k.g.tiles, k.tile + left);
+            s.pad = 0;
+            s.slot = (long long)k.task + k.no + k.piece;
+            left -= s.end - s.tile;
+            k.tile = s.end;
+            if (k.tile == k.g.tiles) {
+                k.tile = 0;
+                k.no++;
+            }
+            if (!room()) return;
+            plan[run & 1] = s;
+            R.arrive(B_PLAN + (run & 1));
+            run++;
+        }
+    }
+    if (!room()) return;
+    plan[run & 1].tile = plan[run & 1].end = 0;
+    R.arrive(B_PLAN + (run & 1));
+}
+
+// ---- the cache's bytes on their way: a warp for keys, one for values.  Half a tile at a time is copied in bulk into one of two places, as soon as what was there has
+// been read; tiles further on are asked for from HBM into the L2, so that a copy has the L2's latency only.
+// (Tried instead: pieces in the registers of those who widen them, whose loads a warp waits for all together; 16-byte copies, of which a warp issues one in some 100 cycles.)
 template <int HD>
-__device__ __forceinline__ void widen_role(const PrefixArgs &P, const PrefixRoom &R, Walk walk, const long long *units, const int *tasks)
+__device__ __forceinline__ void copy_role(const PrefixArgs &P, const PrefixRoom &R, const Stretch *plan, const int values)
 {
     using S = PrefixShape<HD>;
     const AttnArgs &A = P.a;
-    constexpr int ROWS = 32 / (HD / 16);                // rows of a warp's pass
-    constexpr int N = kTok / (2 * ROWS), PER16 = 16 / (2 * ROWS);      // passes, and passes of 16 tokens
+    const int lane = threadIdx.x & 31;
+    const uint8_t *cache = values ? A.c.d_v : A.c.d_k;
+    const uint32_t ring = R.smem + S::kRing + values * kTok * HD, have_at = R.smem + S::kHave + values * 8;
+    const int raw = values ? B_VRAW : B_KRAW, read = values ? B_VREAD : B_KREAD;
+    // a run: tokens of half a tile that lie side by side in the cache.  (A copy takes the warp some 100 cycles, whatever its size.)
+    const int page_log2 = 31 - __clz(A.c.page), run_log2 = min(page_log2, 6), runs = kTok >> run_log2;
+    unsigned n = 0, asked[2] = {0, 0};                  // tiles so far, and of either half those that were asked for
+    bool good = true;
+    Stretch s;
+    for (unsigned run = 0; good && R.next(plan, run, s); R.done(run), run++) {
+        const int32_t *row = P.ptable + (int64_t)s.group * P.pcols;
+        auto page_of = [&](int tile) {                  // lane i: page of the tile's i-th run, negative: none
+            const int tok = tile * kTok + (lane << run_log2);
+            return lane < runs && tile < s.end && tok < s.len ? row[tok >> page_log2] : -1;
+        };
+        auto there = [&](int page) { return page >= 0 && page < A.c.n_pages; };
+        auto place_of = [&](int page) { return cache + (((int64_t)page * A.c.n_kv + s.kv) * A.c.page + ((lane << run_log2) & (A.c.page - 1))) * HD; };
+        auto ahead = [&](int page) {
+            if (there(page)) asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(place_of(page)), "r"(HD << run_log2) : "memory");
+        };
+        // The keys' warp also leaves the tile's scales.  Missing pages and 16 tokens behind the end: log2 -infinity.
+        float ks = 1.f, vs = -1.f;
+        auto scales_of = [&](int pages) {
+            const int page = __shfl_sync(0xFFFFFFFFu, pages, (lane & 7) >> (run_log2 - 4));
+            const int64_t ph = (int64_t)page * A.c.n_kv + s.kv;
+            ks = there(page) ? __ldg(A.c.d_k_scale + ph) : 1.f;
+            vs = there(page) ? __ldg(A.c.d_v_scale + ph) : -1.f;
+        };
+        int page = page_of(s.tile), next = page_of(s.tile + 1), far = page_of(s.tile + kAhead);
+        if (!values) scales_of(page);
+        for (int t = s.tile; good && t < s.end; t++, n++) {
+            const uint8_t *from = place_of(page);
+            const int bytes = there(page) ? min(1 << run_log2, s.len - t * kTok - (lane << run_log2)) * HD : 0;
+            const unsigned have = __ballot_sync(0xFFFFFFFFu, bytes > 0);
+            if (!values) {
+                // Eight tiles' places: what lies in tile n's, the scales of tile n - 8, has been read when the keys of tile n - 1 are being widened
+                if (lane < 8) {
+                    const float v = fmaxf(vs, 8.673617379884035e-19f);      // 2^-60
+                    asm volatile("st.shared.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(R.smem + S::kScales + (n & 7) * 128 + lane * 16), "f"(ks),
+                                 "f"(vs < 0.f ? -INFINITY : __log2f(v)), "f"(__fdividef(1.f, v)), "f"(0.f) : "memory");
+                }
+                __syncwarp();
+                scales_of(next);
+            }
+#pragma unroll
+            for (int h = 0; h < 2; h++) {
+                const bool mine = lane >> (6 - run_log2) == h && bytes > 0;
+                const int all = __reduce_add_sync(0xFFFFFFFFu, mine ? bytes : 0);
+                good = good && R.wait_warp(read + h, (n & 1u) ^ 1u);
+                if (!good) break;
+                if (lane == 0) {
+                    asm volatile("st.shared.u32 [%0], %1;" ::"r"(have_at + 4 * h), "r"(have) : "memory");
+                    bar_expect(R.bars + 8 * (raw + h), all);
+                }
+                asked[h]++;
+                __syncwarp();
+                if (mine) bulk_in(ring + (lane << run_log2) * HD, from, bytes, R.bars + 8 * (raw + h));
+            }
+            page = next;
+            next = page_of(t + 2);
+            ahead(far);
+            far = page_of(t + 1 + kAhead);
+        }
+        if (!good) break;
+    }
+    for (int h = 0; h < 2; h++)                         // what is under way arrives before the block may end
+        if (asked[h]) bar_wait(R.bars + 8 * (raw + h), (asked[h] - 1) & 1u, kDrainLimit, R.gave_up + 4);
+}
+
+// ---- the cache's bytes -> fp16 operands.  Two warps widen keys, two values.  Eight neighbouring lanes have four pieces of 16 bytes of each of two rows, so that neither their
+// loads nor their stores meet a bank twice.
+template <int HD>
+__device__ __forceinline__ void widen_role(const PrefixRoom &R, const Stretch *plan)
+{
+    using S = PrefixShape<HD>;
+    constexpr int ROWS = 64 / (HD / 16);                // rows of a pass of both warps
+    constexpr int N = 64 / ROWS, B = 4;                 // passes of half a tile, and of them at a time
     const int lane = threadIdx.x & 31, w = threadIdx.x / 32 - kSoftWarps, values = w >> 1;
-    const int c = HD == 128 ? (lane & 3) + (lane >> 4) * 4 : lane & 3, r0 = (w & 1) * ROWS + (HD == 128 ? (lane >> 2) & 3 : lane >> 2);
-    const uint8_t *from = (values ? A.c.d_v : A.c.d_k) + r0 * HD + c * 16;
+    // HD 128: lanes 0 - 3 row 0 pieces 0 - 3, 4 - 7 row 1 pieces 4 - 7, 8 - 11 row 0 pieces 4 - 7, 12 - 15 row 1 pieces 0 - 3, 16 - 31 rows 2 and 3 likewise
+    const int c = HD == 128 ? (lane & 3) + 4 * (((lane >> 2) ^ (lane >> 3)) & 1) : lane & 3;
+    const int r0 = (w & 1) * (ROWS / 2) + (HD == 128 ? ((lane >> 2) & 1) + 2 * (lane >> 4) : lane >> 2);
     const uint32_t to = R.smem + (values ? S::kV : S::kK) + (uint32_t)(c >> 2) * 16384u;
     const uint32_t to0 = to + operand_at(r0, 2 * (c & 3)), to1 = to + operand_at(r0, 2 * (c & 3) + 1);
-    const int full = values ? B_VFULL : B_KFULL, empty = values ? B_VEMPTY : B_KEMPTY;
-    const int page_log2 = 31 - __clz(A.c.page);
+    const uint32_t own = R.smem + S::kRing + values * kTok * HD + r0 * HD + c * 16, have_at = R.smem + S::kHave + values * 8;
+    const int full = values ? B_VFULL : B_KFULL, empty = values ? B_VEMPTY : B_KEMPTY, raw = values ? B_VRAW : B_KRAW, read = values ? B_VREAD : B_KREAD;
+    const int run_log2 = R.run_log2;
     unsigned n = 0;                                     // tiles so far
     Stretch s;
-    while (walk.next(P, units, tasks, s)) {
-        const int32_t *row = P.ptable + (int64_t)s.group * P.pcols;
-        uint4 x[N];
-        auto page_of = [&](int tile) {                  // lane i < 8: page of the tile's i-th 16 tokens, negative: none
-            const int tok = tile * kTok + 16 * lane;
-            return lane < 8 && tile < s.end && tok < s.g.len ? row[tok >> page_log2] : -1;
-        };
-        auto place_of = [&](int page) {                 // and where they begin in the cache, negative: nowhere
-            return page < 0 || page >= A.c.n_pages ? (int64_t)-1 : (((int64_t)page * A.c.n_kv + s.kv) * A.c.page + ((16 * lane) & (A.c.page - 1))) * HD;
-        };
-        auto load = [&](const uint8_t *src, bool there) { return there ? __ldg(reinterpret_cast<const uint4 *>(src)) : make_uint4(0u, 0u, 0u, 0u); };
-        int64_t at = place_of(page_of(s.tile));
-        int left = s.g.len - s.tile * kTok - r0;
-#pragma unroll
-        for (int g = 0; g < 8; g++) {
-            const int64_t base = __shfl_sync(0xFFFFFFFFu, at, g);
-#pragma unroll
-            for (int i = 0; i < PER16; i++) x[g * PER16 + i] = load(from + base + i * 2 * ROWS * HD, base >= 0 && (g * PER16 + i) * 2 * ROWS < left);
-        }
-        int page = page_of(s.tile + 1);
+    for (unsigned run = 0; R.next(plan, run, s); R.done(run), run++) {
         for (int t = s.tile; t < s.end; t++, n++) {
-            const int stage = n & 1;
-            at = place_of(page);
-            left -= kTok;
-            const bool whole = __all_sync(0xFFFFFFFFu, (at >= 0 || lane >= 8) && left >= kTok);      // of the next tile
-            page = page_of(t + 2);
+            const int stage = n & 1, left = s.len - t * kTok;
             if (!R.wait_warp(empty + stage, ((n >> 1) & 1u) ^ 1u)) return;
 #pragma unroll
-            for (int g = 0; g < 8; g++) {
+            for (int h = 0; h < 2; h++) {
+                if (!R.wait_warp(raw + h, n)) return;
+                uint32_t have;                          // runs of the tile that were copied
+                asm volatile("ld.shared.u32 %0, [%1];" : "=r"(have) : "r"(have_at + 4 * h) : "memory");
+                const bool whole = have == (1u << (7 - run_log2)) - 1 && left >= kTok;
+                uint4 x[B], y[B];                       // the next ones are loaded while these are widened
 #pragma unroll
-                for (int i = g * PER16; i < (g + 1) * PER16; i++) {
-                    uint32_t h[8];
-                    widen4(x[i].x, h[0], h[1]);
-                    widen4(x[i].y, h[2], h[3]);
-                    widen4(x[i].z, h[4], h[5]);
-                    widen4(x[i].w, h[6], h[7]);
-                    const uint32_t on = stage * S::kOperand + i * 2 * ROWS * 128;
-                    sts128(to0 + on, h[0], h[1], h[2], h[3]);
-                    sts128(to1 + on, h[4], h[5], h[6], h[7]);
+                for (int i = 0; i < B; i++) y[i] = lds128(own + (h * 64 + i * ROWS) * HD);
+#pragma unroll
+                for (int q = 0; q < N; q += B) {
+#pragma unroll
+                    for (int i = 0; i < B; i++) {
+                        x[i] = y[i];
+                        if (q + B < N) y[i] = lds128(own + (h * 64 + (q + B + i) * ROWS) * HD);
+                    }
+                    if (!whole) {
+#pragma unroll
+                        for (int i = 0; i < B; i++) {
+                            const int at = h * 64 + (q + i) * ROWS + r0;
+                            if (at >= left || !(have >> (at >> run_log2) & 1u)) x[i] = make_uint4(0u, 0u, 0u, 0u);
+                        }
+                    }
+#pragma unroll
+                    for (int i = 0; i < B; i++) {
+                        uint32_t v[8];
+                        widen4(x[i].x, v[0], v[1]);
+                        widen4(x[i].y, v[2], v[3]);
+                        widen4(x[i].z, v[4], v[5]);
+                        widen4(x[i].w, v[6], v[7]);
+                        const uint32_t on = stage * S::kOperand + (h * 64 + (q + i) * ROWS) * 128;
+                        sts128(to0 + on, v[0], v[1], v[2], v[3]);
+                        sts128(to1 + on, v[4], v[5], v[6], v[7]);
+                    }
                 }
+                __syncwarp();
+                if (lane == 0) R.arrive(read + h);
             }
             publish_shared();
             __syncwarp();
             if (lane == 0) R.arrive(full + stage);
-            if (whole) {
-#pragma unroll
-                for (int g = 0; g < 8; g++) {
-                    const uint8_t *src = from + __shfl_sync(0xFFFFFFFFu, at, g);
-#pragma unroll
-                    for (int i = 0; i < PER16; i++) x[g * PER16 + i] = __ldg(reinterpret_cast<const uint4 *>(src + i * 2 * ROWS * HD));
-                }
-            } else {
-#pragma unroll
-                for (int g = 0; g < 8; g++) {
-                    const int64_t base = __shfl_sync(0xFFFFFFFFu, at, g);
-#pragma unroll
-                    for (int i = 0; i < PER16; i++) x[g * PER16 + i] = load(from + base + i * 2 * ROWS * HD, base >= 0 && (g * PER16 + i) * 2 * ROWS < left);
-                }
-            }
         }
     }
 }
@@ -257,7 +380,7 @@ __device__ __forceinline__ void widen_role(const PrefixArgs &P, const PrefixRoom
 // (With one thread going through all this, their computation took longer than the products.)
 // Tensor memory: 128 columns of scores of either stream, which weights replace, then HD columns of values of either
 template <int HD>
-__device__ __forceinline__ void product_role(const PrefixArgs &P, const PrefixRoom &R, Walk walk, const long long *units, const int *tasks)
+__device__ __forceinline__ void product_role(const PrefixArgs &P, const PrefixRoom &R, const Stretch *plan)
 {
     using S = PrefixShape<HD>;
     constexpr uint32_t kScores = mma_shape(kTok, false), kValues = mma_shape(HD, true);
@@ -297,11 +420,10 @@ __device__ __forceinline__ void product_role(const PrefixArgs &P, const PrefixRo
         return true;
     };
     Stretch s;
-    while (walk.next(P, units, tasks, s)) {
+    for (; R.next(plan, runs, s); R.done(runs), runs++) {
         const int m = s.end - s.tile;
         const bool turns = s.turns();
         if (!R.wait_warp(B_QFULL, runs) || !R.wait_warp(B_QFULL + 1, runs)) return;
-        runs++;
         const unsigned base = n;
         const int lag = turns ? 2 : 1;
         // step i: the scores of tile i, behind the values of the tile `lag` in front, whose weights lie where the scores go
@@ -360,14 +482,14 @@ __device__ __forceinline__ float score_of(const uint32_t (&x)[8][16], int k) { r
 
 // ---- the rows: thread r of a stream owns row r of its 128
 template <typename T, int HD>
-__device__ __forceinline__ bool rows_run(const PrefixArgs &P, const PrefixRoom &R, const Stretch &s, int j, unsigned &tiles, float (&zl)[2])
+__device__ __forceinline__ bool rows_run(const PrefixArgs &P, const PrefixRoom &R, const Stretch &s, int j, unsigned first, unsigned &tiles, float (&zl)[2])
 {
     using S = PrefixShape<HD>;
     const AttnArgs &A = P.a;
     const int warp = threadIdx.x / 32 % 4, lane = threadIdx.x & 31, r = 32 * warp + lane;
     const int at = s.row0 + (s.turns() ? 0 : 128 * j) + r;
-    const bool live = at < s.g.rows;
-    const bool any = s.row0 + (s.turns() ? 0 : 128 * j) + 32 * warp < s.g.rows;       // of the warp
+    const bool live = at < s.members;
+    const bool any = s.row0 + (s.turns() ? 0 : 128 * j) + 32 * warp < s.members;       // of the warp
     const int count = s.tiles_of(j);
     const uint32_t lanes = (uint32_t)(32 * warp) << 16, score = kTmem + lanes + j * 128, value = kTmem + lanes + 256 + j * HD;
     // The query row, as in the kernel of a sequence's own tokens: its largest finite element goes to [2^13, 2^14), and the power of two and the sign of
@@ -375,7 +497,7 @@ __device__ __forceinline__ bool rows_run(const PrefixArgs &P, const PrefixRoom &
     float up;
     {
         uint4 raw[HD / 8];
-        const uint16_t *src = A.q + (int64_t)(s.g.first + at / A.group) * A.qs + (int64_t)(s.kv * A.group + at % A.group) * HD;
+        const uint16_t *src = A.q + (int64_t)(s.first + at / A.group) * A.qs + (int64_t)(s.kv * A.group + at % A.group) * HD;
         float top = 0.f;
 #pragma unroll
         for (int i = 0; i < HD / 8; i++) {
@@ -412,43 +534,28 @@ __device__ __forceinline__ bool rows_run(const PrefixArgs &P, const PrefixRoom &
     z = -INFINITY;
     l = 0.f;
     const int step = s.turns() ? 2 : 1;
-    // lane x < 8: scales of the x-th 16 tokens' page of a tile; missing pages and 16 tokens behind the end: lv -infinity
-    const int32_t *row = P.ptable + (int64_t)s.group * P.pcols;
-    int page = -1;
-    float ks = 0.f, vs = -1.f, next_ks = 0.f, next_vs = -1.f;
-    auto find = [&](int tile) {
-        const int tok = tile * kTok + 16 * lane;
-        page = lane < 8 && tile < s.end && tok < s.g.len ? row[tok >> (31 - __clz(A.c.page))] : -1;
-    };
-    auto fetch = [&]() {
-        const bool there = page >= 0 && page < A.c.n_pages;
-        const int64_t ph = (int64_t)page * A.c.n_kv + s.kv;
-        next_ks = there ? __ldg(A.c.d_k_scale + ph) : 0.f;
-        next_vs = there ? __ldg(A.c.d_v_scale + ph) : -1.f;
-    };
-    int tile = s.tile + (s.turns() ? j : 0);
-    find(tile);
-    fetch();
-    find(tile + step);
-    for (int i = 0; i < count; i++, tile += step, tiles++) {
-        ks = next_ks;
-        vs = next_vs;
-        fetch();
-        find(tile + 2 * step);
-        const float v = fmaxf(vs, 8.673617379884035e-19f);      // 2^-60
-        const float my_lv = vs < 0.f ? -INFINITY : __log2f(v), my_iv = __fdividef(1.f, v);
+    int left = s.len - s.tile * kTok;                 // tokens of the tile that exist
+    if (s.turns()) left -= j * kTok;
+    unsigned place = first + (s.turns() ? j : 0);       // the tile's number
+    for (int i = 0; i < count; i++, tiles++, place += step, left -= step * kTok) {
+        const uint32_t scales = R.smem + S::kScales + (place & 7) * 128;
+        auto scale_of = [&](int g) {
+            float4 v;
+            asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(scales + 16 * g) : "memory");
+            v.x = fmaxf(v.x * up, 1.1754944e-38f);      // never 0, which times -infinity would be no number
+            return v;
+        };
         if (!R.wait_warp(B_SFULL + j, tiles)) return false;
         tmem_after_sync();
         if (any) {
-            const int left = s.g.len - tile * kTok;
             uint32_t x[8][16];                          // the row's scores
 #pragma unroll
             for (int c = 0; c < 8; c++) tmem_ld16(score + 16 * c, x[c]);
-            // factor of each 16 tokens' scores; never 0, which times -infinity would be no number
-            auto factor = [&](int g) { return fmaxf(up * __shfl_sync(0xFFFFFFFFu, ks, g), 1.1754944e-38f); };
+            tmem_wait_ld(x[0]);
 #pragma unroll
-            for (int c = 0; c < 8; c++) tmem_wait_ld(x[c]);
+            for (int c = 1; c < 8; c++) tmem_named(x[c]);
             if (left < kTok) {
+                asm volatile("" ::: "memory");          // a branch: most tiles are whole, and 128 selections are not to be made in all of them
 #pragma unroll
                 for (int k = 0; k < kTok; k++)
                     if (k >= left) x[k / 16][k % 16] = 0xFF800000u;      // -infinity: weight 0
@@ -464,8 +571,8 @@ __device__ __forceinline__ bool rows_run(const PrefixArgs &P, const PrefixRoom &
                 }
                 m0 = max3(m0, m1, score_of(x, 16 * g + 14));
                 m0 = max3(m0, m0, score_of(x, 16 * g + 15));
-                const float most = fmaf(m0, factor(g), __shfl_sync(0xFFFFFFFFu, my_lv, g));
-                top = max3(top, top, most);
+                const float4 sc = scale_of(g);
+                top = max3(top, top, fmaf(m0, sc.x, sc.y));
             }
             // a score that is no number, or infinite, makes the row NaN, whichever way its weight is computed
             if (!(top < INFINITY)) l = __int_as_float(0x7FC00000);
@@ -495,8 +602,9 @@ __device__ __forceinline__ bool rows_run(const PrefixArgs &P, const PrefixRoom &
 #pragma unroll
                 for (int h = 0; h < 2; h++) {
                     const int g = 2 * c + h;
-                    const float f = factor(g), shift = __shfl_sync(0xFFFFFFFFu, my_lv, g) - ref;
-                    const Two ff = two(f, f), ss = two(shift, shift);
+                    const float4 sc = scale_of(g);
+                    const float shift = sc.y - ref;
+                    const Two ff = two(sc.x, sc.x), ss = two(shift, shift);
                     Two sum = two(0.f, 0.f);
 #pragma unroll
                     for (int k = 0; k < 8; k++) {
@@ -514,7 +622,7 @@ __device__ __forceinline__ bool rows_run(const PrefixArgs &P, const PrefixRoom &
                     }
                     float s0, s1;
                     apart(sum, s0, s1);
-                    l32 = fmaf(s0 + s1, __shfl_sync(0xFFFFFFFFu, my_iv, g), l32);
+                    l32 = fmaf(s0 + s1, sc.z, l32);
                 }
                 tmem_st16(score + 16 * c, w);           // over scores that have been read
                 if (c == 1) {                           // half of the weights: their products may begin
@@ -541,38 +649,33 @@ __device__ __forceinline__ bool rows_run(const PrefixArgs &P, const PrefixRoom &
 }
 
 template <typename T, int HD>
-__device__ __forceinline__ void rows_role(const PrefixArgs &P, const PrefixRoom &R, Walk walk, const long long *units, const int *tasks)
+__device__ __forceinline__ void rows_role(const PrefixArgs &P, const PrefixRoom &R, const Stretch *plan)
 {
     const int j = threadIdx.x / 128, warp = threadIdx.x / 32 % 4, lane = threadIdx.x & 31, r = 32 * warp + lane;
-    unsigned runs = 0, tiles = 0;                       // stretches, and tiles of this stream, so far
-    bool good = true;
+    unsigned runs = 0, tiles = 0, all = 0;              // stretches, tiles of this stream and of both, so far
     Stretch s;
-    while (walk.next(P, units, tasks, s)) {
-        float zl[2] = {0.f, __int_as_float(0x7FC00000)};
+    for (; R.next(plan, runs, s); R.done(runs), runs++) {
+        float zl[2];
         const int count = s.tiles_of(j);
-        if (good) good = rows_run<T, HD>(P, R, s, j, tiles, zl);
-        if (good) good = R.wait_warp(B_OFULL + j, runs);
-        runs++;
-        if (!good) zl[1] = __int_as_float(0x7FC00000);  // a wait ran out: these rows are NaN
-        const int row = s.turns() ? r : 128 * j + r;
+        if (!rows_run<T, HD>(P, R, s, j, all, tiles, zl) || !R.wait_warp(B_OFULL + j, runs)) return;
+        all += s.end - s.tile;
+        const int row = s.turns() ? r : 128 * j + r, place = 128 * j + r;
         const bool live = row < s.rows && s.slot < P.n_slots;
         float *to = P.slots + s.slot * (kRows * (HD + 2));
-        const int place = 128 * j + r;
         if (live) {
             to[kRows * HD + place] = zl[0];
             to[kRows * (HD + 1) + place] = zl[1];
         }
-        if (good && count) {
+        if (count) {
             tmem_after_sync();
-#pragma unroll
-            for (int c = 0; c < HD / 32; c++) {
-                uint32_t x[32];
-                tmem_ld32(kTmem + ((uint32_t)(32 * warp) << 16) + 256 + j * HD + 32 * c, x);
+#pragma unroll 1
+            for (int c = 0; c < HD / 16; c++) {
+                uint32_t x[16];
+                tmem_ld16(kTmem + ((uint32_t)(32 * warp) << 16) + 256 + j * HD + 16 * c, x);
                 tmem_wait_ld(x);
                 if (live)
 #pragma unroll
-                    for (int k = 0; k < 32; k += 4)
-                        *reinterpret_cast<uint4 *>(to + place * HD + 32 * c + k) = make_uint4(x[k], x[k + 1], x[k + 2], x[k + 3]);
+                    for (int k = 0; k < 16; k += 4) *reinterpret_cast<uint4 *>(to + place * HD + 16 * c + k) = make_uint4(x[k], x[k + 1], x[k + 2], x[k + 3]);
             }
             tmem_before_sync();
         } else if (live) {
@@ -586,59 +689,70 @@ __global__ void __launch_bounds__(kPrefixThreads, 1) prefix_kernel(const __grid_
 {
     using S = PrefixShape<HD>;
     extern __shared__ __align__(1024) uint8_t prefix_smem[];
-    uint8_t *room = prefix_smem + (-smem_addr(prefix_smem) & 1023u);      // operands begin at multiples of 1024
-    __shared__ __align__(8) uint64_t bars[B_COUNT];
-    __shared__ uint32_t tmem_at;
-    __shared__ int gave_up;
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-    long long *units = reinterpret_cast<long long *>(room + S::kBytes);
-    int *tasks = reinterpret_cast<int *>(units + P.n_groups + 1);
-    group_prefix(P, units, tasks);
-    const long long total = units[P.n_groups];
-    if (total == 0 || (int)blockIdx.x >= pieces_of(total, gridDim.x)) return;
+    // the groups' prefix sums lie where operands come later
+    long long *units = reinterpret_cast<long long *>(prefix_smem);
+    int *tasks = reinterpret_cast<int *>(units + PF_PREFIX_MAX_GROUPS + 1);
+    group_prefix(P, units, tasks, tasks + PF_PREFIX_MAX_GROUPS + 1);
+    Walk walk;
+    if (!walk.begin(P, units, tasks)) return;
+    uint32_t *words = reinterpret_cast<uint32_t *>(prefix_smem + S::kBars + 8 * B_COUNT);
+    uint32_t *gave_up = words + 1;
+    Stretch *plan = reinterpret_cast<Stretch *>(prefix_smem + S::kPlan);
     const int warp = threadIdx.x >> 5;
-    PrefixRoom R{smem_addr(room), smem_addr(bars), &gave_up, P.wait_limit};
+    const PrefixRoom R{smem_addr(prefix_smem), smem_addr(prefix_smem) + S::kBars, smem_addr(gave_up), P.wait_limit, min(31 - __clz(P.a.c.page), 6)};
     if (threadIdx.x == 0) {
-        gave_up = 0;
+        words[1] = words[2] = 0;
         for (int i = 0; i < 2; i++) {
             bar_init(R.bars + 8 * (B_KFULL + i), kWidenWarps / 2);
             bar_init(R.bars + 8 * (B_VFULL + i), kWidenWarps / 2);
             bar_init(R.bars + 8 * (B_KEMPTY + i), 1);
             bar_init(R.bars + 8 * (B_VEMPTY + i), 1);
+            bar_init(R.bars + 8 * (B_KRAW + i), 1);
+            bar_init(R.bars + 8 * (B_VRAW + i), 1);
+            bar_init(R.bars + 8 * (B_KREAD + i), kWidenWarps / 2);
+            bar_init(R.bars + 8 * (B_VREAD + i), kWidenWarps / 2);
+            bar_init(R.bars + 8 * (B_PLAN + i), 1);
+            bar_init(R.bars + 8 * (B_DONE + i), kSoftWarps + kWidenWarps + 3);
             bar_init(R.bars + 8 * (B_QFULL + i), 4);
             bar_init(R.bars + 8 * (B_SFULL + i), 1);
-            bar_init(R.bars + 8 * (B_PFULL + i), 4);
             bar_init(R.bars + 8 * (B_PHALF + i), 4);
+            bar_init(R.bars + 8 * (B_PFULL + i), 4);
             bar_init(R.bars + 8 * (B_OFULL + i), 1);
         }
         bar_init(R.bars + 8 * B_DRAIN, 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
-    if (warp == kSoftWarps + kWidenWarps) tmem_alloc(smem_addr(&tmem_at), 512);
+    if (warp == kSoftWarps + kWidenWarps) tmem_alloc(smem_addr(words), 512);
     tmem_before_sync();
     __syncthreads();
     tmem_after_sync();
-    const Walk walk(total);
     if (warp < kSoftWarps) {
         take_registers<kSoftRegs>();
-        rows_role<T, HD>(P, R, walk, units, tasks);
+        rows_role<T, HD>(P, R, plan);
     } else if (warp < kSoftWarps + kWidenWarps) {
         leave_registers<kWidenRegs>();
-        widen_role<HD>(P, R, walk, units, tasks);
+        widen_role<HD>(R, plan);
     } else {
         leave_registers<kProductRegs>();
         if (warp == kSoftWarps + kWidenWarps) {
-            product_role<HD>(P, R, walk, units, tasks);
+            product_role<HD>(P, R, plan);
             // whatever was begun is done before the block gives its memory back
             __syncwarp();
             if (elected()) mma_commit(R.bars + 8 * B_DRAIN);
-            int alone = 0;
-            bar_wait(R.bars + 8 * B_DRAIN, 0, kDrainLimit, &alone);
+            const uint32_t alone = smem_addr(words + 2);
+            bar_wait(R.bars + 8 * B_DRAIN, 0, kDrainLimit, alone);
+        } else if (threadIdx.x == 32 * (kSoftWarps + kWidenWarps + 1)) {
+            plan_role(P, R, walk, plan);
+        } else if (warp >= kSoftWarps + kWidenWarps + 2) {
+            copy_role<HD>(P, R, plan, warp & 1);
         }
+        __syncwarp();
     }
     tmem_before_sync();
     __syncthreads();
-    if (warp == kSoftWarps + kWidenWarps) tmem_free(tmem_at, 512);
+    if (warp == kSoftWarps + kWidenWarps) tmem_free(words[0], 512);
+    if (threadIdx.x == 0) P.status[blockIdx.x] = words[1];      // a wait that ran out: the join makes NaN of what this block had to do
 }
 
 // ------------------------------------------------------------------ the join
@@ -655,11 +769,12 @@ __global__ void __launch_bounds__(256) prefix_join_kernel(const __grid_constant_
     int *tasks = reinterpret_cast<int *>(units + P.n_groups + 1);
     int *prefix = tasks + P.n_groups + 1;
     __shared__ int warp_sum[8];
-    group_prefix(P, units, tasks);
+    __shared__ __align__(8) int scratch[100];
+    group_prefix(P, units, tasks, scratch);
     tile_prefix(A, prefix, warp_sum);
     const int lane = threadIdx.x & 31;
     const long long total = units[P.n_groups], own_total = (long long)prefix[A.n_seq] * A.jobs_per_seq;
-    const int n_pieces = total ? pieces_of(total, prefix_grid) : 0, own_blocks = blocks_used(own_total, own_grid);
+    const int n_pieces = total ? pieces_of(total, prefix_grid) : 0, each = pieces_each(n_pieces, prefix_grid), own_blocks = blocks_used(own_total, own_grid);
     asm volatile("griddepcontrol.wait;" ::: "memory");
     const float *blocks = A.part + (int64_t)own_grid * S::kWarps * S::kPartFloats;
     const long long n_rows = (long long)A.n_seq * A.n_heads;
@@ -678,7 +793,7 @@ __global__ void __launch_bounds__(256) prefix_join_kernel(const __grid_constant_
         }
         // parts of its group's prefix
         long long slot = 0;
-        int n_pre = 0, at = 0, both = 1;          // parts of a slot
+        int n_pre = 0, at = 0, p0 = 0, both = 1;  // parts of a slot
         if (total) {
             const int gi = P.cu ? last_at(P.cu, P.n_groups, b) : 0;
             const Group g = group_of(P, gi);
@@ -688,7 +803,7 @@ __global__ void __launch_bounds__(256) prefix_join_kernel(const __grid_constant_
                 both = g.rows - at / kRows * kRows <= 128 ? 2 : 1;
                 at %= kRows;
                 const long long begin = units[gi] + (long long)no * g.tiles;
-                const int p0 = piece_of(total, n_pieces, begin);
+                p0 = piece_of(total, n_pieces, begin);
                 n_pre = piece_of(total, n_pieces, begin + g.tiles - 1) - p0 + 1;
                 slot = (long long)tasks[gi] + no + p0;
                 if (slot + n_pre > P.n_slots) n_pre = 0;
@@ -717,7 +832,7 @@ __global__ void __launch_bounds__(256) prefix_join_kernel(const __grid_constant_
                 const float *p = P.slots + (slot + (both == 2 ? no >> 1 : no)) * (kRows * (HD + 2));
                 from = p + place * HD;
                 z = p[kRows * HD + place];
-                l = p[kRows * (HD + 1) + place];
+                l = P.status[(p0 + (both == 2 ? no >> 1 : no)) / each] ? __int_as_float(0x7FC00000) : p[kRows * (HD + 1) + place];
             }
             float most = fmaxf(top, z);
 #pragma unroll
@@ -748,7 +863,7 @@ __global__ void __launch_bounds__(256) prefix_join_kernel(const __grid_constant_
 
 // ------------------------------------------------------------------ host
 struct PrefixSizes {
-    size_t own_v, own_z, own_l, slots, bytes;      // offsets in the workspace, and its size
+    size_t own_v, own_z, own_l, status, slots, bytes;      // offsets in the workspace, and its size
     long long n_slots;
 };
 static PrefixSizes prefix_sizes(int hd, int page, int n_kv, int n_seq, int n_heads, int n_groups, int pcols, int sms)
@@ -759,7 +874,8 @@ static PrefixSizes prefix_sizes(int hd, int page, int n_kv, int n_seq, int n_hea
     s.own_v = up(attention_workspace_bytes(hd, sms));
     s.own_z = s.own_v + up(rows * hd * 4);
     s.own_l = s.own_z + up(rows * 4);
-    s.slots = s.own_l + up(rows * 4);
+    s.status = s.own_l + up(rows * 4);
+    s.slots = s.status + up((size_t)sms * 4);
     const long long tiles = ((long long)pcols * page + kTok - 1) / kTok;
     const long long tasks = (long long)n_kv * (((long long)n_seq * (n_heads / n_kv)) / kRows + n_groups);
     const long long per = (tasks * tiles + (long long)sms * kMostTiles - 1) / ((long long)sms * kMostTiles);
@@ -776,7 +892,7 @@ static int prefix_launch(PrefixArgs p, int device, int sms, cudaStream_t st)
     a.row_blocks = (a.group + S::kHeads - 1) / S::kHeads;
     a.jobs_per_seq = a.c.n_kv * a.row_blocks;
     const size_t groups = (size_t)(p.n_groups + 1) * 12, own = ((size_t)a.n_seq + 1) * 4;
-    const size_t smem0 = 1024 + PrefixShape<HD>::kBytes + groups, smem1 = (size_t)S::kWarps * S::kWarpBytes + own, smem2 = groups + own;
+    const size_t smem0 = PrefixShape<HD>::kBytes, smem1 = (size_t)S::kWarps * S::kWarpBytes + own, smem2 = groups + own;
     PF_CUDA_TRY(ensure_dynamic_smem((const void *)prefix_kernel<T, HD>, device, smem0), "prefix_kernel shared memory");
     PF_CUDA_TRY(ensure_dynamic_smem((const void *)attention_kernel<T, HD, NB, true>, device, smem1), "attention_kernel shared memory");
     PF_CUDA_TRY(ensure_dynamic_smem((const void *)prefix_join_kernel<T, HD, NB>, device, smem2), "prefix_join_kernel shared memory");
@@ -848,6 +964,7 @@ extern "C" int pf_prefix_attention(const pf_kv_cache_t *cache, int32_t dtype, in
     a.own_v = (float *)(ws + z.own_v); a.own_z = (float *)(ws + z.own_z); a.own_l = (float *)(ws + z.own_l);
     p.cu = d_cu_seqs; p.plen = d_prefix_len; p.ptable = d_prefix_table;
     p.n_groups = n_groups; p.pcols = prefix_cols; p.n_slots = z.n_slots;
+    p.status = (uint32_t *)(ws + z.status);
     p.slots = (float *)(ws + z.slots);
     p.wait_limit = kWaitLimit;
     cudaStream_t st = (cudaStream_t)stream;

@@ -8,6 +8,15 @@ namespace pf {
 // ------------------------------------------------------------------ barriers in shared memory
 __device__ __forceinline__ void bar_init(uint32_t b, unsigned count) { asm volatile("mbarrier.init.shared.b64 [%0], %1;" ::"r"(b), "r"(count) : "memory"); }
 __device__ __forceinline__ void bar_arrive(uint32_t b) { asm volatile("mbarrier.arrive.shared.b64 _, [%0];" ::"r"(b) : "memory"); }
+__device__ __forceinline__ void bar_expect(uint32_t b, uint32_t bytes)      // an arrival, and so many bytes to come
+{
+    asm volatile("mbarrier.arrive.expect_tx.shared.b64 _, [%0], %1;" ::"r"(b), "r"(bytes) : "memory");
+}
+// a bulk copy into shared memory: addresses and size are multiples of 16
+__device__ __forceinline__ void bulk_in(uint32_t dst, const void *src, uint32_t bytes, uint32_t bar)
+{
+    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src), "r"(bytes), "r"(bar) : "memory");
+}
 __device__ __forceinline__ bool bar_poll(uint32_t b, unsigned parity)
 {
     uint32_t done;
@@ -17,14 +26,16 @@ __device__ __forceinline__ bool bar_poll(uint32_t b, unsigned parity)
 }
 // Waits for the phase of that parity; false where `limit` polls of some 2 us each did not see it, or where another wait of the block gave up
 // (`gave_up`, one word of shared memory, which this one then sets too).
-__device__ __forceinline__ bool bar_wait(uint32_t b, unsigned parity, unsigned limit, volatile int *gave_up)
+__device__ __forceinline__ bool bar_wait(uint32_t b, unsigned parity, unsigned limit, uint32_t gave_up)
 {
     if (bar_poll(b, parity)) return true;
     for (unsigned i = 0; i < limit; i++) {
         if (bar_poll(b, parity)) return true;
-        if (*gave_up) return false;
+        uint32_t over;
+        asm volatile("ld.shared.u32 %0, [%1];" : "=r"(over) : "r"(gave_up) : "memory");
+        if (over) return false;
     }
-    *gave_up = 1;
+    asm volatile("st.shared.u32 [%0], %1;" ::"r"(gave_up), "r"(1u) : "memory");
     return false;
 }
 // what threads wrote to shared memory becomes visible to the matrix instruction
@@ -39,13 +50,19 @@ __device__ __forceinline__ void tmem_alloc(uint32_t where, uint32_t columns)    
 __device__ __forceinline__ void tmem_free(uint32_t addr, uint32_t columns) { asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(addr), "r"(columns)); }
 __device__ __forceinline__ void tmem_before_sync() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void tmem_after_sync() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
-// the loads into r are done (r is named so that nothing that reads it moves in front)
+// r is named, so that nothing that reads it moves in front of a wait
+template <int N>
+__device__ __forceinline__ void tmem_named(uint32_t (&r)[N])
+{
+#pragma unroll
+    for (int i = 0; i < N; i++) asm volatile("" : "+r"(r[i]));
+}
+// all loads are done, those into r among them
 template <int N>
 __device__ __forceinline__ void tmem_wait_ld(uint32_t (&r)[N])
 {
     asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
-#pragma unroll
-    for (int i = 0; i < N; i++) asm volatile("" : "+r"(r[i]));
+    tmem_named(r);
 }
 __device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 // 32 columns of a warp's 32 lanes, a lane a thread
