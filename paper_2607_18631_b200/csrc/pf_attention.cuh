@@ -23,6 +23,8 @@ struct AttnArgs {
     int64_t qs, os;
     int n_seq, n_heads, group, cols, row_blocks, jobs_per_seq;   // jobs_per_seq = n_kv * row_blocks, row_blocks of 8 NB heads
     float scale_log2;                                            // sm_scale * log2(e)
+    const int32_t *cu, *plen;                                    // OWN: shared prefixes, for the kernel that runs beside this one (see there)
+    int n_groups, pcols;
     float *own_v, *own_z, *own_l;                                // OWN: [n_seq * n_heads] x HD values, references, sums of what one block finished
     float *part;                                                 // [warps] x (8 NB x HD values, 8 NB references z, 8 NB sums), then [2 blocks] of the same
 };
@@ -79,6 +81,59 @@ __device__ __forceinline__ int seq_of_tile(const AttnArgs &A, const int *prefix,
         if ((long long)prefix[mid] * A.jobs_per_seq <= t) lo = mid; else hi = mid;
     }
     return lo;
+}
+
+// ---- shared prefixes: a group's rows (sequences times query heads of a key head) in tiles of kRows, its tokens in tiles of kTok
+constexpr int kRows = 256, kTok = 128;
+struct Group { int first, rows, row_tiles, len, tiles; };
+__device__ __forceinline__ Group group_of(const AttnArgs &A, int g)
+{
+    Group r;
+    r.first = A.cu ? min(max(A.cu[g], 0), A.n_seq) : 0;      // without offsets: one group of all
+    const int last = A.cu ? min(max(A.cu[g + 1], r.first), A.n_seq) : A.n_seq;
+    r.rows = (last - r.first) * A.group;
+    r.row_tiles = (r.rows + kRows - 1) / kRows;
+    const long long cap = (long long)A.pcols * A.c.page;
+    r.len = max(0, A.plen[g]);
+    if (r.len > cap) r.len = (int)cap;
+    r.tiles = (r.len + kTok - 1) / kTok;
+    return r;
+}
+// The kernel for prefixes and this one run side by side: SMs that the former takes, given both lists' tiles.  One of its tiles takes an SM 1.4 us (up to 128 rows) to
+// 2.5 us, one of this kernel's 0.23 us; cut by the sum of these, both end at about the same time, and neither waits for the other's start and end.
+__device__ __forceinline__ int prefix_share(long long units, long long own_tiles, int sms)
+{
+    if (units == 0) return 0;
+    if (own_tiles == 0) return sms;
+    const long long n = (units * 9 * sms + (units * 9 + own_tiles) / 2) / (units * 9 + own_tiles);
+    return (int)(n < 1 ? 1 : n >= sms ? sms - 1 : n);
+}
+// sum of a word of each thread, to all; `room`: a word a warp
+__device__ __forceinline__ long long block_total(long long v, long long *room)
+{
+#pragma unroll
+    for (int o = 16; o; o >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, o);
+    __syncthreads();
+    if ((threadIdx.x & 31) == 0) room[threadIdx.x >> 5] = v;
+    __syncthreads();
+    v = 0;
+    for (int i = 0; i < (int)blockDim.x >> 5; i++) v += room[i];
+    return v;
+}
+__device__ __forceinline__ long long prefix_units(const AttnArgs &A, long long *room)
+{
+    long long v = 0;
+    for (int g = threadIdx.x; g < A.n_groups; g += blockDim.x) {
+        const Group r = group_of(A, g);
+        v += (long long)r.row_tiles * A.c.n_kv * r.tiles;
+    }
+    return block_total(v, room);
+}
+__device__ __forceinline__ long long own_tiles(const AttnArgs &A, long long *room)
+{
+    long long v = 0;
+    for (int b = threadIdx.x; b < A.n_seq; b += blockDim.x) v += (seq_len(A, b) + kTile - 1) / kTile;
+    return block_total(v, room) * A.jobs_per_seq;
 }
 
 struct TileCursor {
@@ -244,7 +299,12 @@ __global__ void __launch_bounds__(AttnShape<HD, NB>::kWarps * 32, 1) attention_k
     }
 
     const long long total = (long long)prefix[A.n_seq] * A.jobs_per_seq;
-    const int n_blocks = total == 0 ? 0 : blocks_used(total, gridDim.x);
+    int sms = gridDim.x;
+    if (OWN) {
+        __shared__ long long room[S::kWarps];
+        sms -= prefix_share(prefix_units(A, room), total, sms);
+    }
+    const int n_blocks = total == 0 ? 0 : blocks_used(total, sms);
     if ((int)blockIdx.x >= n_blocks) {
         if (OWN) asm volatile("griddepcontrol.wait;" ::: "memory");
         return;

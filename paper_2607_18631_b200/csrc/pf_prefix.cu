@@ -13,8 +13,6 @@
 
 namespace pf {
 
-constexpr int kRows = 256;               // rows of a task
-constexpr int kTok = 128;                // tokens of a tile
 constexpr int kMostTiles = 512;          // tiles of a piece at most: 32-bit sums do not run over more than 65536 tokens
 constexpr int kAhead = 4;                // tiles that are under way from HBM to the L2
 constexpr int kLeastTiles = 4;           // a piece takes no fewer while others have none
@@ -23,29 +21,12 @@ constexpr float kSetLift = 7.f;          // log2 of the largest weight when a ro
 
 struct PrefixArgs {
     AttnArgs a;
-    const int32_t *cu, *plen, *ptable;
-    int n_groups, pcols;
+    const int32_t *ptable;
     unsigned wait_limit;                 // polls of a wait inside the kernel
     long long n_slots;
     uint32_t *status;                    // [blocks], written by those with work
     float *slots;                        // [n_slots] x (kRows x HD values, kRows references, kRows sums)
 };
-
-struct Group { int first, rows, row_tiles, len, tiles; };
-__device__ __forceinline__ Group group_of(const PrefixArgs &P, int g)
-{
-    const AttnArgs &A = P.a;
-    Group r;
-    r.first = P.cu ? min(max(P.cu[g], 0), A.n_seq) : 0;      // without offsets: one group of all
-    const int last = P.cu ? min(max(P.cu[g + 1], r.first), A.n_seq) : A.n_seq;
-    r.rows = (last - r.first) * A.group;
-    r.row_tiles = (r.rows + kRows - 1) / kRows;
-    const long long cap = (long long)P.pcols * A.c.page;
-    r.len = max(0, P.plen[g]);
-    if (r.len > cap) r.len = (int)cap;
-    r.tiles = (r.len + kTok - 1) / kTok;
-    return r;
-}
 
 // Tiles and tasks of the groups in front of each group, by the whole block.  units, tasks: n_groups + 1 words; scratch: 100
 __device__ __forceinline__ void group_prefix(const PrefixArgs &P, long long *units, int *tasks, int *scratch)
@@ -56,11 +37,11 @@ __device__ __forceinline__ void group_prefix(const PrefixArgs &P, long long *uni
     long long base_u = 0;
     int base_t = 0;
     if (tid == 0) units[0] = 0, tasks[0] = 0;
-    for (int g0 = 0; g0 < P.n_groups; g0 += nt) {
+    for (int g0 = 0; g0 < P.a.n_groups; g0 += nt) {
         long long u = 0;
         int t = 0;
-        if (g0 + tid < P.n_groups) {
-            const Group r = group_of(P, g0 + tid);
+        if (g0 + tid < P.a.n_groups) {
+            const Group r = group_of(P.a, g0 + tid);
             t = r.tiles ? r.row_tiles * P.a.c.n_kv : 0;
             u = (long long)t * r.tiles;
         }
@@ -80,7 +61,7 @@ __device__ __forceinline__ void group_prefix(const PrefixArgs &P, long long *uni
             base_u += warp_units[i];
             base_t += warp_tasks[i];
         }
-        if (g0 + tid < P.n_groups) units[g0 + tid + 1] = add_u + u, tasks[g0 + tid + 1] = add_t + t;
+        if (g0 + tid < P.a.n_groups) units[g0 + tid + 1] = add_u + u, tasks[g0 + tid + 1] = add_t + t;
     }
     __syncthreads();
 }
@@ -175,17 +156,17 @@ struct Walk {
     Group g;
     int group, task, no, tile, piece, last, n_pieces;   // task: number of the group's first
     long long total;
-    __device__ __forceinline__ bool begin(const PrefixArgs &P, const long long *units, const int *tasks)
+    __device__ __forceinline__ bool begin(const PrefixArgs &P, const long long *units, const int *tasks, int blocks)
     {
-        total = units[P.n_groups];
-        n_pieces = total ? pieces_of(total, gridDim.x) : 0;
-        const int per = pieces_each(n_pieces, gridDim.x);
+        total = units[P.a.n_groups];
+        n_pieces = total ? pieces_of(total, blocks) : 0;
+        const int per = pieces_each(n_pieces, blocks);
         piece = blockIdx.x * per;
         last = min(n_pieces, piece + per);
         if (piece >= last) return false;
         const long long u = first_tile(total, n_pieces, piece);
-        group = last_at(units, P.n_groups, u);
-        g = group_of(P, group);
+        group = last_at(units, P.a.n_groups, u);
+        g = group_of(P.a, group);
         task = tasks[group];
         no = (int)((u - units[group]) / g.tiles);
         tile = (int)((u - units[group]) - (long long)no * g.tiles);
@@ -202,8 +183,8 @@ __device__ __forceinline__ void plan_role(const PrefixArgs &P, const PrefixRoom 
             while (k.no >= (k.g.tiles ? k.g.row_tiles * P.a.c.n_kv : 0)) {
                 if (k.g.tiles) k.task += k.g.row_tiles * P.a.c.n_kv;
                 k.no = 0;
-                if (++k.group >= P.n_groups) return;    // (not reached: the list ends with the last piece)
-                k.g = group_of(P, k.group);
+                if (++k.group >= P.a.n_groups) return;    // (not reached: the list ends with the last piece)
+                k.g = group_of(P.a, k.group);
             }
             Stretch s;
             s.group = k.group; s.first = k.g.first; s.members = k.g.rows; s.len = k.g.len;
@@ -249,7 +230,7 @@ __device__ __forceinline__ void copy_role(const PrefixArgs &P, const PrefixRoom 
     bool good = true;
     Stretch s;
     for (unsigned run = 0; good && R.next(plan, run, s); R.done(run), run++) {
-        const int32_t *row = P.ptable + (int64_t)s.group * P.pcols;
+        const int32_t *row = P.ptable + (int64_t)s.group * P.a.pcols;
         auto page_of = [&](int tile) {                  // lane i: page of the tile's i-th run, negative: none
             const int tok = tile * kTok + (lane << run_log2);
             return lane < runs && tile < s.end && tok < s.len ? row[tok >> page_log2] : -1;
@@ -694,8 +675,9 @@ __global__ void __launch_bounds__(kPrefixThreads, 1) prefix_kernel(const __grid_
     long long *units = reinterpret_cast<long long *>(prefix_smem);
     int *tasks = reinterpret_cast<int *>(units + PF_PREFIX_MAX_GROUPS + 1);
     group_prefix(P, units, tasks, tasks + PF_PREFIX_MAX_GROUPS + 1);
+    const int blocks = prefix_share(units[P.a.n_groups], own_tiles(P.a, reinterpret_cast<long long *>(prefix_smem + 16384)), gridDim.x);
     Walk walk;
-    if (!walk.begin(P, units, tasks)) return;
+    if (!walk.begin(P, units, tasks, blocks)) return;
     uint32_t *words = reinterpret_cast<uint32_t *>(prefix_smem + S::kBars + 8 * B_COUNT);
     uint32_t *gave_up = words + 1;
     Stretch *plan = reinterpret_cast<Stretch *>(prefix_smem + S::kPlan);
@@ -766,15 +748,15 @@ __global__ void __launch_bounds__(256) prefix_join_kernel(const __grid_constant_
     const AttnArgs &A = P.a;
     extern __shared__ __align__(128) uint8_t smem[];
     long long *units = reinterpret_cast<long long *>(smem);
-    int *tasks = reinterpret_cast<int *>(units + P.n_groups + 1);
-    int *prefix = tasks + P.n_groups + 1;
+    int *tasks = reinterpret_cast<int *>(units + P.a.n_groups + 1);
+    int *prefix = tasks + P.a.n_groups + 1;
     __shared__ int warp_sum[8];
     __shared__ __align__(8) int scratch[100];
     group_prefix(P, units, tasks, scratch);
     tile_prefix(A, prefix, warp_sum);
     const int lane = threadIdx.x & 31;
-    const long long total = units[P.n_groups], own_total = (long long)prefix[A.n_seq] * A.jobs_per_seq;
-    const int n_pieces = total ? pieces_of(total, prefix_grid) : 0, each = pieces_each(n_pieces, prefix_grid), own_blocks = blocks_used(own_total, own_grid);
+    const long long total = units[P.a.n_groups], own_total = (long long)prefix[A.n_seq] * A.jobs_per_seq;
+    const int share = prefix_share(total, own_total, prefix_grid), n_pieces = total ? pieces_of(total, share) : 0, each = pieces_each(n_pieces, share), own_blocks = own_total ? blocks_used(own_total, own_grid - share) : 1;
     asm volatile("griddepcontrol.wait;" ::: "memory");
     const float *blocks = A.part + (int64_t)own_grid * S::kWarps * S::kPartFloats;
     const long long n_rows = (long long)A.n_seq * A.n_heads;
@@ -795,8 +777,8 @@ __global__ void __launch_bounds__(256) prefix_join_kernel(const __grid_constant_
         long long slot = 0;
         int n_pre = 0, at = 0, p0 = 0, both = 1;  // parts of a slot
         if (total) {
-            const int gi = P.cu ? last_at(P.cu, P.n_groups, b) : 0;
-            const Group g = group_of(P, gi);
+            const int gi = P.a.cu ? last_at(P.a.cu, P.a.n_groups, b) : 0;
+            const Group g = group_of(P.a, gi);
             if (g.tiles && b >= g.first && b < g.first + g.rows / A.group) {
                 at = (b - g.first) * A.group + gh;
                 const int no = kv * g.row_tiles + at / kRows;
@@ -878,8 +860,7 @@ static PrefixSizes prefix_sizes(int hd, int page, int n_kv, int n_seq, int n_hea
     s.slots = s.status + up((size_t)sms * 4);
     const long long tiles = ((long long)pcols * page + kTok - 1) / kTok;
     const long long tasks = (long long)n_kv * (((long long)n_seq * (n_heads / n_kv)) / kRows + n_groups);
-    const long long per = (tasks * tiles + (long long)sms * kMostTiles - 1) / ((long long)sms * kMostTiles);
-    s.n_slots = tasks + (per > 1 ? per : 1) * sms;
+    s.n_slots = tasks + tasks * tiles / kMostTiles + 2 * sms;      // a slot for each piece of each task
     s.bytes = s.slots + (size_t)s.n_slots * kRows * (hd + 2) * 4;
     return s;
 }
@@ -891,7 +872,7 @@ static int prefix_launch(PrefixArgs p, int device, int sms, cudaStream_t st)
     AttnArgs &a = p.a;
     a.row_blocks = (a.group + S::kHeads - 1) / S::kHeads;
     a.jobs_per_seq = a.c.n_kv * a.row_blocks;
-    const size_t groups = (size_t)(p.n_groups + 1) * 12, own = ((size_t)a.n_seq + 1) * 4;
+    const size_t groups = (size_t)(p.a.n_groups + 1) * 12, own = ((size_t)a.n_seq + 1) * 4;
     const size_t smem0 = PrefixShape<HD>::kBytes, smem1 = (size_t)S::kWarps * S::kWarpBytes + own, smem2 = groups + own;
     PF_CUDA_TRY(ensure_dynamic_smem((const void *)prefix_kernel<T, HD>, device, smem0), "prefix_kernel shared memory");
     PF_CUDA_TRY(ensure_dynamic_smem((const void *)attention_kernel<T, HD, NB, true>, device, smem1), "attention_kernel shared memory");
@@ -962,8 +943,8 @@ extern "C" int pf_prefix_attention(const pf_kv_cache_t *cache, int32_t dtype, in
     a.scale_log2 = sm_scale * kLog2e;
     a.part = (float *)ws;
     a.own_v = (float *)(ws + z.own_v); a.own_z = (float *)(ws + z.own_z); a.own_l = (float *)(ws + z.own_l);
-    p.cu = d_cu_seqs; p.plen = d_prefix_len; p.ptable = d_prefix_table;
-    p.n_groups = n_groups; p.pcols = prefix_cols; p.n_slots = z.n_slots;
+    a.cu = d_cu_seqs; a.plen = d_prefix_len; p.ptable = d_prefix_table;
+    a.n_groups = n_groups; a.pcols = prefix_cols; p.n_slots = z.n_slots;
     p.status = (uint32_t *)(ws + z.status);
     p.slots = (float *)(ws + z.slots);
     p.wait_limit = kWaitLimit;
