@@ -15,7 +15,7 @@ namespace pf {
 
 constexpr int kMostTiles = 512;          // tiles of a piece at most: 32-bit sums do not run over more than 65536 tokens
 constexpr int kAhead = 4;                // tiles that are under way from HBM to the L2
-constexpr int kLeastTiles = 4;           // a piece takes no fewer while others have none
+constexpr int kLeastTiles = 1;           // a piece takes no fewer while others have none
 constexpr unsigned kWaitLimit = 500000, kDrainLimit = 500000;      // polls of 2 us: a second
 constexpr float kSetLift = 7.f;          // log2 of the largest weight when a row's reference is set; it may grow to kLift
 

@@ -4,7 +4,7 @@
 //
 // Angles.  f_i is held as a fraction of a turn in 64 bits, F_i = f_i / (2 pi) * 2^64, so that the angle modulo a turn is the product
 // p F_i modulo 2^64: two 32-bit multiplications, exact for every 32-bit position, where a product of 32-bit floats would be off by
-// p 2^-24 radians (0.06 at 2^20).  Its upper 32 bits, signed, are half turns in [-1, 1), which sincospif takes (2^-24).
+// p 2^-24 radians (0.06 at 2^20).  Its upper 32 bits, signed, are half turns in [-1, 1).
 #include <math.h>
 
 #include "pf_ops.cuh"
@@ -17,55 +17,82 @@ struct Rot {
     float amp, flip;          // m, and -1 where the transposed rotation is asked for
 };
 
+// cosine and sine of a pair's angle.  For results in 16 or 8 bits the special-function unit's, within 2^-21.4 between -pi and pi, an eighth of fp16's half step
+// (sincospif's took a third of the time of prompts' keys, which need them for every head); for results in 32 bits sincospif's.
+template <bool FAST>
 __device__ __forceinline__ void turn_of(const Rot &r, int pair, int32_t pos, float &c, float &s)
 {
     const uint64_t f = __ldg(r.phase + pair);
-    const uint32_t t = (uint32_t)(((uint64_t)(int64_t)pos * f) >> 32);
-    sincospif((float)(int32_t)t * 4.656612873077393e-10f, &s, &c);      // 2^-31
+    const float t = (float)(int32_t)(uint32_t)(((uint64_t)(int64_t)pos * f) >> 32);
+    if (FAST) {
+        const float x = t * 1.4629180792671596e-9f;                     // pi 2^-31
+        c = __cosf(x);
+        s = __sinf(x);
+    } else {
+        sincospif(t * 4.656612873077393e-10f, &s, &c);                  // 2^-31
+    }
     c *= r.amp;
     s *= r.amp * r.flip;
 }
 
-// a thread's 16 elements of a head are two runs of 8: neighbours where pairs are neighbours or nothing turns, and the runs that turn
-// with one another where a head's halves do
+// A thread's 16 elements of a head are two runs of 8, and the runs of neighbouring threads are neighbours: where a head's halves turn with one another, the
+// runs that do so; where neighbours do, a run of either half of the head.
 template <bool HALF>
-__device__ __forceinline__ void runs_of(int chunk, int rot, int &a, int &b)
-{
-    const bool turns = chunk * 16 < rot;
-    a = HALF && turns ? 8 * chunk : 16 * chunk;
-    b = HALF && turns ? rot / 2 + 8 * chunk : 16 * chunk + 8;
-}
-template <bool HALF>
-__device__ __forceinline__ void turn16(float (&a)[8], float (&b)[8], const float (&c)[8], const float (&s)[8])
-{
-    if (HALF) {
-#pragma unroll
-        for (int j = 0; j < 8; j++) {
-            const float x = a[j], y = b[j];
-            a[j] = fmaf(x, c[j], -y * s[j]);
-            b[j] = fmaf(y, c[j], x * s[j]);
-        }
-    } else {
-#pragma unroll
-        for (int j = 0; j < 4; j++) {
-            const float x = a[2 * j], y = a[2 * j + 1], u = b[2 * j], v = b[2 * j + 1];
-            a[2 * j] = fmaf(x, c[j], -y * s[j]);
-            a[2 * j + 1] = fmaf(y, c[j], x * s[j]);
-            b[2 * j] = fmaf(u, c[4 + j], -v * s[4 + j]);
-            b[2 * j + 1] = fmaf(v, c[4 + j], u * s[4 + j]);
+struct Runs {
+    int a, b;                 // where they begin
+    bool turns_a, turns_b;
+    __device__ __forceinline__ Runs(int chunk, int rot, int hd)
+    {
+        if (!HALF || rot == 0) {
+            a = 8 * chunk;
+            b = hd / 2 + 8 * chunk;
+            turns_a = a < rot;
+            turns_b = b < rot;
+        } else {
+            const int k = chunk - rot / 16;
+            turns_a = turns_b = k < 0;
+            a = turns_a ? 8 * chunk : rot + 8 * k;
+            b = turns_a ? rot / 2 + 8 * chunk : rot + (hd - rot) / 2 + 8 * k;
         }
     }
-}
-__device__ __forceinline__ void turns8(const Rot &r, int chunk, int32_t pos, float (&c)[8], float (&s)[8])
-{
+    template <bool FAST>
+    __device__ __forceinline__ void angles(const Rot &r, int32_t pos, float (&c)[8], float (&s)[8]) const
+    {
 #pragma unroll
-    for (int j = 0; j < 8; j++) turn_of(r, 8 * chunk + j, pos, c[j], s[j]);
-}
+        for (int j = 0; j < 8; j++) {
+            if (HALF) {
+                if (turns_a) turn_of<FAST>(r, a + j, pos, c[j], s[j]);
+            } else if (j < 4 ? turns_a : turns_b) {
+                turn_of<FAST>(r, (j < 4 ? a : b) / 2 + (j & 3), pos, c[j], s[j]);
+            }
+        }
+    }
+    __device__ __forceinline__ void turn(float (&x)[8], float (&y)[8], const float (&c)[8], const float (&s)[8]) const
+    {
+        if (HALF) {
+            if (!turns_a) return;
+#pragma unroll
+            for (int j = 0; j < 8; j++) {
+                const float u = x[j], v = y[j];
+                x[j] = fmaf(u, c[j], -v * s[j]);
+                y[j] = fmaf(v, c[j], u * s[j]);
+            }
+        }
+#pragma unroll
+        for (int j = 0; j < 8 && !HALF; j++) {
+            if (!(j < 4 ? turns_a : turns_b)) continue;
+            float &u = j < 4 ? x[2 * (j & 3)] : y[2 * (j & 3)], &v = j < 4 ? x[2 * (j & 3) + 1] : y[2 * (j & 3) + 1];
+            const float p = u, q = v;
+            u = fmaf(p, c[j], -q * s[j]);
+            v = fmaf(q, c[j], p * s[j]);
+        }
+    }
+};
 
-// 8 neighbouring elements as they lie in memory
+// 8 neighbouring elements as they lie in memory, read and written once: not to be kept in caches
 template <typename T> struct Run8 {
     uint4 w;
-    __device__ __forceinline__ void load(const T *p) { w = *reinterpret_cast<const uint4 *>(p); }
+    __device__ __forceinline__ void load(const T *p) { w = __ldcs(reinterpret_cast<const uint4 *>(p)); }
     __device__ __forceinline__ void get(float (&v)[8]) const
     {
         const uint32_t u[4] = {w.x, w.y, w.z, w.w};
@@ -79,23 +106,23 @@ template <typename T> struct Run8 {
 };
 template <> struct Run8<float> {
     float4 a, b;
-    __device__ __forceinline__ void load(const float *p) { a = reinterpret_cast<const float4 *>(p)[0]; b = reinterpret_cast<const float4 *>(p)[1]; }
+    __device__ __forceinline__ void load(const float *p) { a = __ldcs(reinterpret_cast<const float4 *>(p)); b = __ldcs(reinterpret_cast<const float4 *>(p) + 1); }
     __device__ __forceinline__ void get(float (&v)[8]) const
     {
         v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w;
         v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
     }
 };
-template <typename T> __device__ __forceinline__ void get8(const T *p, float (&v)[8])
+template <typename T> __device__ __forceinline__ void get8(const T *p, float (&v)[8])      // to be read again
 {
     Run8<T> r;
-    r.load(p);
+    r.w = *reinterpret_cast<const uint4 *>(p);
     r.get(v);
 }
 template <typename T> __device__ __forceinline__ void put8(T *p, const float (&v)[8])
 {
-    *reinterpret_cast<uint4 *>(p) =
-        make_uint4(pair_of_f32<T>(v[0], v[1]), pair_of_f32<T>(v[2], v[3]), pair_of_f32<T>(v[4], v[5]), pair_of_f32<T>(v[6], v[7]));
+    __stcs(reinterpret_cast<uint4 *>(p),
+        make_uint4(pair_of_f32<T>(v[0], v[1]), pair_of_f32<T>(v[2], v[3]), pair_of_f32<T>(v[4], v[5]), pair_of_f32<T>(v[6], v[7])));
 }
 template <> __device__ __forceinline__ void put8<float>(float *p, const float (&v)[8])
 {
@@ -118,24 +145,21 @@ struct RopeArgs {
     int heads, hd, per, groups;   // heads a thread takes, and groups of so many
 };
 
-// `n` heads of one token from `head`: 16 elements of each
-template <typename T, bool HALF>
-__device__ __forceinline__ void rope_heads(const Rot &r, int32_t pos, int chunk, const T *x, int64_t xh, T *y, int64_t yh, int n)
+// 16 elements of each of `n` heads of one token, B heads at a time
+template <typename T, bool HALF, int B>
+__device__ __forceinline__ void rope_heads(const Rot &r, int32_t pos, int hd, int chunk, const T *x, int64_t xh, T *y, int64_t yh, int n)
 {
-    int at, bt;
-    runs_of<HALF>(chunk, r.rot, at, bt);
-    const bool turns = chunk * 16 < r.rot;
+    const Runs<HALF> run(chunk, r.rot, hd);
     float c[8], s[8];
-    if (turns) turns8(r, chunk, pos, c, s);
+    run.template angles<sizeof(T) == 2>(r, pos, c, s);
     // x and y may be one tensor, so the loads of a few heads are asked for before the first store
-    constexpr int B = sizeof(T) == 4 ? 2 : 4;
     for (int h = 0; h < n; h += B) {
         Run8<T> in[B][2];
 #pragma unroll
         for (int i = 0; i < B; i++)
             if (h + i < n) {
-                in[i][0].load(x + (h + i) * xh + at);
-                in[i][1].load(x + (h + i) * xh + bt);
+                in[i][0].load(x + (h + i) * xh + run.a);
+                in[i][1].load(x + (h + i) * xh + run.b);
             }
 #pragma unroll
         for (int i = 0; i < B; i++)
@@ -143,9 +167,9 @@ __device__ __forceinline__ void rope_heads(const Rot &r, int32_t pos, int chunk,
                 float a[8], b[8];
                 in[i][0].get(a);
                 in[i][1].get(b);
-                if (turns) turn16<HALF>(a, b, c, s);
-                put8<T>(y + (h + i) * yh + at, a);
-                put8<T>(y + (h + i) * yh + bt, b);
+                run.turn(a, b, c, s);
+                put8<T>(y + (h + i) * yh + run.a, a);
+                put8<T>(y + (h + i) * yh + run.b, b);
             }
     }
 }
@@ -160,7 +184,8 @@ __global__ void __launch_bounds__(256) rope_kernel(const RopeArgs A)
     u /= chunks;
     const int first = (int)(u % A.groups) * A.per;
     const int64_t t = u / A.groups;
-    rope_heads<T, HALF>(A.r, A.pos[t], chunk, (const T *)A.x + t * A.xt + first * A.xh, A.xh, (T *)A.y + t * A.yt + first * A.yh, A.yh,
+    // (8192 tokens of 40 heads: 29 us with four heads' loads under way, 36 with two)
+    rope_heads<T, HALF, sizeof(T) == 4 ? 2 : 4>(A.r, A.pos[t], A.hd, chunk, (const T *)A.x + t * A.xt + first * A.xh, A.xh, (T *)A.y + t * A.yt + first * A.yh, A.yh,
                         min(A.per, A.heads - first));
 }
 
@@ -182,7 +207,7 @@ __global__ void __launch_bounds__(256) rope_any_kernel(const RopeArgs A)
         return;
     }
     float c, s;
-    turn_of(A.r, i, A.pos[t], c, s);
+    turn_of<sizeof(T) == 2>(A.r, i, A.pos[t], c, s);
     const int a = HALF ? i : 2 * i, b = HALF ? i + pairs : 2 * i + 1;
     const float p = get1<T>(x + a), q = get1<T>(x + b);
     put1<T>(y + a, fmaf(p, c, -q * s));
@@ -246,7 +271,8 @@ __device__ __forceinline__ void append_query(const AppendRopeArgs &A, int64_t u)
         if (t < cu0 || t >= cu0 + n) return;
     }
     const int32_t pos = A.pos ? A.pos[t] : (int32_t)((int64_t)max(0, A.len[b]) + (t - cu0));
-    rope_heads<T, HALF>(A.r, pos, chunk, (const T *)A.q + t * A.qs + first * HD, HD, (T *)A.qo + t * A.qos + first * HD, HD, min(A.per, A.n_heads - first));
+    // two heads at a time: the registers of four would leave the units' blocks fewer places (six prompts of up to 4096 tokens: 70 us instead of 76)
+    rope_heads<T, HALF, 2>(A.r, pos, HD, chunk, (const T *)A.q + t * A.qs + first * HD, HD, (T *)A.qo + t * A.qos + first * HD, HD, min(A.per, A.n_heads - first));
 }
 
 template <typename T, int HD, int R, bool HALF>
@@ -285,17 +311,14 @@ __global__ void __launch_bounds__(R == 1 ? 256 : 128) append_rope_kernel(const A
     if (page < 0 || page >= A.c.n_pages) cnt = 0;
     const int64_t xs = which ? A.vs : A.ks;
     const T *x = (const T *)(which ? A.v : A.k) + t0 * xs + h * HD;
-    const bool turns = !which && lane * 16 < A.r.rot;
-    int at = 16 * lane, bt = at + 8;
-    if (!which) runs_of<HALF>(lane, A.r.rot, at, bt);
+    const Runs<HALF> run(lane, which ? 0 : A.r.rot, HD);
     float f[8], g[8];
     auto fetch = [&](int t) {
-        get8<T>(x + t * xs + at, f);
-        get8<T>(x + t * xs + bt, g);
-        if (!turns) return;
+        get8<T>(x + t * xs + run.a, f);
+        get8<T>(x + t * xs + run.b, g);
         float c[8], s[8];
-        turns8(A.r, lane, A.pos ? A.pos[t0 + t] : (int32_t)(lo + t), c, s);
-        turn16<HALF>(f, g, c, s);
+        run.template angles<true>(A.r, A.pos ? A.pos[t0 + t] : (int32_t)(lo + t), c, s);
+        run.turn(f, g, c, s);
     };
     float m = 0.f;
     for (int t = r; t < cnt; t += R) {
@@ -342,8 +365,8 @@ __global__ void __launch_bounds__(R == 1 ? 256 : 128) append_rope_kernel(const A
     for (int t = r; t < cnt; t += R) {
         if (cnt > R) fetch(t);                    // else the thread's one token is still here
         uint8_t *to = bytes + (s0 + t) * HD;
-        *reinterpret_cast<uint2 *>(to + at) = make_uint2(e4m3x4(f[0] * inv, f[1] * inv, f[2] * inv, f[3] * inv), e4m3x4(f[4] * inv, f[5] * inv, f[6] * inv, f[7] * inv));
-        *reinterpret_cast<uint2 *>(to + bt) = make_uint2(e4m3x4(g[0] * inv, g[1] * inv, g[2] * inv, g[3] * inv), e4m3x4(g[4] * inv, g[5] * inv, g[6] * inv, g[7] * inv));
+        *reinterpret_cast<uint2 *>(to + run.a) = make_uint2(e4m3x4(f[0] * inv, f[1] * inv, f[2] * inv, f[3] * inv), e4m3x4(f[4] * inv, f[5] * inv, f[6] * inv, f[7] * inv));
+        *reinterpret_cast<uint2 *>(to + run.b) = make_uint2(e4m3x4(g[0] * inv, g[1] * inv, g[2] * inv, g[3] * inv), e4m3x4(g[4] * inv, g[5] * inv, g[6] * inv, g[7] * inv));
     }
 }
 

@@ -1,7 +1,8 @@
 """pf_rope and pf_kv_append_rope against plain implementations in 64 bits.
 
-Tolerances.  An angle is exact to 2^-32 turns; its upper 32 bits become a 32-bit float (2^-25 turns at most) and sine and cosine carry 2^-23, so
-with pair length r = |(a, b)| and amplitude m an element is off by at most m r (2 pi 2^-25 + 3 * 2^-23) < m r 2^-20, plus half a step of the output type.
+Tolerances.  An angle is exact to 2^-32 turns; its upper 32 bits become a 32-bit float (2^-25 turns, 2 pi 2^-25 radians, at most).  Sine and cosine carry
+2^-21.41 where the result has 16 or 8 bits (the special-function unit's bound between -pi and pi), less otherwise; so with pair length r = |(a, b)| and
+amplitude m an element is off by at most m r (sqrt(2) 2^-21.41 + 2 pi 2^-25) < m r 2^-20, plus half a step of the output type.
 The cache's bytes are compared with what the rounding of any value within that distance gives."""
 from __future__ import annotations
 
