@@ -61,6 +61,10 @@ int pf_check_selftest(pf_plan_t *plan);
  * Errors: PF_ERANGE. */
 int pf_moe_meeting(uint32_t polls, uint32_t missing);
 
+/* The waits inside the kernel of pf_prefix_attention, for a test of their limit: the next calls' waits end after `polls` polls of some 2 us (0: the
+ * default, about a second), and with lost = 1 one block waits for something that does not come.  PF_ERANGE: polls > 2^21, lost > 1. */
+int pf_prefix_waits(uint32_t polls, uint32_t lost);
+
 /* How the plan's latest scoring call inside pf_search was divided between the scoring kernel and the kernel that
  * streams constant blocks: the number of blocks of candidates the call's range was cut into, candidates per block,
  * how many blocks the scoring kernel took itself (the evaluated ones), and how many the fill kernel counted as

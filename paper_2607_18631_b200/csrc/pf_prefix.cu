@@ -8,6 +8,8 @@
 // through the kernel of pf_decode_attention, and a third kernel joins the parts of every row in a fixed order.
 #include <math.h>
 
+#include <atomic>
+
 #include "pf_attention.cuh"
 #include "pf_tcgen.cuh"
 
@@ -17,12 +19,13 @@ constexpr int kMostTiles = 512;          // tiles of a piece at most: 32-bit sum
 constexpr int kAhead = 4;                // tiles that are under way from HBM to the L2
 constexpr int kLeastTiles = 1;           // a piece takes no fewer while others have none
 constexpr unsigned kWaitLimit = 500000, kDrainLimit = 500000;      // polls of 2 us: a second
+std::atomic<unsigned> g_wait_limit{kWaitLimit}, g_wait_lost{0};      // host: what the next calls do (pf_prefix_waits)
 constexpr float kSetLift = 7.f;          // log2 of the largest weight when a row's reference is set; it may grow to kLift
 
 struct PrefixArgs {
     AttnArgs a;
     const int32_t *ptable;
-    unsigned wait_limit;                 // polls of a wait inside the kernel
+    unsigned wait_limit, wait_lost;      // polls of a wait inside the kernel; whether a block waits for what does not come (a test of the limit)
     long long n_slots;
     uint32_t *status;                    // [blocks], written by those with work
     float *slots;                        // [n_slots] x (kRows x HD values, kRows references, kRows sums)
@@ -367,6 +370,7 @@ __device__ __forceinline__ void product_role(const PrefixArgs &P, const PrefixRo
     constexpr uint32_t kScores = mma_shape(kTok, false), kValues = mma_shape(HD, true);
     const uint32_t tmem = kTmem, smem = R.smem, bars = R.bars;
     const bool one = elected();
+    if (P.wait_lost && blockIdx.x == 0 && !R.wait_warp(B_DRAIN, 0)) return;      // nothing arrives there before the end
     unsigned n = 0, runs = 0, weights[2] = {0, 0};      // tiles and stretches so far; each stream's tiles of weights
     auto commit = [&](int bar) {
         if (one) mma_commit(bars + 8 * bar);
@@ -947,7 +951,16 @@ extern "C" int pf_prefix_attention(const pf_kv_cache_t *cache, int32_t dtype, in
     a.n_groups = n_groups; a.pcols = prefix_cols; p.n_slots = z.n_slots;
     p.status = (uint32_t *)(ws + z.status);
     p.slots = (float *)(ws + z.slots);
-    p.wait_limit = kWaitLimit;
+    p.wait_limit = g_wait_limit;
+    p.wait_lost = g_wait_lost;
     cudaStream_t st = (cudaStream_t)stream;
     return dtype == PF_DT_BF16 ? prefix_launch<Bf16>(p, device, sms, st) : prefix_launch<F16>(p, device, sms, st);
+}
+
+extern "C" int pf_prefix_waits(uint32_t polls, uint32_t lost)
+{
+    if (polls > (1u << 21) || lost > 1) return PF_ERANGE;
+    g_wait_limit = polls ? polls : kWaitLimit;
+    g_wait_lost = lost;
+    return PF_OK;
 }

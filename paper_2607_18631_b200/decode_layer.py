@@ -7,7 +7,9 @@ its step with the operators of `ops`; the projections are plain matrix products.
 `with_measured_hbm` puts the rate they reached into a plan space's cluster, so that the space is ranked again with it.
 (The model's other measured numbers, the efficiencies by tokens an expert, stay as they are.)
 
-    python -m paper_2607_18631_b200.decode_layer [--batch N] [--context N]
+    python -m paper_2607_18631_b200.decode_layer [--batch N] [--context N] [--prefix N] [--rope BASE]
+
+With `rotary`, queries and keys are rotated to their positions; with `prefix`, all sequences share that many tokens in front of their own.
 
 Plans with latent attention (attn_kind 1) are refused: the cache here holds keys and values per head.  Collectives
 between the GPUs of a plan are not run (a step's results are this GPU's parts).
@@ -52,9 +54,10 @@ def layer_shape(cfg: dict, plan: dict) -> dict:
 
 class DecodeLayer:
     """A layer's weights and cache on the current device, and its decode step.  shape: see layer_shape (expert_tokens, if left out, is
-    tokens, and shared_ffn is ffn); context: cached tokens of every sequence at the start."""
+    tokens, and shared_ffn is ffn); context: cached tokens of every sequence at the start; prefix: tokens in front of them that all sequences share;
+    rotary: arguments of ops.Rotary, its `rot` among them."""
 
-    def __init__(self, shape: dict, context: int, page: int = 64, seed: int = 0):
+    def __init__(self, shape: dict, context: int, page: int = 64, seed: int = 0, prefix: int = 0, rotary: dict | None = None):
         import torch
 
         from . import ops
@@ -95,19 +98,39 @@ class DecodeLayer:
         self.others = ops.pf_add_rms_norm(others, None, self.norm2, y=True) if others.shape[0] else None
         cols = -(-(context + CAP_SLACK) // page)
         self.table = torch.randperm(T * cols, generator=g, device=dev).to(torch.int32).reshape(T, cols)
-        self.cache = [torch.empty(T * cols, nkv, page, d, dtype=torch.float8_e4m3fn, device=dev) for _ in range(2)]
-        self.scales = [torch.empty(T * cols, nkv, device=dev) for _ in range(2)]
+        if prefix < 0:
+            raise PlanfrontError(PF_EINVAL, f"decode_layer: a prefix of {prefix} tokens")
+        prefix_pages = -(-prefix // page)
+        self.cache = [torch.empty(T * cols + prefix_pages, nkv, page, d, dtype=torch.float8_e4m3fn, device=dev) for _ in range(2)]
+        self.scales = [torch.empty(T * cols + prefix_pages, nkv, device=dev) for _ in range(2)]
+        self.rotary = None if rotary is None else ops.Rotary(**rotary)
+        self.prefix = prefix
         self.lengths = torch.zeros(T, dtype=torch.int32, device=dev)
         self.one_each = torch.arange(T + 1, dtype=torch.int32, device=dev)
         self.room = cols * page
-        at = 0
-        while at < context:         # the prompts, in chunks, as a prefill appends them
-            m = min(context - at, 1024)
-            k, v = (torch.randn(T * m, nkv, d, generator=g, device=dev).to(torch.bfloat16) for _ in range(2))
-            ops.pf_kv_append(*self.cache, *self.scales, k, v, self.one_each * m, self.lengths, self.table, max_new=m)
-            self.lengths += m
-            at += m
+
+        def prompt(n, seqs, lengths, table, first):         # in chunks, as a prefill appends it
+            at = 0
+            while at < n:
+                m = min(n - at, 1024)
+                k, v = (torch.randn(seqs * m, nkv, d, generator=g, device=dev).to(torch.bfloat16) for _ in range(2))
+                self.append(None, k, v, self.one_each[:seqs + 1] * m, lengths, table, m, (lengths[:, None] + torch.arange(first, first + m, device=dev)).flatten().int())
+                lengths += m
+                at += m
+
+        prompt(context, T, self.lengths, self.table, prefix)
+        if prefix:
+            self.prefix_table = torch.arange(T * cols, T * cols + prefix_pages, dtype=torch.int32, device=dev)[None]
+            self.prefix_length = torch.zeros(1, dtype=torch.int32, device=dev)
+            prompt(prefix, 1, self.prefix_length, self.prefix_table, 0)
         self.cached = context
+
+    def append(self, q, k, v, cu_new, lengths, table, max_new, positions):
+        """New keys and values into the cache, rotated to `positions` where the layer does so; returns the queries, rotated likewise."""
+        if self.rotary is None:
+            self.ops.pf_kv_append(*self.cache, *self.scales, k, v, cu_new, lengths, table, max_new=max_new)
+            return q
+        return self.ops.pf_kv_append_rope(*self.cache, *self.scales, q, k, v, cu_new, lengths, table, self.rotary, max_new=max_new, positions=positions)
 
     def step(self, x, residual):
         """One token of every sequence through the layer: x is what the layer before added, residual the stream it adds to (updated
@@ -117,7 +140,7 @@ class DecodeLayer:
             raise PlanfrontError(PF_EINVAL, "decode_layer: the cache is full")
         y = ops.pf_add_rms_norm(x, residual, self.norm1, y=True, q=False, sum_out=residual)["y"]
         q, k, v = self.project(y)
-        ops.pf_kv_append(*self.cache, *self.scales, k, v, self.one_each, self.lengths, self.table, max_new=1)
+        q = self.append(q, k, v, self.one_each, self.lengths, self.table, 1, self.lengths + self.prefix if self.prefix and self.rotary else None)
         self.lengths += 1
         self.cached += 1
         a = self.attend(q)
@@ -130,6 +153,8 @@ class DecodeLayer:
         return qkv.split((s["heads"], s["kv_heads"], s["kv_heads"]), 1)
 
     def attend(self, q):
+        if self.prefix:
+            return self.ops.pf_prefix_attention(q, *self.cache, *self.scales, self.lengths, self.table, self.prefix_length, self.prefix_table)["out"]
         return self.ops.pf_decode_attention(q, *self.cache, *self.scales, self.lengths, self.table)["out"]
 
     def gather(self, n):
@@ -164,7 +189,7 @@ class DecodeLayer:
         ids = self.moe.forward(whole["y"])["ids"]
         touched = int(torch.unique(ids[ids < s["local"]]).numel())
         element = 1 if s["weights"] == "e4m3" else 2
-        cache_bytes = int(self.lengths.sum()) * s["kv_heads"] * s["head_dim"] * 2
+        cache_bytes = (int(self.lengths.sum()) + self.prefix) * s["kv_heads"] * s["head_dim"] * 2
         expert_bytes = 3 * s["hidden"] * (touched * s["ffn"] + s["shared"] * s["shared_ffn"]) * element
 
         def experts():
@@ -235,12 +260,14 @@ def main(argv=None) -> None:
     ap.add_argument("--batch", type=int, default=64)
     ap.add_argument("--context", type=int, default=4096)
     ap.add_argument("--steps", type=int, default=4)
+    ap.add_argument("--prefix", type=int, default=0, help="tokens in front of the context that all sequences share")
+    ap.add_argument("--rope", type=float, default=0.0, metavar="BASE", help="rotate queries and keys, with frequencies of this base")
     a = ap.parse_args(argv)
     cfg = example_space(a.batch, a.context)
     plan, tput = best_plan(cfg)
     shape = layer_shape(cfg, plan)
     print(f"plan: tp {plan['tp']} ep {plan['ep']} kernel {shape['weights']} batch {plan['batch']}: predicted {tput:.1f} tokens/s/GPU")
-    layer = DecodeLayer(shape, a.context)
+    layer = DecodeLayer(shape, a.context, prefix=a.prefix, rotary=dict(rot=shape["head_dim"], base=a.rope) if a.rope else None)
     x = torch.randn(shape["tokens"], shape["hidden"], device="cuda").to(torch.bfloat16)
     residual = torch.zeros_like(x)
     for _ in range(a.steps):
@@ -250,6 +277,8 @@ def main(argv=None) -> None:
     for name, (us, size) in parts.items():
         rate = f"{size / us / 1e6:6.2f} TB/s" if size >= MIN_RATE_BYTES else "(latency)"
         print(f"{name:10s} {us:9.1f} us  {size / 1e6:9.1f} MB  {rate}")
+    if a.prefix:
+        del parts["attention"]      # the model prices every sequence's whole context, so the rate of a shared one is not its rate
     again = with_measured_hbm(cfg, parts)
     plan, tput = best_plan(again)
     print(f"with {again['cluster']['hbm_bw'] / 1e12:.2f} TB/s: tp {plan['tp']} ep {plan['ep']}, predicted {tput:.1f} tokens/s/GPU")
