@@ -267,7 +267,7 @@ __device__ __forceinline__ void copy_role(const PrefixArgs &P, const PrefixRoom 
                 __syncwarp();
                 scales_of(next);
             }
-#pragma unroll
+#pragma unroll 1
             for (int h = 0; h < 2; h++) {
                 const bool mine = lane >> (6 - run_log2) == h && bytes > 0;
                 const int all = __reduce_add_sync(0xFFFFFFFFu, mine ? bytes : 0);
@@ -277,7 +277,8 @@ __device__ __forceinline__ void copy_role(const PrefixArgs &P, const PrefixRoom 
                     asm volatile("st.shared.u32 [%0], %1;" ::"r"(have_at + 4 * h), "r"(have) : "memory");
                     bar_expect(R.bars + 8 * (raw + h), all);
                 }
-                asked[h]++;
+                if (h) asked[1]++;
+                else asked[0]++;
                 __syncwarp();
                 if (mine) bulk_in(ring + (lane << run_log2) * HD, from, bytes, R.bars + 8 * (raw + h));
             }
@@ -315,7 +316,7 @@ __device__ __forceinline__ void widen_role(const PrefixRoom &R, const Stretch *p
         for (int t = s.tile; t < s.end; t++, n++) {
             const int stage = n & 1, left = s.len - t * kTok;
             if (!R.wait_warp(empty + stage, ((n >> 1) & 1u) ^ 1u)) return;
-#pragma unroll
+#pragma unroll 1
             for (int h = 0; h < 2; h++) {
                 if (!R.wait_warp(raw + h, n)) return;
                 uint32_t have;                          // runs of the tile that were copied
@@ -481,13 +482,12 @@ __device__ __forceinline__ bool rows_run(const PrefixArgs &P, const PrefixRoom &
     // sm_scale to the factor of the scores.
     float up;
     {
-        uint4 raw[HD / 8];
         const uint16_t *src = A.q + (int64_t)(s.first + at / A.group) * A.qs + (int64_t)(s.kv * A.group + at % A.group) * HD;
         float top = 0.f;
-#pragma unroll
+#pragma unroll 2
         for (int i = 0; i < HD / 8; i++) {
-            raw[i] = live ? *reinterpret_cast<const uint4 *>(src + 8 * i) : make_uint4(0u, 0u, 0u, 0u);
-            const uint32_t w[4] = {raw[i].x, raw[i].y, raw[i].z, raw[i].w};
+            const uint4 raw = live ? *reinterpret_cast<const uint4 *>(src + 8 * i) : make_uint4(0u, 0u, 0u, 0u);
+            const uint32_t w[4] = {raw.x, raw.y, raw.z, raw.w};
 #pragma unroll
             for (int x = 0; x < 4; x++) {
                 const float2 f = pair_to_f32<T>(w[x]);
@@ -499,9 +499,10 @@ __device__ __forceinline__ bool rows_run(const PrefixArgs &P, const PrefixRoom &
         const float down = A.scale_log2 < 0.f ? -exp2f((float)-e) : exp2f((float)-e);
         up = fabsf(A.scale_log2) * exp2f((float)e);
         const uint32_t q = R.smem + S::kQ + j * S::kOperand;
-#pragma unroll
+#pragma unroll 2
         for (int i = 0; i < HD / 8; i++) {
-            const uint32_t w[4] = {raw[i].x, raw[i].y, raw[i].z, raw[i].w};
+            const uint4 raw = live ? *reinterpret_cast<const uint4 *>(src + 8 * i) : make_uint4(0u, 0u, 0u, 0u);
+            const uint32_t w[4] = {raw.x, raw.y, raw.z, raw.w};
             uint32_t o[4];
 #pragma unroll
             for (int x = 0; x < 4; x++) {
@@ -533,18 +534,26 @@ __device__ __forceinline__ bool rows_run(const PrefixArgs &P, const PrefixRoom &
         if (!R.wait_warp(B_SFULL + j, tiles)) return false;
         tmem_after_sync();
         if (any) {
+            if (left < kTok) {
+                // a last tile: -infinity, so weight 0, for what lies behind the end.  In a loop of its own: what a tile goes through has to fit the instruction cache
+#pragma unroll 1
+                for (int c = left > 0 ? left / 16 : 0; c < 8; c++) {
+                    uint32_t y[16];
+                    tmem_ld16(score + 16 * c, y);
+                    tmem_wait_ld(y);
+#pragma unroll
+                    for (int k = 0; k < 16; k++)
+                        if (16 * c + k >= left) y[k] = 0xFF800000u;
+                    tmem_st16(score + 16 * c, y);
+                }
+                tmem_wait_st();
+            }
             uint32_t x[8][16];                          // the row's scores
 #pragma unroll
             for (int c = 0; c < 8; c++) tmem_ld16(score + 16 * c, x[c]);
             tmem_wait_ld(x[0]);
 #pragma unroll
             for (int c = 1; c < 8; c++) tmem_named(x[c]);
-            if (left < kTok) {
-                asm volatile("" ::: "memory");          // a branch: most tiles are whole, and 128 selections are not to be made in all of them
-#pragma unroll
-                for (int k = 0; k < kTok; k++)
-                    if (k >= left) x[k / 16][k % 16] = 0xFF800000u;      // -infinity: weight 0
-            }
             float top = -INFINITY;
 #pragma unroll
             for (int g = 0; g < 8; g++) {
@@ -664,6 +673,7 @@ __device__ __forceinline__ void rows_role(const PrefixArgs &P, const PrefixRoom 
             }
             tmem_before_sync();
         } else if (live) {
+#pragma unroll 1
             for (int k = 0; k < HD; k += 4) *reinterpret_cast<uint4 *>(to + place * HD + k) = make_uint4(0u, 0u, 0u, 0u);
         }
     }
@@ -721,16 +731,16 @@ __global__ void __launch_bounds__(kPrefixThreads, 1) prefix_kernel(const __grid_
         widen_role<HD>(R, plan);
     } else {
         leave_registers<kProductRegs>();
-        if (warp == kSoftWarps + kWidenWarps) {
+        if (warp == kSoftWarps + kWidenWarps + 3) {
             product_role<HD>(P, R, plan);
             // whatever was begun is done before the block gives its memory back
             __syncwarp();
             if (elected()) mma_commit(R.bars + 8 * B_DRAIN);
             const uint32_t alone = smem_addr(words + 2);
             bar_wait(R.bars + 8 * B_DRAIN, 0, kDrainLimit, alone);
-        } else if (threadIdx.x == 32 * (kSoftWarps + kWidenWarps + 1)) {
+        } else if (threadIdx.x == 32 * (kSoftWarps + kWidenWarps)) {
             plan_role(P, R, walk, plan);
-        } else if (warp >= kSoftWarps + kWidenWarps + 2) {
+        } else if (warp > kSoftWarps + kWidenWarps) {
             copy_role<HD>(P, R, plan, warp & 1);
         }
         __syncwarp();
@@ -831,12 +841,25 @@ __global__ void __launch_bounds__(256) prefix_join_kernel(const __grid_constant_
             sum = fmaf(sum, old, add);
 #pragma unroll
             for (int k = 0; k < V; k++) v[k] *= old;
+            // what the unrolled loop reads past the last part is the first one, with weight 0: no branch between the loads
             const int count = min(32, n - i0);
-            for (int k = 0; k < count; k++) {
-                const float *p = (const float *)__shfl_sync(0xFFFFFFFFu, (unsigned long long)from, k) + lane * V;
-                const float w = __shfl_sync(0xFFFFFFFFu, f, k);
-#pragma unroll
-                for (int j = 0; j < V; j++) v[j] = fmaf(p[j], w, v[j]);
+            const unsigned long long any = __shfl_sync(0xFFFFFFFFu, (unsigned long long)from, 0), mine = from ? (unsigned long long)from : any;
+            const float weight = from ? f : 0.f;
+#pragma unroll 8
+            for (int k = 0; k < (count + 7) / 8 * 8; k++) {
+                const float *p = (const float *)__shfl_sync(0xFFFFFFFFu, mine, k) + lane * V;
+                const float w = __shfl_sync(0xFFFFFFFFu, weight, k);
+                if (V == 4) {
+                    const float4 y = *reinterpret_cast<const float4 *>(p);
+                    v[0] = fmaf(y.x, w, v[0]);
+                    v[1] = fmaf(y.y, w, v[1]);
+                    v[2 % V] = fmaf(y.z, w, v[2 % V]);
+                    v[3 % V] = fmaf(y.w, w, v[3 % V]);
+                } else {
+                    const float2 y = *reinterpret_cast<const float2 *>(p);
+                    v[0] = fmaf(y.x, w, v[0]);
+                    v[1] = fmaf(y.y, w, v[1]);
+                }
             }
         }
         const float inv = sum == 0.f ? 0.f : 1.f / sum;      // (a sum that is not a number stays one)

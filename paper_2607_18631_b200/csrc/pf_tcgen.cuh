@@ -17,26 +17,29 @@ __device__ __forceinline__ void bulk_in(uint32_t dst, const void *src, uint32_t 
 {
     asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src), "r"(bytes), "r"(bar) : "memory");
 }
-__device__ __forceinline__ bool bar_poll(uint32_t b, unsigned parity)
-{
-    uint32_t done;
-    asm volatile("{\n.reg .pred p;\nmbarrier.try_wait.parity.shared.b64 p, [%1], %2, %3;\nselp.u32 %0, 1, 0, p;\n}"
-                 : "=r"(done) : "r"(b), "r"(parity), "r"(2000u) : "memory");
-    return done;
-}
 // Waits for the phase of that parity; false where `limit` polls of some 2 us each did not see it, or where another wait of the block gave up
-// (`gave_up`, one word of shared memory, which this one then sets too).
+// (`gave_up`, the address of a word of shared memory, which this one then sets too).  Written out, so that each of the many places is a dozen instructions: what the
+// warps of a block go through has to fit the instruction cache.
 __device__ __forceinline__ bool bar_wait(uint32_t b, unsigned parity, unsigned limit, uint32_t gave_up)
 {
-    if (bar_poll(b, parity)) return true;
-    for (unsigned i = 0; i < limit; i++) {
-        if (bar_poll(b, parity)) return true;
-        uint32_t over;
-        asm volatile("ld.shared.u32 %0, [%1];" : "=r"(over) : "r"(gave_up) : "memory");
-        if (over) return false;
-    }
-    asm volatile("st.shared.u32 [%0], %1;" ::"r"(gave_up), "r"(1u) : "memory");
-    return false;
+    uint32_t done;
+    asm volatile("{\n.reg .pred p;\n.reg .u32 i, w;\n"
+                 "mov.u32 i, %3;\n"
+                 "AGAIN:\n"
+                 "mbarrier.try_wait.parity.shared.b64 p, [%1], %2, 2000;\n"
+                 "mov.u32 %0, 1;\n"
+                 "@p bra END;\n"
+                 "mov.u32 %0, 0;\n"
+                 "ld.shared.u32 w, [%4];\n"
+                 "setp.ne.u32 p, w, 0;\n"
+                 "@p bra END;\n"
+                 "sub.u32 i, i, 1;\n"
+                 "setp.gt.s32 p, i, 0;\n"
+                 "@p bra AGAIN;\n"
+                 "st.shared.u32 [%4], 1;\n"
+                 "END:\n}"
+                 : "=&r"(done) : "r"(b), "r"(parity), "r"(limit), "r"(gave_up) : "memory");
+    return done;
 }
 // what threads wrote to shared memory becomes visible to the matrix instruction
 __device__ __forceinline__ void publish_shared() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
