@@ -4,8 +4,24 @@
 //
 // A group's rows (sequences times query heads of a key head) are cut into tiles of 256, and such a tile goes through the group's prefix once:
 // the cache is read once for all of them.  All (tile of rows, tile of 128 tokens) pairs of all groups and key heads form one list, which is cut into
-// equal pieces; a piece leaves partial results (reference z, sum, weighted values) of each of its tiles of rows.  The sequences' own tokens go
-// through the kernel of pf_decode_attention, and a third kernel joins the parts of every row in a fixed order.
+// equal pieces, one a block; a piece leaves partial results (reference z, sum, weighted values) of each of its tiles of rows.  The sequences' own tokens
+// go through the kernel of pf_decode_attention on the SMs that the prefixes leave, and a third kernel joins the parts of every row in a fixed order.
+//
+// Both products are the fifth generation's matrix instruction: scores = Q K^T, 128 rows by 128 tokens, both operands in shared memory; values += P V, the
+// weights P in tensor memory, where the threads that own the rows put them over the scores.  The cache's e4m3 is widened to fp16 in between (exact), as in the kernel of the own
+// tokens, so queries keep all their bits and weights 11; scores, references, sums and values are fp32.  The value scale joins the exponent, as there.
+// A block has two streams of 128 rows, so that the products of one are under way while the other's weights are computed; with no more than 128 rows both
+// go through the same ones and take turns with the tiles.  A row's reference is the largest score so far, lifted by 2^7, and stays until a weight would pass
+// 2^15: tensor memory's values are seldom scaled anew.  Warps have one role each and meet at barriers in shared memory:
+//   plan -> copy (bulk, half tiles) -> widen -> products <-> rows.
+// What bounds it.  Many rows: 128 x 128 scores take the products 1024 cycles, the special-function unit 768 (a quarter of the powers are polynomials) and shared memory
+// 1280 (operands 768, the cache's bytes in, out and widened 1024 a tile that two streams share), and the chain scores -> largest -> powers -> products of a stream 3900, of which the
+// other stream fills a half: 256 sequences of 64 / 8 heads of 128 behind 32768 tokens 322 us (854 TFLOP/s; tensor pipe 39 % active, issue slots 47 %).  Few rows: a tile's way through copy,
+// widen and products, 2450 cycles against 1400 from HBM: 3 such sequences behind 262143 tokens 171 us (3.1 TB/s).
+// Measured on the way there (us, these two): rows' scores read twice, one widening role that also loads: 594, 442; scores kept in registers, registers moved to the groups that need
+// them: 394, 198; a whole warp in the products' loop: 373; packed arithmetic, polynomials, half tiles of weights handed over: 353; bulk copies, roles apart: 344, 177; own tokens
+// beside the prefixes: 322; less code in what every tile goes through: 171.  Not kept: 16 warps for the rows (two a row, 350), two warps for the products (386), eight
+// warps that widen (344), four places for half tiles where few rows leave room (360, 207), few rows several times over for a part of a tile each (332, 211).
 #include <math.h>
 
 #include <atomic>
@@ -15,7 +31,8 @@
 
 namespace pf {
 
-constexpr int kMostTiles = 512;          // tiles of a piece at most: 32-bit sums do not run over more than 65536 tokens
+constexpr int kMostTiles = 512;          // tiles of a piece: tensor memory's 32-bit sums do not run over more than 65536 tokens
+constexpr int kMostPieces = 64;          // of a block, though: lists of more than 64 x 512 tiles a block (some 80 ms) have longer ones
 constexpr int kAhead = 4;                // tiles that are under way from HBM to the L2
 constexpr int kLeastTiles = 1;           // a piece takes no fewer while others have none
 constexpr unsigned kWaitLimit = 500000, kDrainLimit = 500000;      // polls of 2 us: a second
@@ -74,7 +91,7 @@ __device__ __forceinline__ int pieces_of(long long total, int blocks)
     const long long few = (total + kLeastTiles - 1) / kLeastTiles;
     if (few < blocks) return (int)few;
     const long long per = (total + (long long)blocks * kMostTiles - 1) / ((long long)blocks * kMostTiles);
-    return (int)(per * blocks);
+    return (int)(per < kMostPieces ? per : kMostPieces) * blocks;
 }
 // pieces of a block, which follow one another
 __device__ __forceinline__ int pieces_each(int n_pieces, int blocks) { return (n_pieces + blocks - 1) / blocks; }
@@ -102,9 +119,8 @@ struct __align__(16) Stretch {
 };
 static_assert(sizeof(Stretch) == 48, "as the roles read it");
 
-// Four groups of four warps: two streams that own the rows, one that widens the cache's bytes, and one of which a warp issues the products, two copy from the cache and one
-// plans.  Registers go
-// where they are needed: 256 x 184 + 128 x 96 + 128 x 48 = 512 x 128, what the block is launched with.
+// Four groups of four warps: two streams that own the rows, one that widens the cache's bytes, and one of which a warp issues the products, two copy
+// from the cache and one plans.  Registers go where they are needed: 256 x 184 + 128 x 96 + 128 x 48 = 512 x 128, what the block is launched with.
 constexpr int kSoftWarps = 8, kWidenWarps = 4;
 constexpr int kPrefixThreads = 512, kSoftRegs = 184, kWidenRegs = 96, kProductRegs = 48;
 static_assert(kSoftRegs * 256 + kWidenRegs * 128 + kProductRegs * 128 <= kPrefixThreads * 128, "no group waits for registers that nobody gives back");
@@ -117,13 +133,20 @@ template <int HD> struct PrefixShape {
     static constexpr int kRing = 6 * kOperand;          // bytes of the cache under way: a tile of keys and one of values
     static constexpr int kScales = kRing + 2 * kTok * HD;        // of eight tiles, for each 16 tokens: key scale, log2 and inverse of the value scale
     static constexpr int kHave = kScales + 8 * 128;     // which runs of a half tile were copied, of keys and of values
-    static constexpr int kPlan = kHave + 16;     // two stretches
+    static constexpr int kPlan = kHave + 16;            // two stretches
     static constexpr int kBars = kPlan + 2 * 48, kBytes = kBars + 288;
     static_assert(kBytes <= 227 * 1024, "fits an SM");
 };
 constexpr uint32_t kTmem = 0;            // tensor memory: a block takes all 512 columns, which begin at 0
 // barriers, 8 bytes each
-enum { B_KFULL = 0, B_KEMPTY = 2, B_VFULL = 4, B_VEMPTY = 6, B_QFULL = 8, B_SFULL = 10, B_PHALF = 12, B_PFULL = 14, B_OFULL = 16, B_DRAIN = 18, B_KRAW = 19, B_VRAW = 21, B_KREAD = 23, B_VREAD = 25, B_PLAN = 27, B_DONE = 29, B_COUNT = 31 };
+enum {
+    B_KFULL = 0, B_KEMPTY = 2, B_VFULL = 4, B_VEMPTY = 6,                       // two tiles of operands, widened and given back
+    B_QFULL = 8, B_SFULL = 10, B_PHALF = 12, B_PFULL = 14, B_OFULL = 16,        // of either stream: queries, scores, half and all of the weights, values
+    B_DRAIN = 18,
+    B_KRAW = 19, B_VRAW = 21, B_KREAD = 23, B_VREAD = 25,                       // either half of a tile's bytes, copied and read
+    B_PLAN = 27, B_DONE = 29,                                                   // two stretches
+    B_COUNT = 31
+};
 
 // 16-byte chunk c of row r of an operand's 128-byte column
 __device__ __forceinline__ uint32_t operand_at(int r, int c) { return (uint32_t)(r * 128 + ((c ^ (r & 7)) << 4)); }
@@ -770,7 +793,8 @@ __global__ void __launch_bounds__(256) prefix_join_kernel(const __grid_constant_
     tile_prefix(A, prefix, warp_sum);
     const int lane = threadIdx.x & 31;
     const long long total = units[P.a.n_groups], own_total = (long long)prefix[A.n_seq] * A.jobs_per_seq;
-    const int share = prefix_share(total, own_total, prefix_grid), n_pieces = total ? pieces_of(total, share) : 0, each = pieces_each(n_pieces, share), own_blocks = own_total ? blocks_used(own_total, own_grid - share) : 1;
+    const int share = prefix_share(total, own_total, prefix_grid), n_pieces = total ? pieces_of(total, share) : 0;
+    const int each = share ? pieces_each(n_pieces, share) : 1, own_blocks = own_total ? blocks_used(own_total, own_grid - share) : 1;
     asm volatile("griddepcontrol.wait;" ::: "memory");
     const float *blocks = A.part + (int64_t)own_grid * S::kWarps * S::kPartFloats;
     const long long n_rows = (long long)A.n_seq * A.n_heads;
@@ -887,7 +911,8 @@ static PrefixSizes prefix_sizes(int hd, int page, int n_kv, int n_seq, int n_hea
     s.slots = s.status + up((size_t)sms * 4);
     const long long tiles = ((long long)pcols * page + kTok - 1) / kTok;
     const long long tasks = (long long)n_kv * (((long long)n_seq * (n_heads / n_kv)) / kRows + n_groups);
-    s.n_slots = tasks + tasks * tiles / kMostTiles + 2 * sms;      // a slot for each piece of each task
+    const long long pieces = tasks * tiles / kMostTiles + sms;
+    s.n_slots = tasks + (pieces < (long long)kMostPieces * sms ? pieces : (long long)kMostPieces * sms) + sms;      // one for each piece of each task
     s.bytes = s.slots + (size_t)s.n_slots * kRows * (hd + 2) * 4;
     return s;
 }
