@@ -142,8 +142,11 @@ int pf_kv_append_rope(const pf_kv_cache_t *cache, const pf_rotary_t *rotary, int
  * missing pages, scales, q, out and lse otherwise as in pf_decode_attention.  A row that sees no token gives zeros and -infinity.
  * A prefix token's weight enters the values' sum with 11 bits (fewer below 2^-21 of the row's largest, none below 2^-32).
  * A wait inside the kernel that runs out makes the rows that it concerns NaN.
- * PF_EINVAL, PF_ERANGE (also: n_groups above PF_PREFIX_MAX_GROUPS), PF_EWORKSPACE as there.  n_groups = 0: no sequence has a prefix. */
+ * Values are added up in 32 bits over 65536 tokens at a time, more in calls of more than 4.8 million (tile of rows, 128 tokens) pairs.
+ * PF_EINVAL, PF_ERANGE (also: n_groups above PF_PREFIX_MAX_GROUPS, a prefix table row with room for more than PF_PREFIX_MAX_TOKENS, n_seq * n_heads
+ * of 2^30 and more), PF_EWORKSPACE as there.  n_groups = 0: no sequence has a prefix. */
 #define PF_PREFIX_MAX_GROUPS 1024
+#define PF_PREFIX_MAX_TOKENS 2147479552 /* 2^31 - 4096 */
 size_t pf_prefix_attention_workspace(const pf_kv_cache_t *cache, int32_t n_seq, int32_t n_heads, int32_t n_groups, int32_t prefix_cols);
 int pf_prefix_attention(const pf_kv_cache_t *cache, int32_t dtype, int32_t n_seq, int32_t n_heads, const void *d_q, int64_t q_stride,
                         const int32_t *d_len, const int32_t *d_table, int32_t table_cols, int32_t n_groups, const int32_t *d_cu_seqs,

@@ -965,7 +965,8 @@ extern "C" int pf_prefix_attention(const pf_kv_cache_t *cache, int32_t dtype, in
 {
     if (!kv_cache_ok(cache) || (dtype != PF_DT_BF16 && dtype != PF_DT_F16)) return PF_EINVAL;
     if (n_seq < 0 || n_seq > PF_ATTN_MAX_SEQ || n_heads < 0 || table_cols < 0 || (int64_t)table_cols * cache->page >= (1ll << 31)) return PF_ERANGE;
-    if (n_groups < 0 || n_groups > PF_PREFIX_MAX_GROUPS || prefix_cols < 0 || (int64_t)prefix_cols * cache->page >= (1ll << 31)) return PF_ERANGE;
+    if (n_groups < 0 || n_groups > PF_PREFIX_MAX_GROUPS || prefix_cols < 0) return PF_ERANGE;
+    if ((int64_t)prefix_cols * cache->page > PF_PREFIX_MAX_TOKENS) return PF_ERANGE;      // tile numbers times 128, a few tiles past the end, fit 32 bits
     const int64_t tiles = ((int64_t)table_cols * cache->page + kTile - 1) / kTile;      // as in pf_decode_attention
     if ((int64_t)n_seq * tiles >= (1ll << 31)) return PF_ERANGE;
     if ((int64_t)n_seq * n_heads >= (1ll << 30)) return PF_ERANGE;

@@ -78,7 +78,7 @@ def test_prefix_refusals(lib):
                 dict(out=PTR + 8), dict(qs=1000), dict(qs=1028), dict(os_=512), dict(lse=PTR + 1), dict(groups=2, cu=None), dict(pl=None), dict(pt=None), dict(cu=PTR + 2),
                 dict(pl=PTR + 1), dict(pt=PTR + 3)):
         assert prefix(lib, **bad) == B.PF_EINVAL, bad
-    for bad in (dict(n_seq=-1), dict(n_seq=8193), dict(heads=-8), dict(cols=-1), dict(cols=1 << 26), dict(groups=-1), dict(groups=1025), dict(pcols=-1), dict(pcols=1 << 26),
+    for bad in (dict(n_seq=-1), dict(n_seq=8193), dict(heads=-8), dict(cols=-1), dict(cols=1 << 26), dict(groups=-1), dict(groups=1025), dict(pcols=-1), dict(pcols=1 << 26), dict(pcols=(1 << 25) - 63),
                 dict(n_seq=8192, cols=1 << 17), dict(n_seq=8192, heads=1 << 20, qs=1 << 27, os_=1 << 27)):
         assert prefix(lib, **bad) == B.PF_ERANGE, bad
 
