@@ -197,7 +197,8 @@ def pf_add_rms_norm(x, residual=None, weight=None, *, eps: float = 1e-6, group: 
 
 def _cache(torch, what, k_cache, v_cache, k_scale, v_scale):
     shape = k_cache.shape
-    if len(shape) != 4 or shape != v_cache.shape or k_scale.shape != shape[:2] or v_scale.shape != shape[:2]:
+    scales = shape[:2]
+    if len(shape) != 4 or shape != v_cache.shape or k_scale.shape != scales or v_scale.shape != scales:
         _refuse(f"{what}: caches are [pages, kv heads, page, head_dim], scales [pages, kv heads]")
     f8, f32 = torch.float8_e4m3fn, torch.float32
     if k_cache.dtype != f8 or v_cache.dtype != f8 or k_scale.dtype != f32 or v_scale.dtype != f32:
@@ -209,9 +210,10 @@ def _cache(torch, what, k_cache, v_cache, k_scale, v_scale):
 
 def _heads(t, what, heads, hd):
     """[rows, heads, hd], contiguous within a row; returns the row stride in elements."""
-    if t.dim() != 3 or t.shape[1] != heads or t.shape[2] != hd or t.stride(2) != 1 or (heads > 1 and t.stride(1) != hd):
-        _refuse(f"{what}: expected [rows, {heads}, {hd}] with contiguous rows, got shape {tuple(t.shape)}, strides {t.stride()}")
-    return t.stride(0) if t.shape[0] > 1 else heads * hd
+    shape, strides = t.shape, t.stride()
+    if len(shape) != 3 or shape[1] != heads or shape[2] != hd or strides[2] != 1 or (heads > 1 and strides[1] != hd):
+        _refuse(f"{what}: expected [rows, {heads}, {hd}] with contiguous rows, got shape {tuple(shape)}, strides {strides}")
+    return strides[0] if shape[0] > 1 else heads * hd
 
 
 def _int32(torch, what, t, dims):
@@ -397,9 +399,10 @@ def rotary_frequencies(rot: int, *, base: float = 10000.0, scaling: str = "none"
 
 def _strided_heads(t, what):
     """[tokens, heads, hd] with contiguous heads; returns the strides of a token and of a head."""
-    if t.dim() != 3 or (t.stride(2) != 1 and t.shape[2] > 1):
-        _refuse(f"{what}: expected [tokens, heads, head_dim] with contiguous heads, got shape {tuple(t.shape)}, strides {t.stride()}")
-    return t.stride(0), t.stride(1)
+    strides = t.stride()
+    if len(strides) != 3 or (strides[2] != 1 and t.shape[2] > 1):
+        _refuse(f"{what}: expected [tokens, heads, head_dim] with contiguous heads, got shape {tuple(t.shape)}, strides {strides}")
+    return strides[0], strides[1]
 
 
 def pf_rope(x, positions, rotary: Rotary, *, transposed: bool = False, out=None, stream=None):
