@@ -323,7 +323,7 @@ __device__ __forceinline__ void widen_role(const PrefixRoom &R, const Stretch *p
 {
     using S = PrefixShape<HD>;
     constexpr int ROWS = 64 / (HD / 16);                // rows of a pass of both warps
-    constexpr int N = 64 / ROWS, B = 4;                 // passes of half a tile, and of them at a time
+    constexpr int N = 64 / ROWS, B = N < 8 ? N : 8;                 // passes of half a tile, and of them at a time
     const int lane = threadIdx.x & 31, w = threadIdx.x / 32 - kSoftWarps, values = w >> 1;
     // HD 128: lanes 0 - 3 row 0 pieces 0 - 3, 4 - 7 row 1 pieces 4 - 7, 8 - 11 row 0 pieces 4 - 7, 12 - 15 row 1 pieces 0 - 3, 16 - 31 rows 2 and 3 likewise
     const int c = HD == 128 ? (lane & 3) + 4 * (((lane >> 2) ^ (lane >> 3)) & 1) : lane & 3;
@@ -345,16 +345,11 @@ __device__ __forceinline__ void widen_role(const PrefixRoom &R, const Stretch *p
                 uint32_t have;                          // runs of the tile that were copied
                 asm volatile("ld.shared.u32 %0, [%1];" : "=r"(have) : "r"(have_at + 4 * h) : "memory");
                 const bool whole = have == (1u << (7 - run_log2)) - 1 && left >= kTok;
-                uint4 x[B], y[B];                       // the next ones are loaded while these are widened
-#pragma unroll
-                for (int i = 0; i < B; i++) y[i] = lds128(own + (h * 64 + i * ROWS) * HD);
 #pragma unroll
                 for (int q = 0; q < N; q += B) {
+                    uint4 x[B];
 #pragma unroll
-                    for (int i = 0; i < B; i++) {
-                        x[i] = y[i];
-                        if (q + B < N) y[i] = lds128(own + (h * 64 + (q + B + i) * ROWS) * HD);
-                    }
+                    for (int i = 0; i < B; i++) x[i] = lds128(own + (h * 64 + (q + i) * ROWS) * HD);
                     if (!whole) {
 #pragma unroll
                         for (int i = 0; i < B; i++) {
