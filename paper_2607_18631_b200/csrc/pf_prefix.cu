@@ -323,7 +323,7 @@ __device__ __forceinline__ void widen_role(const PrefixRoom &R, const Stretch *p
 {
     using S = PrefixShape<HD>;
     constexpr int ROWS = 64 / (HD / 16);                // rows of a pass of both warps
-    constexpr int N = 64 / ROWS, B = N < 8 ? N : 8;                 // passes of half a tile, and of them at a time
+    constexpr int N = 64 / ROWS, B = N < 8 ? N : 8;     // passes of half a tile, and of them at a time
     const int lane = threadIdx.x & 31, w = threadIdx.x / 32 - kSoftWarps, values = w >> 1;
     // HD 128: lanes 0 - 3 row 0 pieces 0 - 3, 4 - 7 row 1 pieces 4 - 7, 8 - 11 row 0 pieces 4 - 7, 12 - 15 row 1 pieces 0 - 3, 16 - 31 rows 2 and 3 likewise
     const int c = HD == 128 ? (lane & 3) + 4 * (((lane >> 2) ^ (lane >> 3)) & 1) : lane & 3;
@@ -790,7 +790,7 @@ __global__ void __launch_bounds__(256) prefix_join_kernel(const __grid_constant_
     const long long total = units[P.a.n_groups], own_total = (long long)prefix[A.n_seq] * A.jobs_per_seq;
     const int share = prefix_share(total, own_total, prefix_grid), n_pieces = total ? pieces_of(total, share) : 0;
     const int each = share ? pieces_each(n_pieces, share) : 1, own_blocks = own_total ? blocks_used(own_total, own_grid - share) : 1;
-    asm volatile("griddepcontrol.wait;" ::: "memory");
+    bool waited = false;                          // where a warp's first row has its parts follows from the lengths alone
     const float *blocks = A.part + (int64_t)own_grid * S::kWarps * S::kPartFloats;
     const long long n_rows = (long long)A.n_seq * A.n_heads;
     for (long long row = (long long)blockIdx.x * 8 + (threadIdx.x >> 5); row < n_rows; row += (long long)gridDim.x * 8) {
@@ -825,6 +825,8 @@ __global__ void __launch_bounds__(256) prefix_join_kernel(const __grid_constant_
                 n_pre *= both;
             }
         }
+        if (!waited) asm volatile("griddepcontrol.wait;" ::: "memory");
+        waited = true;
         const int n = n_own + n_pre;
         float top = -INFINITY, sum = 0.f, v[V];
 #pragma unroll
@@ -887,6 +889,7 @@ __global__ void __launch_bounds__(256) prefix_join_kernel(const __grid_constant_
         for (int k = 0; k < V; k += 2) dst[k / 2] = pair_of_f32<T>(v[k] * inv, v[k + 1] * inv);
         if (A.lse && lane == 0) A.lse[row] = sum == 0.f ? -INFINITY : (top + log2f(sum)) * kLn2;
     }
+    if (!waited) asm volatile("griddepcontrol.wait;" ::: "memory");      // what follows on the stream waits for this kernel only
 }
 
 // ------------------------------------------------------------------ host
