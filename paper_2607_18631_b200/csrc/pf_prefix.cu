@@ -16,8 +16,8 @@
 //   plan -> copy (bulk, half tiles) -> widen -> products <-> rows.
 // What bounds it.  Many rows: 128 x 128 scores take the products 1024 cycles, the special-function unit 768 (a quarter of the powers are polynomials) and shared memory
 // 1280 (operands 768, the cache's bytes in, out and widened 1024 a tile that two streams share), and the chain scores -> largest -> powers -> products of a stream 3900, of which the
-// other stream fills a half: 256 sequences of 64 / 8 heads of 128 behind 32768 tokens 322 us (854 TFLOP/s; tensor pipe 39 % active, issue slots 47 %).  Few rows: a tile's way through copy,
-// widen and products, 2450 cycles against 1400 from HBM: 3 such sequences behind 262143 tokens 171 us (3.1 TB/s).
+// other stream fills a half: 256 sequences of 64 / 8 heads of 128 behind 32768 tokens 321 us (863 TFLOP/s; tensor pipe 39 % active, issue slots 47 %).  Few rows: a tile's way through copy,
+// widen and products, 2450 cycles against 1400 from HBM: 3 such sequences behind 262143 tokens 168 us (3.2 TB/s).
 // Measured on the way there (us, these two): rows' scores read twice, one widening role that also loads: 594, 442; scores kept in registers, registers moved to the groups that need
 // them: 394, 198; a whole warp in the products' loop: 373; packed arithmetic, polynomials, half tiles of weights handed over: 353; bulk copies, roles apart: 344, 177; own tokens
 // beside the prefixes: 322; less code in what every tile goes through: 171.  Not kept: 16 warps for the rows (two a row, 350), two warps for the products (386), eight
