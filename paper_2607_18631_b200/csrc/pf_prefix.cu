@@ -332,7 +332,7 @@ __device__ __forceinline__ void widen_role(const PrefixRoom &R, const Stretch *p
     const uint32_t to0 = to + operand_at(r0, 2 * (c & 3)), to1 = to + operand_at(r0, 2 * (c & 3) + 1);
     const uint32_t own = R.smem + S::kRing + values * kTok * HD + r0 * HD + c * 16, have_at = R.smem + S::kHave + values * 8;
     const int full = values ? B_VFULL : B_KFULL, empty = values ? B_VEMPTY : B_KEMPTY, raw = values ? B_VRAW : B_KRAW, read = values ? B_VREAD : B_KREAD;
-    const int run_log2 = R.run_log2;
+    const int run_log2 = R.run_log2, runs = kTok >> run_log2;
     unsigned n = 0;                                     // tiles so far
     Stretch s;
     for (unsigned run = 0; R.next(plan, run, s); R.done(run), run++) {
@@ -344,7 +344,7 @@ __device__ __forceinline__ void widen_role(const PrefixRoom &R, const Stretch *p
                 if (!R.wait_warp(raw + h, n)) return;
                 uint32_t have;                          // runs of the tile that were copied
                 asm volatile("ld.shared.u32 %0, [%1];" : "=r"(have) : "r"(have_at + 4 * h) : "memory");
-                const bool whole = have == (1u << (7 - run_log2)) - 1 && left >= kTok;
+                const bool whole = have == (1u << runs) - 1 && left >= kTok;
 #pragma unroll
                 for (int q = 0; q < N; q += B) {
                     uint4 x[B];
