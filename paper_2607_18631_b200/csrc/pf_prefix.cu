@@ -266,7 +266,7 @@ __device__ __forceinline__ void copy_role(const PrefixArgs &P, const PrefixRoom 
         auto ahead = [&](int page) {
             if (there(page)) asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(place_of(page)), "r"(HD << run_log2) : "memory");
         };
-        // The keys' warp also leaves the tile's scales.  Missing pages and 16 tokens behind the end: log2 -infinity.
+        // The keys' warp also leaves the tile's scales.  Missing pages and 16 tokens behind the end: log2 -infinity, inverse 0.
         float ks = 1.f, vs = -1.f;
         auto scales_of = [&](int pages) {
             const int page = __shfl_sync(0xFFFFFFFFu, pages, (lane & 7) >> (run_log2 - 4));
@@ -285,7 +285,7 @@ __device__ __forceinline__ void copy_role(const PrefixArgs &P, const PrefixRoom 
                 if (lane < 8) {
                     const float v = fmaxf(vs, 8.673617379884035e-19f);      // 2^-60
                     asm volatile("st.shared.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(R.smem + S::kScales + (n & 7) * 128 + lane * 16), "f"(ks),
-                                 "f"(vs < 0.f ? -INFINITY : __log2f(v)), "f"(__fdividef(1.f, v)), "f"(0.f) : "memory");
+                                 "f"(vs < 0.f ? -INFINITY : __log2f(v)), "f"(vs < 0.f ? 0.f : __fdividef(1.f, v)), "f"(0.f) : "memory");
                 }
                 __syncwarp();
                 scales_of(next);
@@ -455,14 +455,16 @@ struct Two { uint64_t v; };
 __device__ __forceinline__ Two two(float lo, float hi) { Two r; asm("mov.b64 %0, {%1, %2};" : "=l"(r.v) : "f"(lo), "f"(hi)); return r; }
 __device__ __forceinline__ void apart(Two a, float &lo, float &hi) { asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(a.v)); }
 __device__ __forceinline__ Two fma2(Two a, Two b, Two c) { Two r; asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.v) : "l"(a.v), "l"(b.v), "l"(c.v)); return r; }
-__device__ __forceinline__ Two add2(Two a, Two b) { Two r; asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v)); return r; }
+// (what lies below the normals counts as 0)
+__device__ __forceinline__ Two add2(Two a, Two b) { Two r; asm("add.rn.ftz.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v)); return r; }
 // 2^a without the special-function unit, which computes 16 a cycle and SM where a tile asks for 16384: a = n + f, n whole, |f| <= 1/2, and the
-// polynomial of degree 4 that is nearest to 2^f there (relative error 2.6e-6, found by exchange).  Below 2^-126 (-infinity): 2^-126.  No NaN comes out.
+// polynomial of degree 4 that is nearest to 2^f there (relative error 2.6e-6, found by exchange).  Below 2^-126 (-infinity) a
+// number below the normals comes out, which add2 and the conversion to fp16 take as 0: value scales reach 2^118, so 2^-126 times an inverse scale could outweigh the sum.  No NaN comes out.
 __device__ __forceinline__ void pow2_two(Two a, float &lo, float &hi)
 {
     float x, y;
     apart(a, x, y);
-    a = two(fmaxf(x, -126.f), fmaxf(y, -126.f));
+    a = two(fmaxf(x, -126.75f), fmaxf(y, -126.75f));      // n = -127, f = 1/4
     const float big = 12582912.f;                       // 1.5 * 2^23: what is added to it is rounded to a whole number
     const Two m = add2(a, two(big, big)), n = add2(m, two(-big, -big)), f = fma2(n, two(-1.f, -1.f), a);
     Two r = fma2(f, two(0.009570102207362652f, 0.009570102207362652f), two(0.05591785907745361f, 0.05591785907745361f));
