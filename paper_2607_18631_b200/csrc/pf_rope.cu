@@ -407,7 +407,8 @@ extern "C" int pf_rotary_phases(int32_t n, const double *freq, uint64_t *phase)
     for (int32_t i = 0; i < n; i++) {
         if (!isfinite(freq[i])) return PF_EINVAL;
         const long double turns = (long double)freq[i] / 6.283185307179586476925286766559L;
-        phase[i] = (uint64_t)roundl((turns - floorl(turns)) * 18446744073709551616.0L);      // the fraction has 64 bits: below 2^64
+        const long double whole = 18446744073709551616.0L, part = roundl((turns - floorl(turns)) * whole);
+        phase[i] = part < whole ? (uint64_t)part : 0;      // (a fraction that is rounded up to a turn: a tiny negative frequency)
     }
     return PF_OK;
 }
