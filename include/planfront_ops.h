@@ -141,7 +141,8 @@ int pf_kv_append_rope(const pf_kv_cache_t *cache, const pf_rotary_t *rotary, int
  * d_cu_seqs: n_groups + 1 offsets that do not decrease (NULL, with one group: all sequences); a sequence in no group sees its own tokens only.  Prefixes of any length, and tables, lengths,
  * missing pages, scales, q, out and lse otherwise as in pf_decode_attention.  A row that sees no token gives zeros and -infinity.
  * A prefix token's weight enters the values' sum with 11 bits (fewer below 2^-21 of the row's largest, none below 2^-32).
- * A wait inside the kernel that runs out makes the rows that it concerns NaN.
+ * A wait inside the kernel that runs out makes the rows that it concerns NaN; pf_prefix_attention_status says so too: one int32 of device memory, 0 after a
+ * complete call, 1 otherwise (d_status may be NULL: pf_prefix_attention).
  * Values are added up in 32 bits over 65536 tokens at a time, more in calls of more than 4.8 million (tile of rows, 128 tokens) pairs.
  * PF_EINVAL, PF_ERANGE (also: n_groups above PF_PREFIX_MAX_GROUPS, a prefix table row with room for more than PF_PREFIX_MAX_TOKENS, n_seq * n_heads
  * of 2^30 and more), PF_EWORKSPACE as there.  n_groups = 0: no sequence has a prefix. */
@@ -152,6 +153,10 @@ int pf_prefix_attention(const pf_kv_cache_t *cache, int32_t dtype, int32_t n_seq
                         const int32_t *d_len, const int32_t *d_table, int32_t table_cols, int32_t n_groups, const int32_t *d_cu_seqs,
                         const int32_t *d_prefix_len, const int32_t *d_prefix_table, int32_t prefix_cols, float sm_scale, void *d_out,
                         int64_t out_stride, float *d_lse, void *d_workspace, size_t workspace_bytes, void *stream);
+int pf_prefix_attention_status(const pf_kv_cache_t *cache, int32_t dtype, int32_t n_seq, int32_t n_heads, const void *d_q, int64_t q_stride,
+                               const int32_t *d_len, const int32_t *d_table, int32_t table_cols, int32_t n_groups, const int32_t *d_cu_seqs,
+                               const int32_t *d_prefix_len, const int32_t *d_prefix_table, int32_t prefix_cols, float sm_scale, void *d_out,
+                               int64_t out_stride, float *d_lse, int32_t *d_status, void *d_workspace, size_t workspace_bytes, void *stream);
 
 /* One mixture-of-experts layer as this GPU holds it: experts [first, first + n_local) of n_experts, and n_shared
  * experts that every token takes with weight 1 (indices n_local .. n_local + n_shared - 1 of the weight tensors).

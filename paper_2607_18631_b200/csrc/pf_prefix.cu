@@ -46,6 +46,7 @@ struct PrefixArgs {
     long long n_slots;
     uint32_t *status;                    // [blocks], written by those with work
     float *slots;                        // [n_slots] x (kRows x HD values, kRows references, kRows sums)
+    int32_t *report;                     // the call's status, or NULL
 };
 
 // Tiles and tasks of the groups in front of each group, by the whole block.  units, tasks: n_groups + 1 words; scratch: 100
@@ -774,8 +775,9 @@ __global__ void __launch_bounds__(kPrefixThreads, 1) prefix_kernel(const __grid_
 // ------------------------------------------------------------------ the join
 // A warp joins the parts of one row: what its own tokens left (one part where a single block finished them, else one of each block), and
 // one of each piece that goes through the prefix.
+// (Four blocks an SM, so 64 registers: with 48, which the compiler takes for more of them, 2 us more for 4 behind 777 and 6 for 3 behind 262143.)
 template <typename T, int HD, int NB>
-__global__ void __launch_bounds__(256) prefix_join_kernel(const __grid_constant__ PrefixArgs P, const int own_grid, const int prefix_grid)
+__global__ void __launch_bounds__(256, 4) prefix_join_kernel(const __grid_constant__ PrefixArgs P, const int own_grid, const int prefix_grid)
 {
     using S = AttnShape<HD, NB>;
     constexpr int V = HD / 32;
@@ -892,6 +894,12 @@ __global__ void __launch_bounds__(256) prefix_join_kernel(const __grid_constant_
         if (A.lse && lane == 0) A.lse[row] = sum == 0.f ? -INFINITY : (top + log2f(sum)) * kLn2;
     }
     if (!waited) asm volatile("griddepcontrol.wait;" ::: "memory");      // what follows on the stream waits for this kernel only
+    if (P.report && blockIdx.x == 0 && threadIdx.x < 32) {
+        unsigned lost = 0;
+        for (int i = lane; i < (n_pieces + each - 1) / each; i += 32) lost |= P.status[i];      // of the blocks with work
+        lost = __any_sync(0xFFFFFFFFu, lost != 0);
+        if (lane == 0) *P.report = (int)lost;
+    }
 }
 
 // ------------------------------------------------------------------ host
@@ -958,11 +966,16 @@ extern "C" size_t pf_prefix_attention_workspace(const pf_kv_cache_t *cache, int3
     return prefix_sizes(cache->hd, cache->page, cache->n_kv, n_seq, n_heads, n_groups, prefix_cols, sms).bytes;
 }
 
-extern "C" int pf_prefix_attention(const pf_kv_cache_t *cache, int32_t dtype, int32_t n_seq, int32_t n_heads, const void *d_q, int64_t q_stride,
-                                   const int32_t *d_len, const int32_t *d_table, int32_t table_cols, int32_t n_groups, const int32_t *d_cu_seqs,
-                                   const int32_t *d_prefix_len, const int32_t *d_prefix_table, int32_t prefix_cols, float sm_scale, void *d_out,
-                                   int64_t out_stride, float *d_lse, void *d_workspace, size_t workspace_bytes, void *stream)
+extern "C" int pf_prefix_attention_status(const pf_kv_cache_t *cache, int32_t dtype, int32_t n_seq, int32_t n_heads, const void *d_q, int64_t q_stride,
+                                          const int32_t *d_len, const int32_t *d_table, int32_t table_cols, int32_t n_groups, const int32_t *d_cu_seqs,
+                                          const int32_t *d_prefix_len, const int32_t *d_prefix_table, int32_t prefix_cols, float sm_scale, void *d_out,
+                                          int64_t out_stride, float *d_lse, int32_t *d_status, void *d_workspace, size_t workspace_bytes, void *stream)
 {
+    cudaStream_t st = (cudaStream_t)stream;
+    auto complete = [&]() -> int {                      // calls without a wait inside
+        if (d_status) PF_CUDA_TRY(cudaMemsetAsync(d_status, 0, 4, st), "pf_prefix_attention status");
+        return PF_OK;
+    };
     if (!kv_cache_ok(cache) || (dtype != PF_DT_BF16 && dtype != PF_DT_F16)) return PF_EINVAL;
     if (n_seq < 0 || n_seq > PF_ATTN_MAX_SEQ || n_heads < 0 || table_cols < 0 || (int64_t)table_cols * cache->page >= (1ll << 31)) return PF_ERANGE;
     if (n_groups < 0 || n_groups > PF_PREFIX_MAX_GROUPS || prefix_cols < 0) return PF_ERANGE;
@@ -970,17 +983,19 @@ extern "C" int pf_prefix_attention(const pf_kv_cache_t *cache, int32_t dtype, in
     const int64_t tiles = ((int64_t)table_cols * cache->page + kTile - 1) / kTile;      // as in pf_decode_attention
     if ((int64_t)n_seq * tiles >= (1ll << 31)) return PF_ERANGE;
     if ((int64_t)n_seq * n_heads >= (1ll << 30)) return PF_ERANGE;
-    if (n_heads % cache->n_kv != 0 || !isfinite(sm_scale)) return PF_EINVAL;
-    if (n_seq == 0 || n_heads == 0) return PF_OK;
+    if (n_heads % cache->n_kv != 0 || !isfinite(sm_scale) || (uintptr_t)d_status % 4) return PF_EINVAL;
+    if (n_seq == 0 || n_heads == 0) return complete();
     if (!d_q || !d_out || !d_len || (!d_table && table_cols > 0) || !aligned16(d_q) || !aligned16(d_out)) return PF_EINVAL;
     if (n_groups > 0 && ((!d_cu_seqs && n_groups > 1) || !d_prefix_len || (!d_prefix_table && prefix_cols > 0))) return PF_EINVAL;
     if ((uintptr_t)d_len % 4 || (uintptr_t)d_table % 4 || (uintptr_t)d_lse % 4 || (uintptr_t)d_cu_seqs % 4 || (uintptr_t)d_prefix_len % 4 || (uintptr_t)d_prefix_table % 4)
         return PF_EINVAL;
     const int64_t row = (int64_t)n_heads * cache->hd;
     if (q_stride < row || out_stride < row || q_stride % 8 || out_stride % 8) return PF_EINVAL;
-    if (n_groups == 0 || prefix_cols == 0)
-        return pf_decode_attention(cache, dtype, n_seq, n_heads, d_q, q_stride, d_len, d_table, table_cols, sm_scale, d_out, out_stride, d_lse, d_workspace,
-                                   workspace_bytes, stream);
+    if (n_groups == 0 || prefix_cols == 0) {
+        const int rc = pf_decode_attention(cache, dtype, n_seq, n_heads, d_q, q_stride, d_len, d_table, table_cols, sm_scale, d_out, out_stride, d_lse, d_workspace,
+                                           workspace_bytes, stream);
+        return rc == PF_OK ? complete() : rc;
+    }
     int device, sms;
     if (int rc = current_sm_count(&device, &sms)) return rc;
     const PrefixSizes z = prefix_sizes(cache->hd, cache->page, cache->n_kv, n_seq, n_heads, n_groups, prefix_cols, sms);
@@ -1002,8 +1017,17 @@ extern "C" int pf_prefix_attention(const pf_kv_cache_t *cache, int32_t dtype, in
     p.slots = (float *)(ws + z.slots);
     p.wait_limit = g_wait_limit;
     p.wait_lost = g_wait_lost;
-    cudaStream_t st = (cudaStream_t)stream;
+    p.report = d_status;
     return dtype == PF_DT_BF16 ? prefix_launch<Bf16>(p, device, sms, st) : prefix_launch<F16>(p, device, sms, st);
+}
+
+extern "C" int pf_prefix_attention(const pf_kv_cache_t *cache, int32_t dtype, int32_t n_seq, int32_t n_heads, const void *d_q, int64_t q_stride,
+                                   const int32_t *d_len, const int32_t *d_table, int32_t table_cols, int32_t n_groups, const int32_t *d_cu_seqs,
+                                   const int32_t *d_prefix_len, const int32_t *d_prefix_table, int32_t prefix_cols, float sm_scale, void *d_out,
+                                   int64_t out_stride, float *d_lse, void *d_workspace, size_t workspace_bytes, void *stream)
+{
+    return pf_prefix_attention_status(cache, dtype, n_seq, n_heads, d_q, q_stride, d_len, d_table, table_cols, n_groups, d_cu_seqs, d_prefix_len, d_prefix_table,
+                                      prefix_cols, sm_scale, d_out, out_stride, d_lse, nullptr, d_workspace, workspace_bytes, stream);
 }
 
 extern "C" int pf_prefix_waits(uint32_t polls, uint32_t lost)

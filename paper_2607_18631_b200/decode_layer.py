@@ -92,7 +92,7 @@ class DecodeLayer:
         together = not s["shared"] or (s["shared_ffn"] == s["ffn"] and s["expert_tokens"] == T)
         self.moe = layer_of(s["local"] + (s["shared"] if together else 0), s["ffn"], s["shared"] if together else 0)
         self.shared = None if together else layer_of(s["shared"], s["shared_ffn"], s["shared"])
-        self.status = torch.zeros(2, dtype=torch.int32, device=dev)        # of the two layers' latest calls
+        self.status = torch.zeros(3, dtype=torch.int32, device=dev)        # of the latest calls of the two layers of experts and of the attention
         # the other GPUs' tokens, which an all-gather would bring: they stay the same from step to step
         others = torch.randn(s["expert_tokens"] - T, H, generator=g, device=dev).to(torch.bfloat16)
         self.others = ops.pf_add_rms_norm(others, None, self.norm2, y=True) if others.shape[0] else None
@@ -154,7 +154,8 @@ class DecodeLayer:
 
     def attend(self, q):
         if self.prefix:
-            return self.ops.pf_prefix_attention(q, *self.cache, *self.scales, self.lengths, self.table, self.prefix_length, self.prefix_table)["out"]
+            return self.ops.pf_prefix_attention(q, *self.cache, *self.scales, self.lengths, self.table, self.prefix_length, self.prefix_table,
+                                                status=self.status[2:3])["out"]
         return self.ops.pf_decode_attention(q, *self.cache, *self.scales, self.lengths, self.table)["out"]
 
     def gather(self, n):
@@ -174,9 +175,12 @@ class DecodeLayer:
         return out if self.shared is None else out + self.run(self.shared, n, 1)
 
     def check(self):
-        """Waits for the device; raises if a wait inside a layer's latest call ran out (its output is NaN then)."""
-        if self.status.any().item():
+        """Waits for the device; raises if a wait inside the experts' or the attention's latest call ran out (its output is NaN then)."""
+        *experts, attention = self.status.tolist()
+        if any(experts):
             raise PlanfrontError(PF_ECUDA, "decode_layer: a wait inside the experts' kernel ran out")
+        if attention:
+            raise PlanfrontError(PF_ECUDA, "decode_layer: a wait inside the kernel for shared prefixes ran out")
 
     def measure(self, repeats: int = 20) -> dict:
         """{part: (microseconds, bytes it cannot do without)} of the attention and the experts, device time of a call whose cache and weights

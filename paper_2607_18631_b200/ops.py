@@ -21,7 +21,7 @@ from .binding import PF_EINVAL, PF_ERANGE, PF_OK, PlanfrontError, _check, _torch
 
 EXPORTS = ("pf_add_rms_norm", "pf_kv_append", "pf_decode_attention_workspace", "pf_decode_attention",
            "pf_moe_packed_bytes", "pf_moe_pack", "pf_moe_workspace", "pf_moe_forward", "pf_rotary_phases", "pf_rope", "pf_kv_append_rope",
-           "pf_prefix_attention_workspace", "pf_prefix_attention")
+           "pf_prefix_attention_workspace", "pf_prefix_attention", "pf_prefix_attention_status")
 DT_BF16, DT_F16, DT_F32, DT_E4M3 = 0, 1, 2, 3
 SCALE_GROUP = 128
 MOE_MAX_TOKENS = 512
@@ -70,6 +70,7 @@ def declare(L):
                        ("pf_rope", [rotary, i32, i32, i64, i32, i32, _vp, i64, i64, _vp, _vp, i64, i64, _vp]),
                        ("pf_kv_append_rope", [cache, rotary, i32, i32, i64, i32, i32] + [_vp, i64] * 4 + [_vp, _vp, _vp, i32, _vp, _vp]),
                        ("pf_prefix_attention", [cache, i32, i32, i32, _vp, i64, _vp, _vp, i32, i32, _vp, _vp, _vp, i32, f32, _vp, i64, _vp, _vp, _sz, _vp]),
+                       ("pf_prefix_attention_status", [cache, i32, i32, i32, _vp, i64, _vp, _vp, i32, i32, _vp, _vp, _vp, i32, f32, _vp, i64, _vp, _vp, _vp, _sz, _vp]),
                        ("pf_moe_forward", [moe, i32, _vp, i64] + [_vp] * 8 + [_vp, _sz, _vp])):
         fn = getattr(L, name)
         fn.restype, fn.argtypes = C.c_int, args
@@ -301,20 +302,21 @@ def pf_decode_attention(q, k_cache, v_cache, k_scale, v_scale, lengths, table, *
 
 
 def pf_prefix_attention(q, k_cache, v_cache, k_scale, v_scale, lengths, table, prefix_lengths, prefix_table, cu_seqs=None, *, sm_scale: float | None = None,
-                        lse: bool = False, out=None, workspace=None, stream=None) -> dict:
+                        lse: bool = False, out=None, status=None, workspace=None, stream=None) -> dict:
     """pf_decode_attention of sequences that share prefixes: sequences cu_seqs[g] .. cu_seqs[g + 1] - 1 (all, without cu_seqs) see the
     prefix_lengths[g] tokens on the pages prefix_table[g] in front of their own lengths[b] tokens, and a prefix is read once for its group.
 
     prefix_lengths: [groups], prefix_table: [groups, columns], cu_seqs: [groups + 1], int32, not decreasing; a sequence in no group sees its own tokens
-    only.  Everything else, and what comes back, as in pf_decode_attention."""
+    only.  status: int32 tensor of one element, 0 after a complete call, 1 if a wait inside the kernel ran out; the rows that it concerns are then NaN, with or
+    without it.  Everything else, and what comes back, as in pf_decode_attention."""
     L, torch = _ready or _lib()
     if stream is not None:
-        _used_on(torch, stream, q, k_cache, v_cache, k_scale, v_scale, lengths, table, prefix_lengths, prefix_table, cu_seqs, out, workspace)
+        _used_on(torch, stream, q, k_cache, v_cache, k_scale, v_scale, lengths, table, prefix_lengths, prefix_table, cu_seqs, out, status, workspace)
         with torch.cuda.stream(stream):
             return pf_prefix_attention(q, k_cache, v_cache, k_scale, v_scale, lengths, table, prefix_lengths, prefix_table, cu_seqs, sm_scale=sm_scale, lse=lse,
-                                       out=out, workspace=workspace)
+                                       out=out, status=status, workspace=workspace)
     what = "pf_prefix_attention"
-    dev = _on_device(torch, what, q, k_cache, v_cache, k_scale, v_scale, lengths, table, prefix_lengths, prefix_table, cu_seqs, out, workspace)
+    dev = _on_device(torch, what, q, k_cache, v_cache, k_scale, v_scale, lengths, table, prefix_lengths, prefix_table, cu_seqs, out, status, workspace)
     c = _cache(torch, what, k_cache, v_cache, k_scale, v_scale)
     dt = _dtypes.get(q.dtype)
     shape = q.shape
@@ -332,6 +334,8 @@ def pf_prefix_attention(q, k_cache, v_cache, k_scale, v_scale, lengths, table, p
     cols = prefix_table.shape[1]
     if (n_seq | heads | table.shape[1] | n_groups | cols) >> 31:
         _cut_off(what)
+    if status is not None and (status.dtype != torch.int32 or status.numel() != 1):
+        _refuse(f"{what}: status is one int32")
     res = {}
     if out is None:
         out = _like(torch, q)
@@ -347,12 +351,12 @@ def pf_prefix_attention(q, k_cache, v_cache, k_scale, v_scale, lengths, table, p
         workspace = torch.empty(size, dtype=torch.uint8, device=q.device)
     else:
         size = _work_bytes(workspace, what)
-    status = L.pf_prefix_attention(c, dt, n_seq, heads, q.data_ptr(), _heads(q, what, heads, hd), _int32(torch, what, lengths, 1), _int32(torch, what, table, 2),
-                                   table.shape[1], n_groups, None if cu_seqs is None else _int32(torch, what, cu_seqs, 1), _int32(torch, what, prefix_lengths, 1),
-                                   _int32(torch, what, prefix_table, 2), cols, 1.0 / math.sqrt(hd) if sm_scale is None else sm_scale, out.data_ptr(),
-                                   _heads(out, what, heads, hd), lse_ptr, workspace.data_ptr(), size, _stream(torch, dev, None))
-    if status != PF_OK:
-        _check(status, what)
+    code = L.pf_prefix_attention_status(c, dt, n_seq, heads, q.data_ptr(), _heads(q, what, heads, hd), _int32(torch, what, lengths, 1), _int32(torch, what, table, 2),
+                                        table.shape[1], n_groups, None if cu_seqs is None else _int32(torch, what, cu_seqs, 1), _int32(torch, what, prefix_lengths, 1),
+                                        _int32(torch, what, prefix_table, 2), cols, 1.0 / math.sqrt(hd) if sm_scale is None else sm_scale, out.data_ptr(),
+                                        _heads(out, what, heads, hd), lse_ptr, _ptr(status), workspace.data_ptr(), size, _stream(torch, dev, None))
+    if code != PF_OK:
+        _check(code, what)
     return res
 
 
