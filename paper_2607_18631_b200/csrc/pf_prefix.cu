@@ -25,6 +25,7 @@
 #include <math.h>
 
 #include <atomic>
+#include <type_traits>
 
 #include "pf_attention.cuh"
 #include "pf_tcgen.cuh"
@@ -37,6 +38,7 @@ constexpr int kAhead = 4;                // tiles that are under way from HBM to
 constexpr int kLeastTiles = 1;           // a piece takes no fewer while others have none
 constexpr unsigned kWaitLimit = 500000, kDrainLimit = 500000;      // polls of 2 us: a second
 std::atomic<unsigned> g_wait_limit{kWaitLimit}, g_wait_lost{0};      // host: what the next calls do (pf_prefix_waits)
+constexpr float kCoarse = 131072.f;      // references from here on: a unit in the last place is 2^-6 or more
 constexpr float kSetLift = 7.f;          // log2 of the largest weight when a row's reference is set; it may grow to kLift
 
 struct PrefixArgs {
@@ -611,19 +613,22 @@ __device__ __forceinline__ bool rows_run(const PrefixArgs &P, const PrefixRoom &
                 }
             }
             const float ref = z == -INFINITY ? 0.f : z;
-#pragma unroll
-            for (int c = 0; c < 4; c++) {
+            // weights of tokens 32 c .. 32 c + 31 (two groups of scores), over scores that have been read
+            auto weigh = [&](auto any_coarse, bool coarse, const uint32_t (&y0)[16], const uint32_t (&y1)[16], int c) {
                 uint32_t w[16];
 #pragma unroll
                 for (int h = 0; h < 2; h++) {
-                    const int g = 2 * c + h;
-                    const float4 sc = scale_of(g);
-                    const float shift = sc.y - ref;
-                    const Two ff = two(sc.x, sc.x), ss = two(shift, shift);
+                    const uint32_t(&y)[16] = h ? y1 : y0;
+                    const float4 sc = scale_of(2 * c + h);
+                    const bool first = decltype(any_coarse)::value && coarse;
+                    const float times = first ? 1.f : sc.x, shift = first ? -ref : sc.y - ref;
+                    const Two ff = two(times, times), ss = two(shift, shift);
                     Two sum = two(0.f, 0.f);
 #pragma unroll
                     for (int k = 0; k < 8; k++) {
-                        const Two a = fma2(two(score_of(x, 16 * g + 2 * k), score_of(x, 16 * g + 2 * k + 1)), ff, ss);
+                        float p = __uint_as_float(y[2 * k]), q = __uint_as_float(y[2 * k + 1]);
+                        if (first) p = fmaf(p, sc.x, sc.y), q = fmaf(q, sc.x, sc.y);
+                        const Two a = fma2(two(p, q), ff, ss);
                         float e0, e1;
                         if (k % 4 == 3) {               // a quarter: the special-function unit and the others take about as long
                             pow2_two(a, e0, e1);
@@ -639,12 +644,29 @@ __device__ __forceinline__ bool rows_run(const PrefixArgs &P, const PrefixRoom &
                     apart(sum, s0, s1);
                     l32 = fmaf(s0 + s1, sc.z, l32);
                 }
-                tmem_st16(score + 16 * c, w);           // over scores that have been read
+                tmem_st16(score + 16 * c, w);
                 if (c == 1) {                           // half of the weights: their products may begin
                     tmem_wait_st();
                     tmem_before_sync();
                     __syncwarp();
                     if (lane == 0) R.arrive(B_PHALF + j);
+                }
+            };
+            // A weight is 2^(score x scale + (log2 - reference)), the product not rounded.  Where fp32 is coarse at the reference's size the rounding of that sum could lift it by
+            // any amount, so there the score is rounded first, as for the reference itself: no weight is above what the reference allows then.
+            const bool coarse = fabsf(ref) >= kCoarse;
+            if (!__any_sync(0xFFFFFFFFu, coarse)) {
+#pragma unroll
+                for (int c = 0; c < 4; c++) weigh(std::false_type{}, false, x[2 * c], x[2 * c + 1], c);
+            } else {
+#pragma unroll 1
+                for (int c = 0; c < 4; c++) {           // rare, so little code: the scores are read anew
+                    uint32_t y0[16], y1[16];
+                    tmem_ld16(score + 32 * c, y0);
+                    tmem_ld16(score + 32 * c + 16, y1);
+                    tmem_wait_ld(y0);
+                    tmem_named(y1);
+                    weigh(std::true_type{}, coarse, y0, y1, c);
                 }
             }
             tmem_wait_st();
