@@ -140,7 +140,7 @@ int pf_kv_append_rope(const pf_kv_cache_t *cache, const pf_rotary_t *rotary, int
  *   out[b, h] = softmax over both of sm_scale * q[b, h] . K[t], times V[t]
  * d_cu_seqs: n_groups + 1 offsets that do not decrease (NULL, with one group: all sequences); a sequence in no group sees its own tokens only.  Prefixes of any length, and tables, lengths,
  * missing pages, scales, q, out and lse otherwise as in pf_decode_attention.  A row that sees no token gives zeros and -infinity.
- * A prefix token's weight enters the values' sum with 11 bits (fewer below 2^-21 of the row's largest, none below 2^-32).
+ * Weights enter the values' sum with the bits that they have there.
  * A wait inside the kernel that runs out makes the rows that it concerns NaN; pf_prefix_attention_status says so too: one int32 of device memory, 0 after a
  * complete call, 1 otherwise (d_status may be NULL: pf_prefix_attention).
  * Values are added up in 32 bits over 65536 tokens at a time, more in calls of more than 4.8 million (tile of rows, 128 tokens) pairs.

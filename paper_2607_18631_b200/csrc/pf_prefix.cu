@@ -11,8 +11,8 @@
 // weights P in tensor memory, where the threads that own the rows put them over the scores.  The cache's e4m3 is widened to fp16 in between (exact), as in the kernel of the own
 // tokens, so queries keep all their bits and weights 11; scores, references, sums and values are fp32.  The value scale joins the exponent, as there.
 // A block has two streams of 128 rows, so that the products of one are under way while the other's weights are computed; with no more than 128 rows both
-// go through the same ones and take turns with the tiles.  A row's reference is the largest score so far, lifted by 2^7, and stays until a weight would pass
-// 2^15: tensor memory's values are seldom scaled anew.  Warps have one role each and meet at barriers in shared memory:
+// go through the same ones and take turns with the tiles.  A row's reference lies 15 below the largest score when it is set, and stays until a weight would pass
+// 2^15.9: tensor memory's values are scaled anew in the first tiles of a piece for the most part.  Warps have one role each and meet at barriers in shared memory:
 //   plan -> copy (bulk, half tiles) -> widen -> products <-> rows.
 // What bounds it.  Many rows: 128 x 128 scores take the products 1024 cycles, the special-function unit 768 (a quarter of the powers are polynomials) and shared memory
 // 1280 (operands 768, the cache's bytes in, out and widened 1024 a tile that two streams share), and the chain scores -> largest -> powers -> products of a stream 3900, of which the
@@ -39,7 +39,9 @@ constexpr int kLeastTiles = 1;           // a piece takes no fewer while others 
 constexpr unsigned kWaitLimit = 500000, kDrainLimit = 500000;      // polls of 2 us: a second
 std::atomic<unsigned> g_wait_limit{kWaitLimit}, g_wait_lost{0};      // host: what the next calls do (pf_prefix_waits)
 constexpr float kCoarse = 131072.f;      // references from here on: a unit in the last place is 2^-6 or more
-constexpr float kSetLift = 7.f;          // log2 of the largest weight when a row's reference is set; it may grow to kLift
+// log2 of the largest weight when a row's reference is set (kLift, as in the kernel of the own tokens: weights keep 11 bits down to 2^-29 of the largest and count down
+// to 2^-40 of it), and what it may grow to before the reference is set anew: fp16 ends at 2^15.9999
+constexpr float kMostLift = 15.9f;
 
 struct PrefixArgs {
     AttnArgs a;
@@ -593,9 +595,10 @@ __device__ __forceinline__ bool rows_run(const PrefixArgs &P, const PrefixRoom &
             }
             // a score that is no number, or infinite, makes the row NaN, whichever way its weight is computed
             if (!(top < INFINITY)) l = __int_as_float(0x7FC00000);
-            // A new reference where a weight would pass 2^15; it brings the largest to 2^7, so that the next one is far off.
-            if (__any_sync(0xFFFFFFFFu, __fsub_ru(top, kLift) > z)) {
-                const float n = __fsub_ru(top, kLift) > z ? __fsub_ru(top, kSetLift) : z;
+            // A new reference where a weight would pass 2^15.9; it brings the largest to 2^15.  (Less, with more room to the next time, costs the small weights their bits: with 2^14
+            // 1 to 2 % less time, with 2^7 3 to 5 %.  Moving the other rows of the warp along would save 0.7 %, but a row's bits would depend on its neighbours.)
+            if (__any_sync(0xFFFFFFFFu, __fsub_ru(top, kMostLift) > z)) {
+                const float n = __fsub_ru(top, kMostLift) > z ? __fsub_ru(top, kLift) : z;
                 const float a = n == -INFINITY ? 1.f : ex2(z - n);
                 z = n;
                 l *= a;
