@@ -463,7 +463,7 @@ __device__ __forceinline__ Two fma2(Two a, Two b, Two c) { Two r; asm("fma.rn.f3
 // (what lies below the normals counts as 0)
 __device__ __forceinline__ Two add2(Two a, Two b) { Two r; asm("add.rn.ftz.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v)); return r; }
 // 2^a without the special-function unit, which computes 16 a cycle and SM where a tile asks for 16384: a = n + f, n whole, |f| <= 1/2, and the
-// polynomial of degree 4 that is nearest to 2^f there (relative error 2.6e-6, found by exchange).  Below 2^-126 (-infinity) a
+// polynomial of degree 5 that is nearest to 2^f there (found by exchange; in 32 bits 2^-22 relative, as the unit's).  Below 2^-126 (-infinity) a
 // number below the normals comes out, which add2 and the conversion to fp16 take as 0: value scales reach 2^118, so 2^-126 times an inverse scale could outweigh the sum.  No NaN comes out.
 __device__ __forceinline__ void pow2_two(Two a, float &lo, float &hi)
 {
@@ -472,10 +472,11 @@ __device__ __forceinline__ void pow2_two(Two a, float &lo, float &hi)
     a = two(fmaxf(x, -126.75f), fmaxf(y, -126.75f));      // n = -127, f = 1/4
     const float big = 12582912.f;                       // 1.5 * 2^23: what is added to it is rounded to a whole number
     const Two m = add2(a, two(big, big)), n = add2(m, two(-big, -big)), f = fma2(n, two(-1.f, -1.f), a);
-    Two r = fma2(f, two(0.009570102207362652f, 0.009570102207362652f), two(0.05591785907745361f, 0.05591785907745361f));
-    r = fma2(r, f, two(0.240247443318367f, 0.240247443318367f));
-    r = fma2(r, f, two(0.6931217908859253f, 0.6931217908859253f));
-    r = fma2(r, f, two(0.9999992847442627f, 0.9999992847442627f));
+    Two r = fma2(f, two(0.0013276472454890609f, 0.0013276472454890609f), two(0.009675540961325169f, 0.009675540961325169f));
+    r = fma2(r, f, two(0.05550713092088699f, 0.05550713092088699f));
+    r = fma2(r, f, two(0.24022120237350464f, 0.24022120237350464f));
+    r = fma2(r, f, two(0.6931469440460205f, 0.6931469440460205f));
+    r = fma2(r, f, two(1.0000001192092896f, 1.0000001192092896f));
     float mx, my;
     apart(m, mx, my);
     apart(r, x, y);
