@@ -17,19 +17,28 @@ struct Rot {
     float amp, flip;          // m, and -1 where the transposed rotation is asked for
 };
 
-// cosine and sine of a pair's angle.  For results in 16 or 8 bits the special-function unit's, within 2^-21.4 between -pi and pi, an eighth of fp16's half step
-// (sincospif's took a third of the time of prompts' keys, which need them for every head); for results in 32 bits sincospif's.
+// Cosine and sine of a pair's angle, each within 2^-23 of its own size, so that an element next to a zero of its sine or cosine is as exact as the others.  The angle is taken apart into
+// quarter turns and the rest, an integer of 30 bits between -1/8 and 1/8 of a turn.  Of the rest u (in eighths) the sine is u S(u^2), the cosine C(u^2), of the least degrees whose
+// nearest polynomials (by exchange, relative) are off by less than 2^-28; the sine's first coefficient, pi / 4, is two numbers.  8192 tokens of 40 heads of 128: 31.5 us, with the
+// special-function unit 30.9, which is off by up to 2^-21.4 of the pair's length whatever the element's size.
+// FAST, for results in 8 bits: the unit's.  At the page's scale e4m3's least half step is 2^-18.8 of the largest element, and an element is off by 2^-20.4 of it at most.
 template <bool FAST>
 __device__ __forceinline__ void turn_of(const Rot &r, int pair, int32_t pos, float &c, float &s)
 {
     const uint64_t f = __ldg(r.phase + pair);
-    const float t = (float)(int32_t)(uint32_t)(((uint64_t)(int64_t)pos * f) >> 32);
+    const int32_t t = (int32_t)(uint32_t)(((uint64_t)(int64_t)pos * f) >> 32);
     if (FAST) {
-        const float x = t * 1.4629180792671596e-9f;                     // pi 2^-31
+        const float x = (float)t * 1.4629180792671596e-9f;              // pi 2^-31
         c = __cosf(x);
         s = __sinf(x);
     } else {
-        sincospif(t * 4.656612873077393e-10f, &s, &c);                  // 2^-31
+        const uint32_t quarter = ((uint32_t)t + 0x20000000u) >> 30;
+        const float u = (float)(int32_t)((uint32_t)t - (quarter << 30)) * 1.862645149230957e-9f, v = u * u;      // 2^-29
+        const float sine = fmaf(u, 0.7853981852531433f, u * fmaf(fmaf(fmaf(-3.59504520019982e-5f, v, 2.49000103212893e-3f), v, -0.08074543625116348f), v, -2.1855694e-8f));
+        const float cosine = fmaf(fmaf(fmaf(fmaf(3.52876168108196e-6f, v, -3.259365039411932e-4f), v, 0.015854323282837868f), v, -0.3084251284599304f), v, 1.f);
+        const bool swap = quarter & 1;
+        c = __uint_as_float(__float_as_uint(swap ? sine : cosine) ^ ((quarter + 1) & 2) << 30);
+        s = __uint_as_float(__float_as_uint(swap ? cosine : sine) ^ (quarter & 2) << 30);
     }
     c *= r.amp;
     s *= r.amp * r.flip;
@@ -151,7 +160,7 @@ __device__ __forceinline__ void rope_heads(const Rot &r, int32_t pos, int hd, in
 {
     const Runs<HALF> run(chunk, r.rot, hd);
     float c[8], s[8];
-    run.template angles<sizeof(T) == 2>(r, pos, c, s);
+    run.template angles<false>(r, pos, c, s);
     // x and y may be one tensor, so the loads of a few heads are asked for before the first store
     for (int h = 0; h < n; h += B) {
         Run8<T> in[B][2];
@@ -207,7 +216,7 @@ __global__ void __launch_bounds__(256) rope_any_kernel(const RopeArgs A)
         return;
     }
     float c, s;
-    turn_of<sizeof(T) == 2>(A.r, i, A.pos[t], c, s);
+    turn_of<false>(A.r, i, A.pos[t], c, s);
     const int a = HALF ? i : 2 * i, b = HALF ? i + pairs : 2 * i + 1;
     const float p = get1<T>(x + a), q = get1<T>(x + b);
     put1<T>(y + a, fmaf(p, c, -q * s));
