@@ -10,11 +10,14 @@ stream the call runs on (`stream`, or the current one).  There is no CPU path.
 That they are ready on that stream, and that its results are not used elsewhere before they are, is up to the caller.
 
 8-bit tensors are torch.float8_e4m3fn.
+
+pf_rope is differentiable; the other operators are for serving, and what they return has no graph.
 """
 from __future__ import annotations
 
 import contextlib
 import ctypes as C
+import functools
 import math
 
 from .binding import PF_EINVAL, PF_ERANGE, PF_OK, PlanfrontError, _check, _torch, i32, i64, load_library
@@ -409,17 +412,44 @@ def _strided_heads(t, what):
     return strides[0], strides[1]
 
 
+@functools.cache
+def _differentiable_rope():
+    torch = _torch()
+
+    class Rope(torch.autograd.Function):
+        @staticmethod
+        def forward(ctx, x, positions, rotary, transposed):
+            ctx.save_for_backward(positions)
+            ctx.rotary, ctx.transposed = rotary, transposed
+            return pf_rope(x, positions, rotary, transposed=transposed)
+
+        @staticmethod
+        def backward(ctx, dy):
+            positions, = ctx.saved_tensors
+            if dy.stride(2) != 1 or 0 in dy.stride():      # expanded, as a sum's gradient is
+                dy = dy.clone(memory_format=torch.contiguous_format)
+            return pf_rope(dy, positions, ctx.rotary, transposed=not ctx.transposed), None, None, None
+    return Rope.apply
+
+
 def pf_rope(x, positions, rotary: Rotary, *, transposed: bool = False, out=None, stream=None):
     """Heads rotated to their tokens' positions: [tokens, heads, head_dim] bf16, fp16 or fp32, heads contiguous, tokens and heads at any stride.
 
     positions: [tokens] int32.  transposed: the transposed rotation, which takes the gradient with respect to the result to
-    that with respect to x.  out: like x (x itself allowed); returned."""
+    that with respect to x.  out: like x (x itself allowed); returned.
+
+    Differentiable with respect to x, any number of times; positions then stay as they are until the backward pass (it raises if they did not), and `out`
+    is refused."""
     L, torch = _ready or _lib()
     if stream is not None:
         _used_on(torch, stream, x, positions, rotary.phase, out)
         with torch.cuda.stream(stream):
             return pf_rope(x, positions, rotary, transposed=transposed, out=out)
     what = "pf_rope"
+    if (x.requires_grad or (out is not None and out.requires_grad)) and torch.is_grad_enabled():
+        if out is not None:
+            _refuse(f"{what}: out with a tensor that requires grad")
+        return _differentiable_rope()(x, positions, rotary, transposed)
     dev = _on_device(torch, what, x, positions, rotary.phase, out)
     dt = _dtypes.get(x.dtype)
     if dt is None or x.dim() != 3:
