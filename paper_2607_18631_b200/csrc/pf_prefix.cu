@@ -47,46 +47,50 @@ struct PrefixArgs {
     AttnArgs a;
     const int32_t *ptable;
     unsigned wait_limit, wait_lost;      // polls of a wait inside the kernel; whether a block waits for what does not come (a test of the limit)
-    long long n_slots;
+    long long n_rows;                    // rows of partial results
     uint32_t *status;                    // [blocks], written by those with work
-    float *slots;                        // [n_slots] x (kRows x HD values, kRows references, kRows sums)
+    float *part_v, *part_z, *part_l;     // [n_rows] x HD values, references, sums
     int32_t *report;                     // the call's status, or NULL
 };
 
-// Tiles and tasks of the groups in front of each group, by the whole block.  units, tasks: n_groups + 1 words; scratch: 100
-__device__ __forceinline__ void group_prefix(const PrefixArgs &P, long long *units, int *tasks, int *scratch)
+// Partial results.  A task (a tile of a group's rows of a key head) takes as many rows as it has, twice as many where both streams go through the same ones, and each piece of the list leaves
+// those of its tasks `piece_rows` further on than the piece in front, which is no less than any task takes: neighbours on the list are apart.
+__host__ __device__ __forceinline__ int task_rows(int rows) { return rows <= 128 ? 2 * rows : rows; }
+__host__ __device__ __forceinline__ int piece_rows(int n_seq, int group) { return n_seq * (long long)group < kRows / 2 ? 2 * n_seq * group : kRows; }
+// rows of a group's tasks of one key head
+__device__ __forceinline__ int head_rows(const Group &g) { return (g.row_tiles - 1) * kRows + task_rows(g.rows - (g.row_tiles - 1) * kRows); }
+
+// Tiles, and rows of partial results, of the groups in front of each group, by the whole block.  units, rows: n_groups + 1 words; scratch: 64
+__device__ __forceinline__ void group_prefix(const PrefixArgs &P, long long *units, long long *rows, long long *scratch)
 {
-    int *warp_tasks = scratch;
-    long long *warp_units = reinterpret_cast<long long *>(scratch + 32 + ((uintptr_t)scratch & 4 ? 1 : 0));
+    long long *warp_rows = scratch, *warp_units = scratch + 32;
     const int nt = blockDim.x, tid = threadIdx.x, lane = tid & 31, nw = (nt + 31) >> 5;
-    long long base_u = 0;
-    int base_t = 0;
-    if (tid == 0) units[0] = 0, tasks[0] = 0;
+    long long base_u = 0, base_r = 0;
+    if (tid == 0) units[0] = rows[0] = 0;
     for (int g0 = 0; g0 < P.a.n_groups; g0 += nt) {
-        long long u = 0;
-        int t = 0;
+        long long u = 0, r = 0;
         if (g0 + tid < P.a.n_groups) {
-            const Group r = group_of(P.a, g0 + tid);
-            t = r.tiles ? r.row_tiles * P.a.c.n_kv : 0;
-            u = (long long)t * r.tiles;
+            const Group g = group_of(P.a, g0 + tid);
+            if (g.tiles && g.row_tiles) {
+                u = (long long)g.row_tiles * P.a.c.n_kv * g.tiles;
+                r = (long long)head_rows(g) * P.a.c.n_kv;
+            }
         }
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
-            const long long pu = __shfl_up_sync(0xFFFFFFFFu, u, o);
-            const int pt = __shfl_up_sync(0xFFFFFFFFu, t, o);
-            if (lane >= o) u += pu, t += pt;
+            const long long pu = __shfl_up_sync(0xFFFFFFFFu, u, o), pr = __shfl_up_sync(0xFFFFFFFFu, r, o);
+            if (lane >= o) u += pu, r += pr;
         }
         __syncthreads();
-        if (lane == 31) warp_units[tid >> 5] = u, warp_tasks[tid >> 5] = t;
+        if (lane == 31) warp_units[tid >> 5] = u, warp_rows[tid >> 5] = r;
         __syncthreads();
-        long long add_u = base_u;
-        int add_t = base_t;
+        long long add_u = base_u, add_r = base_r;
         for (int i = 0; i < nw; i++) {
-            if (i < (tid >> 5)) add_u += warp_units[i], add_t += warp_tasks[i];
+            if (i < (tid >> 5)) add_u += warp_units[i], add_r += warp_rows[i];
             base_u += warp_units[i];
-            base_t += warp_tasks[i];
+            base_r += warp_rows[i];
         }
-        if (g0 + tid < P.a.n_groups) units[g0 + tid + 1] = add_u + u, tasks[g0 + tid + 1] = add_t + t;
+        if (g0 + tid < P.a.n_groups) units[g0 + tid + 1] = add_u + u, rows[g0 + tid + 1] = add_r + r;
     }
     __syncthreads();
 }
@@ -117,7 +121,7 @@ struct __align__(16) Stretch {
     int group, first, members, len;      // the group, its first sequence, its rows, and its tokens
     int kv, row0, rows, tile;            // the task's rows are row0 .. row0 + rows - 1 of the group
     int end, pad;                        // (end = tile: there are no more)
-    long long slot;
+    long long at;                        // the first of its rows of partial results
     // few rows: both streams go through the same rows, and take turns with the tiles
     __device__ __forceinline__ bool turns() const { return rows <= 128; }
     __device__ __forceinline__ int tiles_of(int stream) const { return turns() ? (end - tile + 1 - stream) / 2 : end - tile; }
@@ -181,13 +185,13 @@ struct PrefixRoom {                     // what the roles share
     }
 };
 
-// ---- one thread finds the block's stretches, one ahead: pieces follow one another, so where the first begins is looked up once (`units`, `tasks`: before the others
+// ---- one thread finds the block's stretches, one ahead: pieces follow one another, so where the first begins is looked up once (`units`, `rows`: before the others
 // overwrite them), and from there it goes on by itself
 struct Walk {
     Group g;
-    int group, task, no, tile, piece, last, n_pieces;   // task: number of the group's first
-    long long total;
-    __device__ __forceinline__ bool begin(const PrefixArgs &P, const long long *units, const int *tasks, int blocks)
+    int group, no, tile, piece, last, n_pieces;         // no: of the group's tasks
+    long long total, row;                               // row: the group's first of partial results
+    __device__ __forceinline__ bool begin(const PrefixArgs &P, const long long *units, const long long *rows, int blocks)
     {
         total = units[P.a.n_groups];
         n_pieces = total ? pieces_of(total, blocks) : 0;
@@ -198,7 +202,7 @@ struct Walk {
         const long long u = first_tile(total, n_pieces, piece);
         group = last_at(units, P.a.n_groups, u);
         g = group_of(P.a, group);
-        task = tasks[group];
+        row = rows[group];
         no = (int)((u - units[group]) / g.tiles);
         tile = (int)((u - units[group]) - (long long)no * g.tiles);
         return true;
@@ -212,7 +216,7 @@ __device__ __forceinline__ void plan_role(const PrefixArgs &P, const PrefixRoom 
         int left = (int)(first_tile(k.total, k.n_pieces, k.piece + 1) - first_tile(k.total, k.n_pieces, k.piece));
         while (left > 0) {
             while (k.no >= (k.g.tiles ? k.g.row_tiles * P.a.c.n_kv : 0)) {
-                if (k.g.tiles) k.task += k.g.row_tiles * P.a.c.n_kv;
+                if (k.g.tiles && k.g.row_tiles) k.row += (long long)head_rows(k.g) * P.a.c.n_kv;
                 k.no = 0;
                 if (++k.group >= P.a.n_groups) return;    // (not reached: the list ends with the last piece)
                 k.g = group_of(P.a, k.group);
@@ -225,7 +229,7 @@ __device__ __forceinline__ void plan_role(const PrefixArgs &P, const PrefixRoom 
             s.tile = k.tile;
             s.end = min(k.g.tiles, k.tile + left);
             s.pad = 0;
-            s.slot = (long long)k.task + k.no + k.piece;
+            s.at = k.row + (long long)s.kv * head_rows(k.g) + s.row0 + (long long)k.piece * piece_rows(P.a.n_seq, P.a.group);
             left -= s.end - s.tile;
             k.tile = s.end;
             if (k.tile == k.g.tiles) {
@@ -700,12 +704,13 @@ __device__ __forceinline__ void rows_role(const PrefixArgs &P, const PrefixRoom 
         const int count = s.tiles_of(j);
         if (!rows_run<T, HD>(P, R, s, j, all, tiles, zl) || !R.wait_warp(B_OFULL + j, runs)) return;
         all += s.end - s.tile;
-        const int row = s.turns() ? r : 128 * j + r, place = 128 * j + r;
-        const bool live = row < s.rows && s.slot < P.n_slots;
-        float *to = P.slots + s.slot * (kRows * (HD + 2));
+        const int row = s.turns() ? r : 128 * j + r;
+        const long long place = s.at + (s.turns() ? j * s.rows : 128 * j) + r;
+        const bool live = row < s.rows && place < P.n_rows;
+        float *to = P.part_v + place * HD;
         if (live) {
-            to[kRows * HD + place] = zl[0];
-            to[kRows * (HD + 1) + place] = zl[1];
+            P.part_z[place] = zl[0];
+            P.part_l[place] = zl[1];
         }
         if (count) {
             tmem_after_sync();
@@ -716,12 +721,12 @@ __device__ __forceinline__ void rows_role(const PrefixArgs &P, const PrefixRoom 
                 tmem_wait_ld(x);
                 if (live)
 #pragma unroll
-                    for (int k = 0; k < 16; k += 4) *reinterpret_cast<uint4 *>(to + place * HD + 16 * c + k) = make_uint4(x[k], x[k + 1], x[k + 2], x[k + 3]);
+                    for (int k = 0; k < 16; k += 4) *reinterpret_cast<uint4 *>(to + 16 * c + k) = make_uint4(x[k], x[k + 1], x[k + 2], x[k + 3]);
             }
             tmem_before_sync();
         } else if (live) {
 #pragma unroll 1
-            for (int k = 0; k < HD; k += 4) *reinterpret_cast<uint4 *>(to + place * HD + k) = make_uint4(0u, 0u, 0u, 0u);
+            for (int k = 0; k < HD; k += 4) *reinterpret_cast<uint4 *>(to + k) = make_uint4(0u, 0u, 0u, 0u);
         }
     }
 }
@@ -734,11 +739,11 @@ __global__ void __launch_bounds__(kPrefixThreads, 1) prefix_kernel(const __grid_
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     // the groups' prefix sums lie where operands come later
     long long *units = reinterpret_cast<long long *>(prefix_smem);
-    int *tasks = reinterpret_cast<int *>(units + PF_PREFIX_MAX_GROUPS + 1);
-    group_prefix(P, units, tasks, tasks + PF_PREFIX_MAX_GROUPS + 1);
-    const int blocks = prefix_share(units[P.a.n_groups], own_tiles(P.a, reinterpret_cast<long long *>(prefix_smem + 16384)), gridDim.x);
+    long long *rows = units + PF_PREFIX_MAX_GROUPS + 1;
+    group_prefix(P, units, rows, rows + PF_PREFIX_MAX_GROUPS + 1);
+    const int blocks = prefix_share(units[P.a.n_groups], own_tiles(P.a, rows + PF_PREFIX_MAX_GROUPS + 1), gridDim.x);
     Walk walk;
-    if (!walk.begin(P, units, tasks, blocks)) return;
+    if (!walk.begin(P, units, rows, blocks)) return;
     uint32_t *words = reinterpret_cast<uint32_t *>(prefix_smem + S::kBars + 8 * B_COUNT);
     uint32_t *gave_up = words + 1;
     Stretch *plan = reinterpret_cast<Stretch *>(prefix_smem + S::kPlan);
@@ -810,16 +815,17 @@ __global__ void __launch_bounds__(256, 4) prefix_join_kernel(const __grid_consta
     const AttnArgs &A = P.a;
     extern __shared__ __align__(128) uint8_t smem[];
     long long *units = reinterpret_cast<long long *>(smem);
-    int *tasks = reinterpret_cast<int *>(units + P.a.n_groups + 1);
-    int *prefix = tasks + P.a.n_groups + 1;
+    long long *rows = units + P.a.n_groups + 1;
+    int *prefix = reinterpret_cast<int *>(rows + P.a.n_groups + 1);
     __shared__ int warp_sum[8];
-    __shared__ __align__(8) int scratch[100];
-    group_prefix(P, units, tasks, scratch);
+    __shared__ long long scratch[64];
+    group_prefix(P, units, rows, scratch);
     tile_prefix(A, prefix, warp_sum);
     const int lane = threadIdx.x & 31;
     const long long total = units[P.a.n_groups], own_total = (long long)prefix[A.n_seq] * A.jobs_per_seq;
     const int share = prefix_share(total, own_total, prefix_grid), n_pieces = total ? pieces_of(total, share) : 0;
     const int each = share ? pieces_each(n_pieces, share) : 1, own_blocks = own_total ? blocks_used(own_total, own_grid - share) : 1;
+    const int next = piece_rows(A.n_seq, A.group);
     bool waited = false;                          // where a warp's first row has its parts follows from the lengths alone
     const float *blocks = A.part + (int64_t)own_grid * S::kWarps * S::kPartFloats;
     const long long n_rows = (long long)A.n_seq * A.n_heads;
@@ -837,21 +843,20 @@ __global__ void __launch_bounds__(256, 4) prefix_join_kernel(const __grid_consta
             n_own = piece_of(own_total, own_blocks, begin + own_tiles - 1) - w0 + 1;
         }
         // parts of its group's prefix
-        long long slot = 0;
-        int n_pre = 0, at = 0, p0 = 0, both = 1;  // parts of a slot
+        long long at = 0;                         // the first's row; the other stream's is `apart` further on, the next piece's `next`
+        int n_pre = 0, p0 = 0, both = 1, apart = 0;      // both: parts of a piece
         if (total) {
             const int gi = P.a.cu ? last_at(P.a.cu, P.a.n_groups, b) : 0;
             const Group g = group_of(P.a, gi);
             if (g.tiles && b >= g.first && b < g.first + g.rows / A.group) {
-                at = (b - g.first) * A.group + gh;
-                const int no = kv * g.row_tiles + at / kRows;
-                both = g.rows - at / kRows * kRows <= 128 ? 2 : 1;
-                at %= kRows;
+                const int r = (b - g.first) * A.group + gh, no = kv * g.row_tiles + r / kRows;
+                apart = g.rows - r / kRows * kRows;
+                both = apart <= 128 ? 2 : 1;
                 const long long begin = units[gi] + (long long)no * g.tiles;
                 p0 = piece_of(total, n_pieces, begin);
                 n_pre = piece_of(total, n_pieces, begin + g.tiles - 1) - p0 + 1;
-                slot = (long long)tasks[gi] + no + p0;
-                if (slot + n_pre > P.n_slots) n_pre = 0;
+                at = rows[gi] + (long long)kv * head_rows(g) + r + (long long)p0 * next;
+                if (at + (long long)(n_pre - 1) * next + (both == 2 ? apart : 0) >= P.n_rows) n_pre = 0;
                 n_pre *= both;
             }
         }
@@ -875,11 +880,11 @@ __global__ void __launch_bounds__(256, 4) prefix_join_kernel(const __grid_consta
                 z = p[S::kHeads * HD + own_row];
                 l = p[S::kHeads * (HD + 1) + own_row];
             } else if (i < n) {
-                const int no = i - n_own, place = both == 2 ? at + 128 * (no & 1) : at;
-                const float *p = P.slots + (slot + (both == 2 ? no >> 1 : no)) * (kRows * (HD + 2));
-                from = p + place * HD;
-                z = p[kRows * HD + place];
-                l = P.status[(p0 + (both == 2 ? no >> 1 : no)) / each] ? __int_as_float(0x7FC00000) : p[kRows * (HD + 1) + place];
+                const int no = i - n_own, piece = both == 2 ? no >> 1 : no;
+                const long long place = at + (long long)piece * next + (both == 2 && (no & 1) ? apart : 0);
+                from = P.part_v + place * HD;
+                z = P.part_z[place];
+                l = P.status[(p0 + piece) / each] ? __int_as_float(0x7FC00000) : P.part_l[place];
             }
             float most = fmaxf(top, z);
 #pragma unroll
@@ -930,8 +935,8 @@ __global__ void __launch_bounds__(256, 4) prefix_join_kernel(const __grid_consta
 
 // ------------------------------------------------------------------ host
 struct PrefixSizes {
-    size_t own_v, own_z, own_l, status, slots, bytes;      // offsets in the workspace, and its size
-    long long n_slots;
+    size_t own_v, own_z, own_l, status, part_v, part_z, part_l, bytes;      // offsets in the workspace, and its size
+    long long n_rows;
 };
 static PrefixSizes prefix_sizes(int hd, int page, int n_kv, int n_seq, int n_heads, int n_groups, int pcols, int sms)
 {
@@ -942,12 +947,16 @@ static PrefixSizes prefix_sizes(int hd, int page, int n_kv, int n_seq, int n_hea
     s.own_z = s.own_v + up(rows * hd * 4);
     s.own_l = s.own_z + up(rows * 4);
     s.status = s.own_l + up(rows * 4);
-    s.slots = s.status + up((size_t)sms * 4);
+    s.part_v = s.status + up((size_t)sms * 4);
     const long long tiles = ((long long)pcols * page + kTok - 1) / kTok;
     const long long tasks = (long long)n_kv * (((long long)n_seq * (n_heads / n_kv)) / kRows + n_groups);
-    const long long pieces = tasks * tiles / kMostTiles + sms;
-    s.n_slots = tasks + (pieces < (long long)kMostPieces * sms ? pieces : (long long)kMostPieces * sms) + sms;      // one for each piece of each task
-    s.bytes = s.slots + (size_t)s.n_slots * kRows * (hd + 2) * 4;
+    const long long wanted = tasks * tiles / kMostTiles + sms, pieces = wanted < (long long)kMostPieces * sms ? wanted : (long long)kMostPieces * sms;
+    // all tasks' rows (of n_groups unknown sizes), and what the pieces are apart
+    const long long all = 2 * (long long)rows < tasks * kRows ? 2 * (long long)rows : tasks * kRows;
+    s.n_rows = all + pieces * piece_rows(n_seq, n_heads / n_kv);
+    s.part_z = s.part_v + up((size_t)s.n_rows * hd * 4);
+    s.part_l = s.part_z + up((size_t)s.n_rows * 4);
+    s.bytes = s.part_l + up((size_t)s.n_rows * 4);
     return s;
 }
 
@@ -958,7 +967,7 @@ static int prefix_launch(PrefixArgs p, int device, int sms, cudaStream_t st)
     AttnArgs &a = p.a;
     a.row_blocks = (a.group + S::kHeads - 1) / S::kHeads;
     a.jobs_per_seq = a.c.n_kv * a.row_blocks;
-    const size_t groups = (size_t)(p.a.n_groups + 1) * 12, own = ((size_t)a.n_seq + 1) * 4;
+    const size_t groups = (size_t)(p.a.n_groups + 1) * 16, own = ((size_t)a.n_seq + 1) * 4;
     const size_t smem0 = PrefixShape<HD>::kBytes, smem1 = (size_t)S::kWarps * S::kWarpBytes + own, smem2 = groups + own;
     PF_CUDA_TRY(ensure_dynamic_smem((const void *)prefix_kernel<T, HD>, device, smem0), "prefix_kernel shared memory");
     PF_CUDA_TRY(ensure_dynamic_smem((const void *)attention_kernel<T, HD, NB, true>, device, smem1), "attention_kernel shared memory");
@@ -1038,9 +1047,9 @@ extern "C" int pf_prefix_attention_status(const pf_kv_cache_t *cache, int32_t dt
     a.part = (float *)ws;
     a.own_v = (float *)(ws + z.own_v); a.own_z = (float *)(ws + z.own_z); a.own_l = (float *)(ws + z.own_l);
     a.cu = d_cu_seqs; a.plen = d_prefix_len; p.ptable = d_prefix_table;
-    a.n_groups = n_groups; a.pcols = prefix_cols; p.n_slots = z.n_slots;
+    a.n_groups = n_groups; a.pcols = prefix_cols; p.n_rows = z.n_rows;
     p.status = (uint32_t *)(ws + z.status);
-    p.slots = (float *)(ws + z.slots);
+    p.part_v = (float *)(ws + z.part_v); p.part_z = (float *)(ws + z.part_z); p.part_l = (float *)(ws + z.part_l);
     p.wait_limit = g_wait_limit;
     p.wait_lost = g_wait_lost;
     p.report = d_status;
