@@ -579,11 +579,14 @@ __device__ __forceinline__ bool rows_run(const PrefixArgs &P, const PrefixRoom &
                 tmem_wait_st();
             }
             uint32_t x[8][16];                          // the row's scores
+            auto read_scores = [&]() {
 #pragma unroll
-            for (int c = 0; c < 8; c++) tmem_ld16(score + 16 * c, x[c]);
-            tmem_wait_ld(x[0]);
+                for (int c = 0; c < 8; c++) tmem_ld16(score + 16 * c, x[c]);
+                tmem_wait_ld(x[0]);
 #pragma unroll
-            for (int c = 1; c < 8; c++) tmem_named(x[c]);
+                for (int c = 1; c < 8; c++) tmem_named(x[c]);
+            };
+            read_scores();
             float top = -INFINITY;
 #pragma unroll
             for (int g = 0; g < 8; g++) {
@@ -610,14 +613,21 @@ __device__ __forceinline__ bool rows_run(const PrefixArgs &P, const PrefixRoom &
                 l32 *= a;
                 if (i > 0) {                            // this stream's products in front are done: their end came before the scores'
 #pragma unroll 1
-                    for (int c = 0; c < HD / 16; c++) {
-                        uint32_t o[16];
-                        tmem_ld16(value + 16 * c, o);
-                        tmem_wait_ld(o);
+                    for (int c = 0; c < HD / 64; c++) {
+                        uint32_t o[4][16];
 #pragma unroll
-                        for (int k = 0; k < 16; k++) o[k] = __float_as_uint(__uint_as_float(o[k]) * a);
-                        tmem_st16(value + 16 * c, o);
+                        for (int h = 0; h < 4; h++) tmem_ld16(value + 16 * (4 * c + h), o[h]);
+                        tmem_wait_ld(o[0]);
+#pragma unroll
+                        for (int h = 1; h < 4; h++) tmem_named(o[h]);
+#pragma unroll
+                        for (int h = 0; h < 4; h++) {
+#pragma unroll
+                            for (int k = 0; k < 16; k++) o[h][k] = __float_as_uint(__uint_as_float(o[h][k]) * a);
+                            tmem_st16(value + 16 * (4 * c + h), o[h]);
+                        }
                     }
+                    read_scores();                      // again: their registers were needed (16 columns at a time without them: 341 us instead of 335 for 256 behind 32768)
                 }
             }
             const float ref = z == -INFINITY ? 0.f : z;
