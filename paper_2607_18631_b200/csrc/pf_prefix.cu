@@ -612,22 +612,23 @@ __device__ __forceinline__ bool rows_run(const PrefixArgs &P, const PrefixRoom &
                 l *= a;
                 l32 *= a;
                 if (i > 0) {                            // this stream's products in front are done: their end came before the scores'
+                    constexpr int N = HD / 32;          // half of the columns at a time (all at once, 3 behind 262143 with heads of 64: 156 us, not 143)
 #pragma unroll 1
-                    for (int c = 0; c < HD / 64; c++) {
-                        uint32_t o[4][16];
+                    for (int c = 0; c < HD / (16 * N); c++) {
+                        uint32_t o[N][16];
 #pragma unroll
-                        for (int h = 0; h < 4; h++) tmem_ld16(value + 16 * (4 * c + h), o[h]);
+                        for (int h = 0; h < N; h++) tmem_ld16(value + 16 * (N * c + h), o[h]);
                         tmem_wait_ld(o[0]);
 #pragma unroll
-                        for (int h = 1; h < 4; h++) tmem_named(o[h]);
+                        for (int h = 1; h < N; h++) tmem_named(o[h]);
 #pragma unroll
-                        for (int h = 0; h < 4; h++) {
+                        for (int h = 0; h < N; h++) {
 #pragma unroll
                             for (int k = 0; k < 16; k++) o[h][k] = __float_as_uint(__uint_as_float(o[h][k]) * a);
-                            tmem_st16(value + 16 * (4 * c + h), o[h]);
+                            tmem_st16(value + 16 * (N * c + h), o[h]);
                         }
                     }
-                    read_scores();                      // again: their registers were needed (16 columns at a time without them: 341 us instead of 335 for 256 behind 32768)
+                    read_scores();                      // again: their registers were needed (16 columns at a time without: 342 us, not 336, for 256 behind 32768)
                 }
             }
             const float ref = z == -INFINITY ? 0.f : z;
