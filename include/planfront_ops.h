@@ -85,8 +85,9 @@ int pf_kv_append(const pf_kv_cache_t *cache, int32_t dtype, int32_t n_seq, int64
  * A query element that is not finite makes its own head's out and lse NaN (0 and -infinity where all its scores are
  * -infinity) and no other's.
  * Keys and values are exact, scores, maxima and sums fp32; a token's weight enters the values' sum with 11 bits (fewer below 2^-29 of
- * the row's largest, none below 2^-40; a page's value scale counts with the weight there), and the denominator with all of them.
- * Scales in the cache have to be positive and finite (below 2^-60 a value scale counts as 2^-60).
+ * the row's largest, none below 2^-40; a page's value scale counts with the weight there), and the denominator with all of them (weight times value scale
+ * from 2^-141 of the row's largest such product on).
+ * Scales in the cache have to be positive and at most 2^126 (below 2^-60 a value scale counts as 2^-60).
  * Several query tokens of one sequence are several rows with the same table row and their own lengths.
  * PF_EINVAL: NULL or misaligned pointers, another dtype, page or hd, n_heads not a multiple of n_kv, sm_scale not
  * finite; PF_ERANGE: counts out of range (n_seq <= PF_ATTN_MAX_SEQ; the table's room, n_seq * table_cols * page, below
@@ -102,7 +103,8 @@ int pf_decode_attention(const pf_kv_cache_t *cache, int32_t dtype, int32_t n_seq
  *   (a, b) -> amplitude * (a cos t - b sin t, b cos t + a sin t),   t = p * freq[i] radians;
  * pair i is elements i and i + rot / 2 (PF_ROPE_HALF) or 2 i and 2 i + 1 (PF_ROPE_INTERLEAVED); elements from `rot` on stay as they are.
  * d_phase: rot / 2 words, freq[i] as a fraction of a turn times 2^64 (pf_rotary_phases), so that angles are exact to 2^-32 turns at every
- * 32-bit position, negative ones included.  An element that is not finite spoils its own pair only. */
+ * 32-bit position, negative ones included; their sines and cosines carry 2^-23 of their own size (2^-21.4 of the pair's length for what is then rounded to 8 bits).
+ * An element that is not finite spoils its own pair only. */
 enum { PF_ROPE_HALF = 0, PF_ROPE_INTERLEAVED = 1 };
 #define PF_ROPE_MAX_HD 1024
 #define PF_ROPE_MAX_HEADS 65535
@@ -140,7 +142,7 @@ int pf_kv_append_rope(const pf_kv_cache_t *cache, const pf_rotary_t *rotary, int
  *   out[b, h] = softmax over both of sm_scale * q[b, h] . K[t], times V[t]
  * d_cu_seqs: n_groups + 1 offsets that do not decrease (NULL, with one group: all sequences); a sequence in no group sees its own tokens only.  Prefixes of any length, and tables, lengths,
  * missing pages, scales, q, out and lse otherwise as in pf_decode_attention.  A row that sees no token gives zeros and -infinity.
- * Weights enter the values' sum with the bits that they have there.
+ * Weights enter the values' sum with the bits that they have there; scores of any finite size are taken.
  * A wait inside the kernel that runs out makes the rows that it concerns NaN; pf_prefix_attention_status says so too: one int32 of device memory, 0 after a
  * complete call, 1 otherwise (d_status may be NULL: pf_prefix_attention).
  * Values are added up in 32 bits over 65536 tokens at a time, more in calls of more than 4.8 million (tile of rows, 128 tokens) pairs.

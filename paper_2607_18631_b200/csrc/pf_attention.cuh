@@ -99,8 +99,9 @@ __device__ __forceinline__ Group group_of(const AttnArgs &A, int g)
     r.tiles = (r.len + kTok - 1) / kTok;
     return r;
 }
-// The kernel for prefixes and this one run side by side: SMs that the former takes, given both lists' tiles.  One of its tiles takes an SM 1.4 us (up to 128 rows) to
-// 2.5 us, one of this kernel's 0.23 us; cut by the sum of these, both end at about the same time, and neither waits for the other's start and end.
+// The kernel for prefixes and this one run side by side: SMs that the former takes, given both lists' tiles.  With heads of 128 and up to 8 of them a key head, one of its tiles takes an SM 1.4 us (up to
+// 128 rows) to 2.5 us, one of this kernel's 0.23 us; a tile of either height counts as 9 of this kernel's, for every head size, and SMs are rounded to the nearest.  So the two end together only for
+// tall tiles: with 65 rows a group and key head (seven groups of 13) the prefixes' SMs are done after two thirds of the time, and where own tokens need 1.5 SMs they get one or two.
 __device__ __forceinline__ int prefix_share(long long units, long long own_tiles, int sms)
 {
     if (units == 0) return 0;

@@ -15,12 +15,13 @@
 // 2^15.9: tensor memory's values are scaled anew in the first tiles of a piece for the most part.  Warps have one role each and meet at barriers in shared memory:
 //   plan -> copy (bulk, half tiles) -> widen -> products <-> rows.
 // What bounds it.  Many rows: 128 x 128 scores take the products 1024 cycles, the special-function unit 768 (a quarter of the powers are polynomials) and shared memory
-// 1280 (operands 768, the cache's bytes in, out and widened 1024 a tile that two streams share), and the chain scores -> largest -> powers -> products of a stream 3900, of which the
-// other stream fills a half: 256 sequences of 64 / 8 heads of 128 behind 32768 tokens 321 us (863 TFLOP/s; tensor pipe 39 % active, issue slots 47 %).  Few rows: a tile's way through copy,
-// widen and products, 2450 cycles against 1400 from HBM: 3 such sequences behind 262143 tokens 168 us (3.2 TB/s).
+// 1280 (operands 768, the cache's bytes in, out and widened 1024 a tile that two streams share), and the chain scores -> largest -> powers -> products of a stream some 4000, of which the
+// other stream fills a half: 256 sequences of 64 / 8 heads of 128 behind 32768 tokens 336 us (825 TFLOP/s; behind 8192 the tensor pipe is 36 % active, issue slots 45 %).  Few rows: a tile's way
+// through copy, widen and products, some 2350 cycles against 1400 from HBM: 3 such sequences behind 262143 tokens 162 us (3.3 TB/s).
 // Measured on the way there (us, these two): rows' scores read twice, one widening role that also loads: 594, 442; scores kept in registers, registers moved to the groups that need
 // them: 394, 198; a whole warp in the products' loop: 373; packed arithmetic, polynomials, half tiles of weights handed over: 353; bulk copies, roles apart: 344, 177; own tokens
-// beside the prefixes: 322; less code in what every tile goes through: 171.  Not kept: 16 warps for the rows (two a row, 350), two warps for the products (386), eight
+// beside the prefixes: 322; less code in what every tile goes through: 171; whole tiles widened without a look at their pages: 161 (few rows); references 15 below the largest score instead of
+// 7, for the small weights' bits, and a way for scores at which fp32 is coarse: 336, 162.  Not kept: 16 warps for the rows (two a row, 350), two warps for the products (386), eight
 // warps that widen (344), four places for half tiles where few rows leave room (360, 207), few rows several times over for a part of a tile each (332, 211).
 #include <math.h>
 
